@@ -383,10 +383,10 @@ def run(s):
         if train:
             out.update(zip(("dq", "dk"), mg.moga_rotary_bwd(s["dq"], s["dk"], s["pos"], s["freqs"], **how)))
         return out
-    o, o2, lse = mg.moga_diff_attn_fwd(s["q"], s["k"], s["v"], s["lam"], s["cu_q"], s["cu_k"], s["scale"], want_second=train)
+    o, parts, lse = mg.moga_diff_attn_fwd(s["q"], s["k"], s["v"], s["lam"], s["cu_q"], s["cu_k"], s["scale"], want_parts=train)
     out = {"o": o}
     if train:
-        dq, dk, dv, dlam = mg.moga_diff_attn_bwd(s["do"], s["q"], s["k"], s["v"], o, o2, lse, s["lam"], s["cu_q"], s["cu_k"], s["scale"])
+        dq, dk, dv, dlam = mg.moga_diff_attn_bwd(s["do"], s["q"], s["k"], s["v"], parts, lse, s["lam"], s["cu_q"], s["cu_k"], s["scale"])
         out.update(dq=dq, dk=dk, dv=dv, dlam=dlam)
     return out
 
