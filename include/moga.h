@@ -61,7 +61,10 @@ typedef enum {
   MOGA_OP_VARLEN_ATTN_BWD = 7, /* N = Nq, M = G */
   MOGA_OP_ATTN_BWD_JOINT = 8,  /* moga_group_attn_bwd_joint, moga_group_attn_bwd_tokens_joint */
   MOGA_OP_ATTN_FWD_CALL = 9,   /* one of the calls of moga_varlen_attn_fwd_calls; N = Nq, M = G */
-  MOGA_OP_FUSED_ATTN_BWD = 10  /* moga_fused_attn_bwd (the bytes of MOGA_OP_ATTN_BWD) */
+  MOGA_OP_FUSED_ATTN_BWD = 10, /* moga_fused_attn_bwd (the bytes of MOGA_OP_ATTN_BWD) */
+  MOGA_OP_DIFF_ATTN_FWD = 11,  /* N = Nq, M = G */
+  MOGA_OP_DIFF_ATTN_BWD = 12,  /* N = Nq, M = G */
+  MOGA_OP_LAYER_NORM_BWD = 13  /* M = 1, d_model = C */
 } moga_op;
 
 /* Human-readable name of a status code (static storage, never NULL). */
@@ -540,6 +543,99 @@ int moga_balance_loss(const int32_t* group, const float* gate, int64_t N, int M,
 int moga_balance_loss_bwd(const int32_t* group, const float* frac, int64_t N, int M, float alpha,
                           float d_loss, const float* d_loss_device_or_null, int accumulate,
                           float* d_gate, void* stream);
+
+/*
+ * Layer norm over the last axis of x [N, C]: the hidden state before the router and the projections (C = d_model), or the rows of single
+ * heads (Q and K before the rotation: N = tokens * H, C = D).
+ *   y = (x - mean) * rstd * weight + bias,  mean = mean_c x,  rstd = 1 / sqrt(mean_c (x - mean)^2 + eps)
+ * weight, bias [C] fp32, each NULL for none; mean, rstd [N] fp32, both or neither (the backward needs them).  dtype F32 or BF16 (x and y),
+ * C in [1, 16384], eps finite and >= 0.  fp32 statistics, one rounding of y.
+ */
+int moga_layer_norm_fwd(const void* x, int dtype, const float* weight_or_null, const float* bias_or_null, int64_t N, int C, float eps,
+                        void* y, float* mean_or_null, float* rstd_or_null, void* stream);
+
+/*
+ * Backward of moga_layer_norm_fwd, with xh = (x - mean) * rstd and g = d_y * weight:
+ *   d_x = rstd * (g - mean_c g - xh * mean_c(g * xh));  d_weight = sum_n d_y * xh;  d_bias = sum_n d_y        fp32, [C]
+ * d_weight, d_bias: each NULL to skip; of N == 0 rows they are zeros.  Sums in a fixed order: results repeat bit by bit.
+ * Workspace: MOGA_OP_LAYER_NORM_BWD (not needed without d_weight and d_bias).
+ */
+int moga_layer_norm_bwd(const void* d_y, const void* x, int dtype, const float* weight_or_null, const float* mean, const float* rstd,
+                        int64_t N, int C, void* d_x, float* d_weight_or_null, float* d_bias_or_null, void* ws, size_t ws_bytes,
+                        void* stream);
+
+/*
+ * Rotary positions.  The first R channels of a head (R even, R <= D; the others are copied) are R / 2 pairs: channels (2 i, 2 i + 1) if
+ * interleaved, else (i, i + R / 2).  Pair i of a token at position p is turned by the angle p * inv_freq[i] and multiplied by factor:
+ *   y1 = factor * (x1 cos - x2 sin),  y2 = factor * (x2 cos + x1 sin)
+ * positions [axes, N] int32 (any value), axes in [1, 4]: axis a turns the next axis_pairs[a] pairs (axis_pairs: a HOST array whose sum is
+ * R / 2, NULL for one axis), e.g. (frame, row, column) of a latent grid.  inv_freq [R / 2] double on the device (moga_rotary_build_freqs per
+ * axis, one after the other).  Angles are reduced in 64 bits, so that far positions keep their accuracy.
+ * q, qo [N, Hq, D], k, ko [N, Hk, D] token order; Hq or Hk may be 0 (then its pointers are ignored).  D a multiple of 8, at most 256;
+ * dtype F32 or BF16; N < 2^28.  Outputs must not alias inputs.
+ */
+int moga_rotary_fwd(const void* q, const void* k, int dtype, int64_t N, int Hq, int Hk, int D, const int32_t* positions, int axes,
+                    const int* axis_pairs_or_null, const double* inv_freq, int R, int interleaved, float factor, void* qo, void* ko,
+                    void* stream);
+/* Backward of moga_rotary_fwd: the gradients turned back by the same angles, times factor. */
+int moga_rotary_bwd(const void* d_qo, const void* d_ko, int dtype, int64_t N, int Hq, int Hk, int D, const int32_t* positions, int axes,
+                    const int* axis_pairs_or_null, const double* inv_freq, int R, int interleaved, float factor, void* d_q, void* d_k,
+                    void* stream);
+
+/*
+ * The rotation on the way into the groups' order: moga_rotary_fwd of q and k followed by the gather of moga_permute, in one launch that
+ * moves no more bytes than the gather.  perm [N] as written by moga_permute (which may be called with NULL q, k, v):
+ *   qh[h][j] = rotated q[perm[j]][h] (kh alike), vh[h][j] = v[perm[j]][h]        [H, N, D]
+ * positions are those of the tokens (positions[a][token]).  The same bits as the two calls.
+ */
+int moga_rotary_permute_fwd(const void* q, const void* k, const void* v, int dtype, int64_t N, int H, int D, const int32_t* perm,
+                            const int32_t* positions, int axes, const int* axis_pairs_or_null, const double* inv_freq, int R,
+                            int interleaved, float factor, void* qh, void* kh, void* vh, void* stream);
+/* Its backward: d_qh, d_kh, d_vh [H, N, D] -> d_q, d_k, d_v [N, H, D]. */
+int moga_rotary_permute_bwd(const void* d_qh, const void* d_kh, const void* d_vh, int dtype, int64_t N, int H, int D,
+                            const int32_t* perm, const int32_t* positions, int axes, const int* axis_pairs_or_null,
+                            const double* inv_freq, int R, int interleaved, float factor, void* d_q, void* d_k, void* d_v, void* stream);
+
+/*
+ * Angles per position of R / 2 pairs, on the HOST, in 64 bits: inv_freq[i] = base^(-2 i / R) (inv_freq: HOST array of R / 2), for contexts
+ * scale_factor (>= 1) times as long as the original one
+ *   PLAIN:  as they are (the other arguments are not read)
+ *   LINEAR: divided by scale_factor
+ *   BASE:   base raised to base * scale_factor^(R / (R - 2)), so that the last pair is divided by scale_factor and the first is as it was
+ *   PARTS:  a pair that turns beta_fast times or more over original_len positions is as it was, one that turns beta_slow times or fewer is
+ *           divided by scale_factor, those between are blended by their turns; *factor (HOST) = 0.1 ln(scale_factor) + 1, else 1
+ */
+typedef enum { MOGA_ROTARY_PLAIN = 0, MOGA_ROTARY_LINEAR = 1, MOGA_ROTARY_BASE = 2, MOGA_ROTARY_PARTS = 3 } moga_rotary_scaling;
+int moga_rotary_build_freqs(int R, double base, int scaling, double scale_factor, double original_len, double beta_fast, double beta_slow,
+                            double* inv_freq, float* factor);
+
+/*
+ * Differential attention inside groups: the difference of two attention maps, one from the first and one from the second half of a head's
+ * channels of Q and K, over the same values (Q = [Q1 | Q2], K = [K1 | K2] of D / 2 channels each):
+ *   A_m = softmax(softmax_scale * Q_m K_m^T) inside a group,   oh = A_1 vh - lambda[h] * A_2 vh
+ *   parts[m] = A_m vh  [2, H, Nq, D] fp32 (NULL to skip; the backward needs it)
+ *   lse[m][h][j] = log sum_k exp(softmax_scale * Q_m . K_m)  [2, H, Nq] fp32
+ * Layouts, groups (cu_seqlens_q, cu_seqlens_k, G), types, limits and rows without keys (oh = parts = 0, lse = -inf) as for
+ * moga_varlen_attn_fwd (fp32 too: fewer than 2^24 rows); cu_seqlens_k == cu_seqlens_q and Nk == Nq for MoGA's groups, one query per group for
+ * a step of serving.  Output rows behind the last group's are left as they are.  lambda [H] fp32 on the device, of any sign.  softmax_scale: usually (D / 2)^-0.5.
+ * Workspace: MOGA_OP_DIFF_ATTN_FWD (0 up to MOGA_MAX_GROUPS groups); with moga_workspace_preferred_bytes the keys of calls of few queries
+ * are split over the chip (rounding differs between the two).
+ */
+int moga_diff_attn_fwd(const void* qh, const void* kh, const void* vh, int dtype, int64_t Nq, int64_t Nk, int H, int D,
+                       const float* lambda, const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, int G, float softmax_scale,
+                       void* oh, float* parts_or_null, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Backward of moga_diff_attn_fwd, per group and head, with P_m = exp(scale * S_m - lse_m) and dP = d_oh vh^T:
+ *   delta_m = rowsum(d_oh * (P_m vh));  dS_1 = P_1 * (dP - delta_1);  dS_2 = -lambda * P_2 * (dP - delta_2)
+ *   d_qh_m = scale * dS_m K_m;  d_kh_m = scale * dS_m^T Q_m;  d_vh = (P_1 - lambda P_2)^T d_oh;  d_lambda[h] = -sum P_2 * dP     [H] fp32
+ * Keys of a group without queries, and queries of a group without keys, get zero gradients.  Sums in a fixed order: results repeat bit
+ * by bit.  Workspace: MOGA_OP_DIFF_ATTN_BWD.
+ */
+int moga_diff_attn_bwd(const void* d_oh, const void* qh, const void* kh, const void* vh, const float* parts,
+                       const float* lse, int dtype, int64_t Nq, int64_t Nk, int H, int D, const float* lambda,
+                       const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, int G, float softmax_scale, void* d_qh, void* d_kh,
+                       void* d_vh, float* d_lambda, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -18,3 +18,23 @@ def moga_attention(x, w, q, k, v, softmax_scale, balance_alpha=None, grad_x=Fals
     """x [N, d_model], w [M, d_model] fp32, q/k/v [N, H, D] -> (o [N, H, D], balancing loss or None, group [N])."""
     o, loss, group = mg._nat.attention(x, w, q, k, v, softmax_scale, balance_alpha, grad_x)
     return o, (loss if balance_alpha is not None else None), group
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-6):
+    """Layer norm over the last axis of x [..., C] (contiguous), weight and bias f32 [C] or None -> y like x."""
+    return mg._nat.layer_norm(x, weight, bias, eps)
+
+
+def rotary(q, k, positions, inv_freq, axis_pairs=None, interleaved=False, factor=1.0):
+    """Rotary positions of q [N, Hq, D] and k [N, Hk, D] (binding.moga_rotary_fwd) -> (qo, ko)."""
+    return mg._nat.rotary_apply(q, k, positions, inv_freq, axis_pairs or [], interleaved, factor)
+
+
+def moga_diff_attention(x, w, q, k, v, lam, softmax_scale, balance_alpha=None, grad_x=False, positions=None, inv_freq=None, axis_pairs=None,
+                        interleaved=False, factor=1.0):
+    """moga_attention with differential attention in the groups: the two halves of a head's channels are two maps, lam f32 [H] the weight of
+    the second (moga_diff_attn_fwd); gradients flow to lam as well.  With positions and inv_freq (binding.moga_rotary_freqs) q and k are
+    rotated on their way into the groups.  -> (o [N, H, D], balancing loss or None, group [N])."""
+    o, loss, group = mg._nat.diff_attention(x, w, q, k, v, lam, softmax_scale, balance_alpha, grad_x, positions, inv_freq, axis_pairs or [],
+                                            interleaved, factor)
+    return o, (loss if balance_alpha is not None else None), group

@@ -21,11 +21,14 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmoga.so")
 
 MOGA_F32, MOGA_BF16 = 0, 1
+ROTARY_SCALINGS = {None: 0, "linear": 1, "base": 2, "parts": 3}
 (OP_ROUTE, OP_PERMUTE, OP_ATTN_FWD, OP_ATTN_BWD, OP_ROUTE_BWD, OP_BALANCE_LOSS, OP_VARLEN_ATTN_FWD,
- OP_VARLEN_ATTN_BWD, OP_ATTN_BWD_JOINT, OP_ATTN_FWD_CALL, OP_FUSED_ATTN_BWD) = range(11)
+ OP_VARLEN_ATTN_BWD, OP_ATTN_BWD_JOINT, OP_ATTN_FWD_CALL, OP_FUSED_ATTN_BWD, OP_DIFF_ATTN_FWD, OP_DIFF_ATTN_BWD,
+ OP_LAYER_NORM_BWD) = range(14)
 
 _c = ctypes
 _vp, _i64, _i32, _f32, _sz = _c.c_void_p, _c.c_int64, _c.c_int, _c.c_float, _c.c_size_t
+_f64 = _c.c_double
 _SIGNATURES = {
     "moga_status_string": (_c.c_char_p, [_i32]),
     "moga_version": (_i32, []),
@@ -91,6 +94,18 @@ _SIGNATURES = {
                                     _vp, _vp, _vp, _vp, _sz, _vp]),
     "moga_balance_loss": (_i32, [_vp, _vp, _i64, _i32, _f32, _vp, _vp, _vp, _vp, _sz, _vp]),
     "moga_balance_loss_bwd": (_i32, [_vp, _vp, _i64, _i32, _f32, _f32, _vp, _i32, _vp, _vp]),
+    "moga_layer_norm_fwd": (_i32, [_vp, _i32, _vp, _vp, _i64, _i32, _f32, _vp, _vp, _vp, _vp]),
+    "moga_layer_norm_bwd": (_i32, [_vp, _vp, _i32, _vp, _vp, _vp, _i64, _i32, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "moga_rotary_fwd": (_i32, [_vp, _vp, _i32, _i64, _i32, _i32, _i32, _vp, _i32, _vp, _vp, _i32, _i32, _f32, _vp, _vp, _vp]),
+    "moga_rotary_bwd": (_i32, [_vp, _vp, _i32, _i64, _i32, _i32, _i32, _vp, _i32, _vp, _vp, _i32, _i32, _f32, _vp, _vp, _vp]),
+    "moga_rotary_permute_fwd": (_i32, [_vp, _vp, _vp, _i32, _i64, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _i32, _i32, _f32, _vp, _vp, _vp,
+                                       _vp]),
+    "moga_rotary_permute_bwd": (_i32, [_vp, _vp, _vp, _i32, _i64, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _i32, _i32, _f32, _vp, _vp, _vp,
+                                       _vp]),
+    "moga_rotary_build_freqs": (_i32, [_i32, _f64, _i32, _f64, _f64, _f64, _f64, _vp, _vp]),
+    "moga_diff_attn_fwd": (_i32, [_vp, _vp, _vp, _i32, _i64, _i64, _i32, _i32, _vp, _vp, _vp, _i32, _f32, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "moga_diff_attn_bwd": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i64, _i64, _i32, _i32, _vp, _vp, _vp, _i32, _f32, _vp, _vp, _vp,
+                                  _vp, _vp, _sz, _vp]),
 }
 EXPORTS = tuple(_SIGNATURES)
 
@@ -412,6 +427,63 @@ def moga_balance_loss_bwd(group, frac, alpha, d_loss=1.0, d_gate=None, stream=No
     `d_loss`: a Python number, or a one-element fp32 device tensor (read by the kernel: no host sync)."""
     host, dev = (1.0, d_loss) if isinstance(d_loss, torch.Tensor) else (float(d_loss), None)
     return _nat.balance_loss_bwd(group, frac, alpha, host, dev, d_gate, _st(stream))
+
+
+def moga_layer_norm_fwd(x, weight=None, bias=None, eps=1e-6, want_stats=True, stream=None):
+    """x [N, C], weight and bias f32 [C] -> (y [N, C], mean f32 [N] | None, rstd f32 [N] | None)"""
+    return _nat.layer_norm_fwd(x, weight, bias, eps, want_stats, _st(stream))
+
+
+def moga_layer_norm_bwd(d_y, x, weight, mean, rstd, want_dw=True, stream=None):
+    """-> (d_x [N, C], d_weight f32 [C] | None, d_bias f32 [C] | None)"""
+    return _nat.layer_norm_bwd(d_y, x, weight, mean, rstd, want_dw, _st(stream))
+
+
+def moga_rotary_freqs(rot_dims, base=10000.0, scaling=None, scale_factor=1.0, original_len=0.0, beta_fast=32.0, beta_slow=1.0, device="cuda"):
+    """Radians per position of every pair, for `rot_dims` channels (a number, or one for each axis, one axis after the other)
+    -> (inv_freq f64 [sum / 2] on `device`, factor).  scaling: None, "linear", "base" or "parts" (moga_rotary_build_freqs)."""
+    import numpy as np
+    dims = [int(rot_dims)] if isinstance(rot_dims, int) else [int(d) for d in rot_dims]
+    if scaling not in ROTARY_SCALINGS:
+        raise ValueError(f"scaling {scaling!r}: one of {list(ROTARY_SCALINGS)}")
+    parts, factor = [], ctypes.c_float(1.0)
+    for d in dims:
+        f = np.empty(max(d, 0) // 2, np.float64)
+        st = load().moga_rotary_build_freqs(d, base, ROTARY_SCALINGS[scaling], scale_factor, original_len, beta_fast, beta_slow,
+                                            f.ctypes.data_as(ctypes.c_void_p), ctypes.byref(factor))
+        _check("moga_rotary_build_freqs", st)
+        parts.append(f)
+    return torch.from_numpy(np.concatenate(parts)).to(device), factor.value
+
+
+def moga_rotary_fwd(q, k, positions, inv_freq, axis_pairs=None, interleaved=False, factor=1.0, stream=None):
+    """q [N, Hq, D], k [N, Hk, D] (or None), positions i32 [N] or [axes, N], inv_freq f64 [R / 2] -> (qo, ko)"""
+    return _nat.rotary(q, k, positions, inv_freq, axis_pairs or [], interleaved, factor, False, _st(stream))
+
+
+def moga_rotary_bwd(d_qo, d_ko, positions, inv_freq, axis_pairs=None, interleaved=False, factor=1.0, stream=None):
+    """-> (d_q, d_k)"""
+    return _nat.rotary(d_qo, d_ko, positions, inv_freq, axis_pairs or [], interleaved, factor, True, _st(stream))
+
+
+def moga_rotary_permute_fwd(q, k, v, perm, positions, inv_freq, axis_pairs=None, interleaved=False, factor=1.0, stream=None):
+    """moga_rotary_fwd of q and k and the gather of moga_permute in one launch: q, k, v [N, H, D] -> (qh, kh, vh [H, N, D])"""
+    return _nat.rotary_permute(q, k, v, perm, positions, inv_freq, axis_pairs or [], interleaved, factor, False, _st(stream))
+
+
+def moga_rotary_permute_bwd(d_qh, d_kh, d_vh, perm, positions, inv_freq, axis_pairs=None, interleaved=False, factor=1.0, stream=None):
+    """-> (d_q, d_k, d_v) each [N, H, D]"""
+    return _nat.rotary_permute(d_qh, d_kh, d_vh, perm, positions, inv_freq, axis_pairs or [], interleaved, factor, True, _st(stream))
+
+
+def moga_diff_attn_fwd(qh, kh, vh, lam, cu_seqlens_q, cu_seqlens_k, softmax_scale, want_parts=True, stream=None):
+    """qh [H, Nq, D]; kh, vh [H, Nk, D]; lam f32 [H] -> (oh [H, Nq, D], parts f32 [2, H, Nq, D] | None, lse f32 [2, H, Nq])"""
+    return _nat.diff_attn_fwd(qh, kh, vh, lam, cu_seqlens_q, cu_seqlens_k, softmax_scale, want_parts, _st(stream))
+
+
+def moga_diff_attn_bwd(d_oh, qh, kh, vh, parts, lse, lam, cu_seqlens_q, cu_seqlens_k, softmax_scale, stream=None):
+    """-> (d_qh [H, Nq, D], d_kh, d_vh [H, Nk, D], d_lam f32 [H])"""
+    return _nat.diff_attn_bwd(d_oh, qh, kh, vh, parts, lse, lam, cu_seqlens_q, cu_seqlens_k, softmax_scale, _st(stream))
 
 
 def moga_forward(x, w, q, k, v, softmax_scale, want_probs=True, stream=None):

@@ -9,6 +9,9 @@ extern "C" size_t moga_attn_bwd_ws_bytes(int64_t N, int H, int D, int dtype);
 extern "C" size_t moga_balance_ws_bytes(int M);
 extern "C" size_t moga_varlen_attn_fwd_ws_bytes(int G);
 extern "C" size_t moga_varlen_attn_bwd_ws_bytes(int64_t Nq, int H, int G);
+extern "C" size_t moga_diff_attn_fwd_ws_bytes(int G);
+extern "C" size_t moga_diff_attn_bwd_ws_bytes(int64_t Nq, int H, int G);
+extern "C" size_t moga_layer_norm_bwd_ws_bytes(int64_t N, int C, int dtype);
 
 extern "C" const char* moga_status_string(int status) {
   switch (status) {
@@ -47,6 +50,9 @@ extern "C" size_t moga_workspace_bytes(int op, int64_t N, int H, int D, int M, i
     case MOGA_OP_VARLEN_ATTN_FWD:
     case MOGA_OP_ATTN_FWD_CALL: return moga_varlen_attn_fwd_ws_bytes(M);
     case MOGA_OP_VARLEN_ATTN_BWD: return moga_varlen_attn_bwd_ws_bytes(N, H, M);
+    case MOGA_OP_DIFF_ATTN_FWD: return moga_diff_attn_fwd_ws_bytes(M);
+    case MOGA_OP_DIFF_ATTN_BWD: return moga_diff_attn_bwd_ws_bytes(N, H, M);
+    case MOGA_OP_LAYER_NORM_BWD: return moga_layer_norm_bwd_ws_bytes(N, d_model, dtype);
     default: return 0;
   }
 }

@@ -1,0 +1,609 @@
+// Differential attention inside groups, forward and backward (diff_attn.h has the formulas of the forward).
+//
+// Backward, with lse_m, P_m = exp(s S_m - lse_m), O_m = P_m V and dP = dO V^T, which both maps share:
+//   delta_m = rowsum(dO * O_m)
+//   dS_1 = P_1 * (dP - delta_1), dS_2 = -lambda P_2 * (dP - delta_2), dQ_m = s dS_m K_m, dK_m = s dS_m^T Q_m
+//   dV = (P_1 - lambda P_2)^T dO, dlambda = -sum P_2 * dP
+// so that a backward has the matrix products of plain attention, and a forward one and a half times them (two weighted sums of V).
+#include <algorithm>
+#include <cmath>
+
+#include "diff_attn.h"
+
+namespace moga {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+template <typename T> constexpr int kCols = sizeof(T) == 4 ? 1 : 2;   // columns of 16 rows of a wave
+template <typename T> constexpr int kRows = 64 * kCols<T>;            // rows of a block of four waves
+
+struct DiffFwd {
+  const void *q, *k, *v;
+  const float* lambda;
+  const int32_t *cu_q, *cu_k, *tile_start;
+  int64_t Nq, Nk;
+  int H, G;
+  float scale;
+  void* o;
+  float* parts;   // NULL, or O_1 and O_2 as they are, [2][H][Nq][D]
+  float* lse;     // [2][H][Nq]
+  // split: pieces of a tile's keys, [piece][H][Nq] rows of two maps' fp32 sums, and of their (maximum, sum)
+  float *part, *stat;
+};
+
+// Running maximum of the exponents, sums of the weights, and sums of V: columns of a wave, both maps.
+template <int D, int NC> struct DiffState {
+  floatx4_t o[2][D / 16][NC];
+  float m[2][NC], l[2][NC], thresh[2][NC];
+};
+
+// One step: 32 keys.  left: keys of the tile that exist.
+template <typename T, int D, int NC, typename Tiles>
+__device__ __forceinline__ void diff_fwd_step(const Tiles& tiles, const Frag<T> (&qf)[NC][D / 32], DiffState<D, NC>& st, float c, int left) {
+  constexpr int KB = D / 64;   // k blocks of a map
+  const int g = (threadIdx.x & 63) >> 4;
+  Frag<T> pf[2][NC];
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    floatx4_t s[2][NC];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const Frag<T> a = tiles.nat(0, t, m * KB + kb);
+#pragma unroll
+        for (int q = 0; q < NC; ++q) s[t][q] = mma(a, qf[q][m * KB + kb], kb == 0 ? floatx4_t{0.f, 0.f, 0.f, 0.f} : s[t][q]);
+      }
+    float x[NC][8], mx[NC];
+    bool up = false;
+#pragma unroll
+    for (int q = 0; q < NC; ++q) {
+      mx[q] = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[q][i] = fmaf(s[i >> 2][q][i & 3], c, -st.m[m][q]);
+        if (left < 32 && 8 * g + i >= left) x[q][i] = -INFINITY;
+        mx[q] = fmaxf(mx[q], x[q][i]);
+      }
+      up = up || mx[q] > st.thresh[m][q];
+    }
+    // The maximum is raised when a weight would exceed 2^8 only: rare after the first step.
+    if (__builtin_amdgcn_ballot_w64(up) != 0) {
+#pragma unroll
+      for (int q = 0; q < NC; ++q) {
+        float all = fmaxf(mx[q], __shfl_xor(mx[q], 16, kWave));
+        all = fmaxf(all, __shfl_xor(all, 32, kWave));
+        const bool first = st.thresh[m][q] == -INFINITY;
+        const float by = first ? (all == -INFINITY ? 0.f : all) : fmaxf(all, 0.f);
+        const float alpha = first ? 0.f : fast_exp2(-by);
+        if (all != -INFINITY) st.thresh[m][q] = 8.f;
+        st.m[m][q] += by;
+        st.l[m][q] *= alpha;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[q][i] -= by;
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) st.o[m][dt][q] *= alpha;
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < NC; ++q) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[q][i] = fast_exp2(x[q][i]);
+      // sums of the weights in 32 bits, before they are rounded: the log-sum-exp is exact enough for the gradient of lambda
+      st.l[m][q] += ((x[q][0] + x[q][1]) + (x[q][2] + x[q][3])) + ((x[q][4] + x[q][5]) + (x[q][6] + x[q][7]));
+      make_frag(pf[m][q], x[q]);
+    }
+  }
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) {
+    const Frag<T> a = tiles.tr(1, dt);
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int q = 0; q < NC; ++q) st.o[m][dt][q] = mma(a, pf[m][q], st.o[m][dt][q]);
+  }
+}
+
+// A tile of kRows queries, or (SPLIT) blockIdx.y's share of its keys.
+template <typename T, int D, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void diff_fwd_kernel(DiffFwd a) {
+  constexpr int NC = kCols<T>;
+  __shared__ typename DiffTiles<T, D>::Lds lds;
+  WorkTile w;
+  if (!find_work<false>(a.cu_q, a.tile_start, a.G, a.H, kRows<T>, blockIdx.x, w)) return;
+  const int head = w.head, ge = w.ti.row_end;
+  int gs = a.cu_k[w.ti.group], n = a.cu_k[w.ti.group + 1] - gs;
+  if constexpr (SPLIT) {   // whole tiles of 32 keys, as evenly as they go
+    const int64_t tiles = (n + 31) >> 5;
+    const int t0 = (int)(tiles * blockIdx.y / gridDim.y), t1 = (int)(tiles * (blockIdx.y + 1) / gridDim.y);
+    const int end = min(n, 32 * t1);
+    gs += 32 * t0;
+    n = end - 32 * t0;
+  }
+  gs = __builtin_amdgcn_readfirstlane(gs);
+  n = __builtin_amdgcn_readfirstlane(n);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  const int row0 = w.ti.tile_row + 16 * NC * wave;
+  const int64_t head_q = (int64_t)head * a.Nq, head_k = (int64_t)head * a.Nk;
+  const bool active = row0 < ge;
+
+  DiffState<D, NC> st;
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int q = 0; q < NC; ++q) {
+      st.m[m][q] = st.l[m][q] = 0.f;
+      st.thresh[m][q] = -INFINITY;
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) st.o[m][dt][q] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+    }
+  if (n > 0) {
+    Frag<T> qf[NC][D / 32];
+    diff_columns<T, D, NC>(qf, (const T*)a.q, row0, ge, head_q);
+    const float c = a.scale * kLog2e;
+    DiffTiles<T, D> tiles;
+    tiles.start(lds, (const T*)a.k + (head_k + gs) * D, (const T*)a.v + (head_k + gs) * D, n);
+    const int steps = (n + 31) >> 5;
+    for (int s = 0; s < steps; ++s) {
+      tiles.ready(s);
+      if (active) diff_fwd_step<T, D, NC>(tiles, qf, st, c, n - 32 * s);
+    }
+    tiles.finish();
+  }
+  if (!active) return;
+#pragma unroll
+  for (int q = 0; q < NC; ++q) {
+    const int row = row0 + 16 * q + r;
+    float l[2];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      l[m] = st.l[m][q] + __shfl_xor(st.l[m][q], 16, kWave);
+      l[m] += __shfl_xor(l[m], 32, kWave);
+    }
+    if (row >= ge) continue;
+    if constexpr (SPLIT) {
+      const int64_t at = ((int64_t)blockIdx.y * a.H * a.Nq + head_q + row) * 2;
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) store4(a.part + (at + m) * D, dt, st.o[m][dt][q]);
+        if (g == 0) *(floatx2_t*)(a.stat + (at + m) * 2) = floatx2_t{st.thresh[m][q] == -INFINITY ? -INFINITY : st.m[m][q], n > 0 ? l[m] : -1.f};
+      }
+    } else {
+      const float inv1 = n > 0 ? 1.f / l[0] : 0.f, inv2 = n > 0 ? 1.f / l[1] : 0.f, lam = a.lambda[head];
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) {
+        const floatx4_t o1 = st.o[0][dt][q] * inv1, o2 = st.o[1][dt][q] * inv2;
+        store4((T*)a.o + (head_q + row) * D, dt, o1 - o2 * lam);
+        if (a.parts) {
+          store4(a.parts + (head_q + row) * D, dt, o1);
+          store4(a.parts + ((int64_t)a.H * a.Nq + head_q + row) * D, dt, o2);
+        }
+      }
+      if (g == 0)
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+          a.lse[(int64_t)m * a.H * a.Nq + head_q + row] = n > 0 ? logf(l[m]) + st.m[m][q] * 0.6931471805599453f : -INFINITY;
+    }
+  }
+}
+
+// The pieces of a row put together: a wave per row, D / 64 channels of both maps per lane.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void diff_merge_kernel(DiffFwd a, int pieces) {
+  constexpr int V = D / 64;
+  const int lane = threadIdx.x & 63;
+  const int64_t rows = (int64_t)a.H * a.Nq, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= rows || row % a.Nq >= a.cu_q[a.G]) return;   // rows behind the last group stay as they are
+  float o[2][V], lse[2];
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    float mx = -INFINITY, l = 0.f;
+    bool empty = true;
+    for (int p = 0; p < pieces; ++p) mx = fmaxf(mx, a.stat[((p * rows + row) * 2 + m) * 2]);
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[m][i] = 0.f;
+    for (int p = 0; p < pieces; ++p) {
+      const int64_t at = (p * rows + row) * 2 + m;
+      const floatx2_t s = *(const floatx2_t*)(a.stat + at * 2);
+      if (s[1] == -1.f) continue;   // no keys
+      empty = false;
+      const float f = mx == -INFINITY ? 1.f : fast_exp2(s[0] - mx);
+      l = fmaf(s[1], f, l);
+#pragma unroll
+      for (int i = 0; i < V; ++i) o[m][i] = fmaf(a.part[at * D + lane * V + i], f, o[m][i]);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[m][i] = empty ? 0.f : o[m][i] / l;
+    lse[m] = empty ? -INFINITY : logf(l) + mx * 0.6931471805599453f;
+  }
+  const float lam = a.lambda[row / a.Nq];
+  T* out = (T*)a.o + row * D + lane * V;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const float v = o[0][i] - lam * o[1][i];
+    if constexpr (sizeof(T) == 4) out[i] = v;
+    else out[i] = f32_to_bf16_bits(v);
+    if (a.parts) {
+      a.parts[row * D + lane * V + i] = o[0][i];
+      a.parts[(rows + row) * D + lane * V + i] = o[1][i];
+    }
+  }
+  if (lane < 2) a.lse[lane * rows + row] = lane ? lse[1] : lse[0];
+}
+
+// ---- backward ---------------------------------------------------------------------------------------------------------
+struct DiffBwd {
+  const void *d_o, *q, *k, *v;
+  const float* lambda;
+  const int32_t *cu_q, *cu_k, *tile_start;   // tiles of the side that the blocks own
+  const floatx4_t* rows;                     // [H][Nq]: lse_1, lse_2 in powers of two, delta_1, delta_2
+  int64_t Nq, Nk;
+  int H, G;
+  float scale;
+  void *d_q, *d_k, *d_v;
+  float* share;   // [H][Nq]: a row's part of -dlambda
+};
+
+// The row constants: 16 lanes per row.  delta is made of the unrounded O_m: from rounded ones the gradients of groups of some hundred keys and
+// fewer are a tenth further off.  share (fp32): the rows' parts of -dlambda, which are delta_2; of bf16 calls, whose O_2 comes from
+// rounded weights, the dQ kernel makes them from the unrounded ones.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void diff_rows_kernel(const T* __restrict__ d_o, const float* __restrict__ parts, const float* __restrict__ lse,
+                                                        int64_t rows, floatx4_t* __restrict__ out, float* __restrict__ share) {
+  const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const int t = threadIdx.x & 15;
+  if (row >= rows) return;
+  float a = 0.f, b = 0.f;
+#pragma unroll
+  for (int col = 4 * t; col < D; col += 64) {
+    floatx4_t d;
+    if constexpr (sizeof(T) == 4) {
+      d = *(const floatx4_t*)(d_o + row * D + col);
+    } else {
+      const uintx2_t u = *(const uintx2_t*)(d_o + row * D + col);
+      d = floatx4_t{bf16_lo_to_f32(u[0]), bf16_hi_to_f32(u[0]), bf16_lo_to_f32(u[1]), bf16_hi_to_f32(u[1])};
+    }
+    const floatx4_t x = *(const floatx4_t*)(parts + row * D + col), y = *(const floatx4_t*)(parts + (rows + row) * D + col);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      a = fmaf(d[e], x[e], a);
+      b = fmaf(d[e], y[e], b);
+    }
+  }
+  a = lanes_sum<16>(a);
+  b = lanes_sum<16>(b);
+  if (t == 0) {
+    out[row] = floatx4_t{lse[row] * kLog2e, lse[rows + row] * kLog2e, a, b};
+    if constexpr (sizeof(T) == 4) share[row] = b;
+  }
+}
+
+// dQ and the rows' shares of dlambda: a wave owns 16 NC queries and sweeps the keys.
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void diff_dq_kernel(DiffBwd a) {
+  constexpr int NC = kCols<T>, KB = D / 64, DT = D / 16;
+  __shared__ typename DiffTiles<T, D>::Lds lds;
+  WorkTile w;
+  if (!find_work<false>(a.cu_q, a.tile_start, a.G, a.H, kRows<T>, blockIdx.x, w)) return;
+  const int head = w.head, ge = w.ti.row_end;
+  const int gs = __builtin_amdgcn_readfirstlane(a.cu_k[w.ti.group]), n = __builtin_amdgcn_readfirstlane(a.cu_k[w.ti.group + 1]) - gs;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  const int row0 = w.ti.tile_row + 16 * NC * wave;
+  const int64_t head_q = (int64_t)head * a.Nq, head_k = (int64_t)head * a.Nk;
+  const bool active = row0 < ge;
+  const float c = a.scale * kLog2e, lam = a.lambda[head];
+  floatx4_t dq[DT][NC];
+  float share[NC];
+#pragma unroll
+  for (int q = 0; q < NC; ++q) {
+    share[q] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) dq[dt][q] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  if (n > 0) {
+    Frag<T> qf[NC][D / 32], df[NC][D / 32];
+    diff_columns<T, D, NC>(qf, (const T*)a.q, row0, ge, head_q);
+    diff_columns<T, D, NC>(df, (const T*)a.d_o, row0, ge, head_q);
+    floatx4_t rc[NC];
+#pragma unroll
+    for (int q = 0; q < NC; ++q) rc[q] = a.rows[head_q + min(row0 + 16 * q + r, ge - 1)];
+    DiffTiles<T, D> tiles;
+    tiles.start(lds, (const T*)a.k + (head_k + gs) * D, (const T*)a.v + (head_k + gs) * D, n);
+    const int steps = (n + 31) >> 5;
+    for (int st = 0; st < steps; ++st) {
+      tiles.ready(st);
+      if (!active) continue;
+      const int left = n - 32 * st;
+      float d1[NC][8], d2[NC][8];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        floatx4_t s[2][NC], dp[NC];
+#pragma unroll
+        for (int kb = 0; kb < 2 * KB; ++kb) {
+          const Frag<T> f = tiles.nat(0, t, kb);
+#pragma unroll
+          for (int q = 0; q < NC; ++q) s[kb / KB][q] = mma(f, qf[q][kb], kb % KB == 0 ? floatx4_t{0.f, 0.f, 0.f, 0.f} : s[kb / KB][q]);
+        }
+#pragma unroll
+        for (int kb = 0; kb < 2 * KB; ++kb) {
+          const Frag<T> f = tiles.nat(1, t, kb);
+#pragma unroll
+          for (int q = 0; q < NC; ++q) dp[q] = mma(f, df[q][kb], kb == 0 ? floatx4_t{0.f, 0.f, 0.f, 0.f} : dp[q]);
+        }
+#pragma unroll
+        for (int q = 0; q < NC; ++q)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float p1 = fast_exp2(fmaf(s[0][q][i], c, -rc[q][0])), p2 = fast_exp2(fmaf(s[1][q][i], c, -rc[q][1]));
+            if (left < 32 && 8 * g + 4 * t + i >= left) p1 = p2 = 0.f;
+            if constexpr (sizeof(T) == 2) share[q] = fmaf(p2, dp[q][i], share[q]);
+            d1[q][4 * t + i] = p1 * (dp[q][i] - rc[q][2]);
+            d2[q][4 * t + i] = p2 * (dp[q][i] - rc[q][3]);
+          }
+      }
+      Frag<T> f1[NC], f2[NC];
+#pragma unroll
+      for (int q = 0; q < NC; ++q) {
+        make_frag(f1[q], d1[q]);
+        make_frag(f2[q], d2[q]);
+      }
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const Frag<T> f = tiles.tr(0, dt);
+#pragma unroll
+        for (int q = 0; q < NC; ++q) dq[dt][q] = mma(f, dt < DT / 2 ? f1[q] : f2[q], dq[dt][q]);
+      }
+    }
+    tiles.finish();
+  }
+  if (!active) return;
+#pragma unroll
+  for (int q = 0; q < NC; ++q) {
+    const int row = row0 + 16 * q + r;
+    float sh = share[q] + __shfl_xor(share[q], 16, kWave);
+    sh += __shfl_xor(sh, 32, kWave);
+    if (row >= ge) continue;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) store4((T*)a.d_q + (head_q + row) * D, dt, dq[dt][q] * (dt < DT / 2 ? a.scale : -lam * a.scale));
+    if (sizeof(T) == 2 && g == 0) a.share[head_q + row] = sh;
+  }
+}
+
+// dK and dV: a wave owns 16 NC keys and sweeps the queries, with their row constants beside them in LDS.
+template <typename T, int D>
+__global__ __launch_bounds__(256, 1) void diff_dkdv_kernel(DiffBwd a) {
+  constexpr int NC = kCols<T>, KB = D / 64, DT = D / 16;
+  __shared__ typename DiffTiles<T, D>::Lds lds;
+  __shared__ floatx4_t rows[2][32];
+  WorkTile w;
+  if (!find_work<false>(a.cu_k, a.tile_start, a.G, a.H, kRows<T>, blockIdx.x, w)) return;
+  const int head = w.head, ge = w.ti.row_end;
+  const int gs = __builtin_amdgcn_readfirstlane(a.cu_q[w.ti.group]), n = __builtin_amdgcn_readfirstlane(a.cu_q[w.ti.group + 1]) - gs;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  const int row0 = w.ti.tile_row + 16 * NC * wave;
+  const int64_t head_q = (int64_t)head * a.Nq, head_k = (int64_t)head * a.Nk;
+  const bool active = row0 < ge;
+  const float c = a.scale * kLog2e, lam = a.lambda[head];
+  floatx4_t dk[DT][NC], dv[DT][NC];
+#pragma unroll
+  for (int k = 0; k < NC; ++k)
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) dk[dt][k] = dv[dt][k] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+  if (n > 0) {
+    Frag<T> kf[NC][D / 32], vf[NC][D / 32];
+    diff_columns<T, D, NC>(kf, (const T*)a.k, row0, ge, head_k);
+    diff_columns<T, D, NC>(vf, (const T*)a.v, row0, ge, head_k);
+    DiffTiles<T, D> tiles;
+    tiles.start(lds, (const T*)a.q + (head_q + gs) * D, (const T*)a.d_o + (head_q + gs) * D, n);
+    const int steps = (n + 31) >> 5;
+    for (int st = 0; st < steps; ++st) {
+      if (threadIdx.x < 32) rows[st & 1][threadIdx.x] = a.rows[head_q + gs + min(32 * st + (int)threadIdx.x, n - 1)];
+      tiles.ready(st);   // its barrier is behind the store, and the other buffer's readers are a step back
+      if (!active) continue;
+      const int left = n - 32 * st;
+      float pa[NC][8], d1[NC][8], d2[NC][8];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        floatx4_t s[2][NC], dp[NC];
+#pragma unroll
+        for (int kb = 0; kb < 2 * KB; ++kb) {
+          const Frag<T> f = tiles.nat(0, t, kb);
+#pragma unroll
+          for (int k = 0; k < NC; ++k) s[kb / KB][k] = mma(f, kf[k][kb], kb % KB == 0 ? floatx4_t{0.f, 0.f, 0.f, 0.f} : s[kb / KB][k]);
+        }
+#pragma unroll
+        for (int kb = 0; kb < 2 * KB; ++kb) {
+          const Frag<T> f = tiles.nat(1, t, kb);
+#pragma unroll
+          for (int k = 0; k < NC; ++k) dp[k] = mma(f, vf[k][kb], kb == 0 ? floatx4_t{0.f, 0.f, 0.f, 0.f} : dp[k]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int q = 8 * g + 4 * t + i;
+          const floatx4_t rc = rows[st & 1][q];
+#pragma unroll
+          for (int k = 0; k < NC; ++k) {
+            float p1 = fast_exp2(fmaf(s[0][k][i], c, -rc[0])), p2 = lam * fast_exp2(fmaf(s[1][k][i], c, -rc[1]));
+            if (left < 32 && q >= left) p1 = p2 = 0.f;
+            pa[k][4 * t + i] = p1 - p2;
+            d1[k][4 * t + i] = p1 * (dp[k][i] - rc[2]);
+            d2[k][4 * t + i] = p2 * (rc[3] - dp[k][i]);
+          }
+        }
+      }
+      Frag<T> fa[NC], f1[NC], f2[NC];
+#pragma unroll
+      for (int k = 0; k < NC; ++k) {
+        make_frag(fa[k], pa[k]);
+        make_frag(f1[k], d1[k]);
+        make_frag(f2[k], d2[k]);
+      }
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const Frag<T> fd = tiles.tr(1, dt), fq = tiles.tr(0, dt);
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+          dv[dt][k] = mma(fd, fa[k], dv[dt][k]);
+          dk[dt][k] = mma(fq, dt < DT / 2 ? f1[k] : f2[k], dk[dt][k]);
+        }
+      }
+    }
+    tiles.finish();
+  }
+  if (!active) return;
+#pragma unroll
+  for (int k = 0; k < NC; ++k) {
+    const int row = row0 + 16 * k + r;
+    if (row >= ge) continue;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      store4((T*)a.d_k + (head_k + row) * D, dt, dk[dt][k] * a.scale);
+      store4((T*)a.d_v + (head_k + row) * D, dt, dv[dt][k]);
+    }
+  }
+}
+
+// A block per head, in a fixed order.
+__global__ __launch_bounds__(1024) void diff_dlambda_kernel(const float* __restrict__ share, const int32_t* __restrict__ cu_q, int G, int64_t Nq,
+                                                           float* __restrict__ d_lambda) {
+  __shared__ float acc[16];
+  const float* p = share + blockIdx.x * Nq;
+  const int n = Nq > 0 ? cu_q[G] : 0;
+  float s = 0.f;
+  for (int i = threadIdx.x; i < n; i += 1024) s += p[i];
+  s = wave_sum(s);
+  if ((threadIdx.x & 63) == 0) acc[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    s = lanes_sum<16>(threadIdx.x < 16 ? acc[threadIdx.x] : 0.f);
+    if (threadIdx.x == 0) d_lambda[blockIdx.x] = 0.f - s;
+  }
+}
+
+int check_diff(int64_t Nq, int64_t Nk, int H, int D, int G, float scale, int dtype) {
+  if (Nq < 0 || Nk < 0 || H < 1 || D < 1 || G < 1) return MOGA_ERR_INVALID_ARG;
+  if (!(scale > 0.f) || !(scale < INFINITY)) return MOGA_ERR_INVALID_ARG;
+  if (dtype != MOGA_F32 && dtype != MOGA_BF16) return MOGA_ERR_UNSUPPORTED;
+  if (dtype == MOGA_BF16 ? D != 128 : D != 64 && D != 128) return MOGA_ERR_UNSUPPORTED;
+  // row offsets inside a group are 32-bit byte offsets
+  if (Nq >= ((int64_t)1 << 24) || Nk >= ((int64_t)1 << 24) || G > MOGA_MAX_SEGMENTS) return MOGA_ERR_UNSUPPORTED;
+  return MOGA_OK;
+}
+
+int rows_of(int dtype) { return dtype == MOGA_F32 ? kRows<float> : kRows<unsigned short>; }
+int64_t diff_blocks(int64_t N, int H, int G, int dtype) { return (max_tiles(N, G, rows_of(dtype)) * H + 7) / 8 * 8; }
+size_t tile_bytes(int G) { return G > MOGA_MAX_GROUPS ? round_up(((size_t)G + 1) * sizeof(int32_t), 256) : 0; }
+
+// Pieces of a forward tile's keys: where the tiles leave CUs idle, as many as fill two blocks a CU, none under 256 keys of a mean group.
+int diff_pieces(int64_t Nq, int64_t Nk, int H, int G, int dtype) {
+  const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(max_tiles(Nq, G, rows_of(dtype)), Nq)) * H;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, 2 * kCus / blocks), Nk / G / 256));
+}
+size_t diff_piece_bytes(int64_t Nq, int H, int D) { return (size_t)Nq * H * 2 * (D + 2) * sizeof(float); }
+
+}  // namespace
+}  // namespace moga
+
+using namespace moga;
+
+extern "C" size_t moga_diff_attn_fwd_ws_bytes(int G) { return tile_bytes(G); }
+// With the pieces of the keys, for calls of few tiles.
+extern "C" size_t moga_diff_attn_fwd_preferred(int64_t Nq, int64_t Nk, int H, int D, int G, int dtype) {
+  if (Nq <= 0 || check_diff(Nq, Nk, H, D, G, 1.f, dtype) != MOGA_OK) return 0;
+  const int pieces = diff_pieces(Nq, Nk, H, G, dtype);
+  return tile_bytes(G) + (pieces > 1 ? pieces * diff_piece_bytes(Nq, H, D) : 0);
+}
+extern "C" size_t moga_diff_attn_bwd_ws_bytes(int64_t Nq, int H, int G) {
+  return Nq > 0 ? tile_bytes(G) * 2 + (size_t)Nq * H * (sizeof(floatx4_t) + sizeof(float)) : 0;
+}
+
+extern "C" int moga_diff_attn_fwd(const void* qh, const void* kh, const void* vh, int dtype, int64_t Nq, int64_t Nk, int H, int D,
+                                  const float* lambda, const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, int G, float softmax_scale,
+                                  void* oh, float* parts, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  const int bad = check_diff(Nq, Nk, H, D, G, softmax_scale, dtype);
+  if (bad) return bad;
+  if (Nq == 0) return MOGA_OK;
+  if (!qh || !lambda || !cu_seqlens_q || !cu_seqlens_k || !oh || !lse || (Nk > 0 && (!kh || !vh))) return MOGA_ERR_INVALID_ARG;
+  if (!(aligned16(qh) && aligned16(kh) && aligned16(vh) && aligned16(oh) && aligned16(parts) && aligned16(ws))) return MOGA_ERR_INVALID_ARG;
+  const size_t need = moga_diff_attn_fwd_ws_bytes(G);
+  if (need && (!ws || ws_bytes < need)) return MOGA_ERR_WORKSPACE;
+  const bool room = ws && ws_bytes >= moga_diff_attn_fwd_preferred(Nq, Nk, H, D, G, dtype);
+  const int pieces = room ? diff_pieces(Nq, Nk, H, G, dtype) : 1;
+  const int64_t blocks = diff_blocks(Nq, H, G, dtype), rows = Nq * H;
+  if (!grid_fits(blocks * pieces, 256) || !grid_fits((rows + 3) / 4, 256)) return MOGA_ERR_UNSUPPORTED;
+  hipStream_t st = (hipStream_t)stream;
+  int32_t* ts = G > MOGA_MAX_GROUPS ? (int32_t*)ws : nullptr;
+  DiffFwd a = {qh, kh, vh, lambda, cu_seqlens_q, cu_seqlens_k, ts, Nq, Nk, H, G, softmax_scale, oh, parts, lse, nullptr, nullptr};
+  if (pieces > 1) {
+    a.part = (float*)((char*)ws + tile_bytes(G));
+    a.stat = a.part + (size_t)pieces * rows * 2 * D;
+  }
+  if (ts) tile_start_kernel<<<1, 1024, 0, st>>>(cu_seqlens_q, G, rows_of(dtype), ts);
+  const dim3 grid((unsigned)blocks, (unsigned)pieces);
+#define MOGA_DIFF_FWD(T, D)                                                          \
+  do {                                                                               \
+    if (pieces > 1) {                                                                \
+      diff_fwd_kernel<T, D, true><<<grid, 256, 0, st>>>(a);                          \
+      diff_merge_kernel<T, D><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a, pieces); \
+    } else {                                                                         \
+      diff_fwd_kernel<T, D, false><<<grid, 256, 0, st>>>(a);                         \
+    }                                                                                \
+  } while (0)
+  if (dtype == MOGA_BF16) MOGA_DIFF_FWD(unsigned short, 128);
+  else if (D == 64) MOGA_DIFF_FWD(float, 64);
+  else MOGA_DIFF_FWD(float, 128);
+#undef MOGA_DIFF_FWD
+  return launch_status();
+}
+
+extern "C" int moga_diff_attn_bwd(const void* d_oh, const void* qh, const void* kh, const void* vh, const float* parts,
+                                  const float* lse, int dtype, int64_t Nq, int64_t Nk, int H, int D, const float* lambda,
+                                  const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, int G, float softmax_scale, void* d_qh, void* d_kh,
+                                  void* d_vh, float* d_lambda, void* ws, size_t ws_bytes, void* stream) {
+  const int bad = check_diff(Nq, Nk, H, D, G, softmax_scale, dtype);
+  if (bad) return bad;
+  if (Nq == 0 && Nk == 0 && !d_lambda) return MOGA_OK;
+  if (!lambda || !cu_seqlens_q || !cu_seqlens_k || !d_lambda) return MOGA_ERR_INVALID_ARG;
+  if (Nq > 0 && (!d_oh || !qh || !parts || !lse || !d_qh)) return MOGA_ERR_INVALID_ARG;
+  if (Nk > 0 && (!kh || !vh || !d_kh || !d_vh)) return MOGA_ERR_INVALID_ARG;
+  if (!(aligned16(d_oh) && aligned16(qh) && aligned16(kh) && aligned16(vh) && aligned16(parts) && aligned16(d_qh) &&
+        aligned16(d_kh) && aligned16(d_vh) && aligned16(ws)))
+    return MOGA_ERR_INVALID_ARG;
+  const size_t need = moga_diff_attn_bwd_ws_bytes(Nq, H, G);
+  if (need && (!ws || ws_bytes < need)) return MOGA_ERR_WORKSPACE;
+  const int64_t q_blocks = diff_blocks(Nq, H, G, dtype), k_blocks = diff_blocks(Nk, H, G, dtype), rows = Nq * H;
+  if (!grid_fits(q_blocks, 256) || !grid_fits(k_blocks, 256) || !grid_fits((rows + 15) / 16, 256)) return MOGA_ERR_UNSUPPORTED;
+  hipStream_t st = (hipStream_t)stream;
+  int32_t *tq = nullptr, *tk = nullptr;
+  if (G > MOGA_MAX_GROUPS && need) {
+    tq = (int32_t*)ws;
+    tk = (int32_t*)((char*)ws + tile_bytes(G));
+    tile_start_kernel<<<1, 1024, 0, st>>>(cu_seqlens_q, G, rows_of(dtype), tq);
+    tile_start_kernel<<<1, 1024, 0, st>>>(cu_seqlens_k, G, rows_of(dtype), tk);
+  }
+  floatx4_t* rc = (floatx4_t*)((char*)ws + 2 * tile_bytes(G));
+  float* share = (float*)(rc + rows);
+  DiffBwd a = {d_oh, qh, kh, vh, lambda, cu_seqlens_q, cu_seqlens_k, tq, rc, Nq, Nk, H, G, softmax_scale, d_qh, d_kh, d_vh, share};
+  DiffBwd b = a;
+  b.tile_start = tk;
+#define MOGA_DIFF_BWD(T, D)                                                                                                            \
+  do {                                                                                                                                 \
+    diff_rows_kernel<T, D><<<(unsigned)((rows + 15) / 16), 256, 0, st>>>((const T*)d_oh, parts, lse, rows, rc, share);                  \
+    diff_dq_kernel<T, D><<<(unsigned)q_blocks, 256, 0, st>>>(a);                                                                       \
+    if (Nk > 0) diff_dkdv_kernel<T, D><<<(unsigned)k_blocks, 256, 0, st>>>(b);                                                          \
+  } while (0)
+  if (Nq > 0) {
+    if (dtype == MOGA_BF16) MOGA_DIFF_BWD(unsigned short, 128);
+    else if (D == 64) MOGA_DIFF_BWD(float, 64);
+    else MOGA_DIFF_BWD(float, 128);
+  } else if (Nk > 0) {   // keys without queries
+    const int64_t floats = Nk * H * D * (int64_t)elem_size(dtype) / 4;
+    launch_fill_zero((float*)d_kh, floats, st);
+    launch_fill_zero((float*)d_vh, floats, st);
+  }
+#undef MOGA_DIFF_BWD
+  diff_dlambda_kernel<<<H, 1024, 0, st>>>(share, cu_seqlens_q, G, Nq, d_lambda);
+  return launch_status();
+}

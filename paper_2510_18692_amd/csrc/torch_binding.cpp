@@ -6,6 +6,7 @@
 // forward calls 72 and 32 us, the four backward calls 70 and 31 us, a training step through autograd 346 and
 // 101 us (its backward now runs in the engine's thread without the interpreter).
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/core/StreamGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/custom_function.h>
@@ -593,6 +594,191 @@ Tensor balance_loss_bwd(const Tensor& group, const Tensor& frac, double alpha, d
   return d_gate;
 }
 
+// ---- layer norm, rotary positions, differential attention ----
+// These look at what the C entry points cannot see: sizes, types and devices of the tensors beside the first one.
+void need(bool ok, const char* text) {
+  if (!ok) raise(PyExc_ValueError, text);
+}
+void need_like(const Tensor& t, const Tensor& first, at::IntArrayRef size, at::ScalarType type, const char* name) {
+  if (t.scalar_type() != type) raise(PyExc_TypeError, std::string(name) + ": expected " + c10::toString(type) + ", got " + c10::toString(t.scalar_type()));
+  if (t.sizes() != size) raise(PyExc_ValueError, std::string(name) + ": unexpected size");
+  if (t.device() != first.device()) raise(PyExc_ValueError, std::string(name) + ": on another device");
+}
+void need_like(const OptTensor& t, const Tensor& first, at::IntArrayRef size, at::ScalarType type, const char* name) {
+  if (t) need_like(*t, first, size, type, name);
+}
+// A vector of 64-bit results' own size is an int in the C calls.
+int to_int(int64_t n) {
+  need(n >= 0 && n <= INT32_MAX, "size beyond 32 bits");
+  return (int)n;
+}
+
+std::tuple<Tensor, OptTensor, OptTensor> layer_norm_fwd(const Tensor& x, const OptTensor& w, const OptTensor& b, double eps, bool want_stats,
+                                                        const OptStream& stream) {
+  require(x, w, b);
+  const c10::OptionalDeviceGuard guard(x.device());
+  const Call call(stream);
+  need_dims(x, 2);
+  const int64_t N = x.size(0), C = x.size(1);
+  need_like(w, x, {C}, at::kFloat, "weight");
+  need_like(b, x, {C}, at::kFloat, "bias");
+  Tensor y = call.make(x.sizes(), x);
+  OptTensor mean, rstd;
+  if (want_stats) mean = call.make({N}, x, at::kFloat), rstd = call.make({N}, x, at::kFloat);
+  check("moga_layer_norm_fwd", moga_layer_norm_fwd(ptr(x), dt(x), as<float>(w), as<float>(b), N, to_int(C), (float)eps, ptr(y), as<float>(mean),
+                                                   as<float>(rstd), call.stream()));
+  return {y, mean, rstd};
+}
+
+std::tuple<Tensor, OptTensor, OptTensor> layer_norm_bwd(const Tensor& d_y, const Tensor& x, const OptTensor& w, const Tensor& mean,
+                                                        const Tensor& rstd, bool want_dw, const OptStream& stream) {
+  require(d_y, x, w, mean, rstd);
+  const c10::OptionalDeviceGuard guard(x.device());
+  const Call call(stream);
+  need_dims(x, 2);
+  const int64_t N = x.size(0), C = x.size(1);
+  need_like(d_y, x, x.sizes(), x.scalar_type(), "d_y");
+  need_like(w, x, {C}, at::kFloat, "weight");
+  need_like(mean, x, {N}, at::kFloat, "mean");
+  need_like(rstd, x, {N}, at::kFloat, "rstd");
+  Tensor d_x = call.make(x.sizes(), x);
+  OptTensor d_w, d_b, ws;
+  size_t bytes = 0;
+  if (want_dw) {
+    d_w = call.make({C}, x, at::kFloat);
+    d_b = call.make({C}, x, at::kFloat);
+    bytes = moga_workspace_bytes(MOGA_OP_LAYER_NORM_BWD, N, 0, 0, 1, to_int(C), dt(x));
+    ws = call.workspace(bytes, x);
+  }
+  check("moga_layer_norm_bwd", moga_layer_norm_bwd(ptr(d_y), ptr(x), dt(x), as<float>(w), as<float>(mean), as<float>(rstd), N, to_int(C), ptr(d_x),
+                                                   as<float>(d_w), as<float>(d_b), ptr(ws), bytes_of(ws), call.stream()));
+  return {d_x, d_w, d_b};
+}
+
+// What turns the pairs of a head: positions [axes, N] (or [N]), radians per position [R / 2], pairs of each axis.
+struct Rotation {
+  Tensor pos, freq;
+  std::vector<int64_t> pairs;
+  bool interleaved;
+  double factor;
+  std::vector<int> axis_pairs;
+  int axes = 1;
+
+  Rotation(const Tensor& pos, const Tensor& freq, const std::vector<int64_t>& pairs, bool interleaved, double factor)
+      : pos(pos), freq(freq), pairs(pairs), interleaved(interleaved), factor(factor) {
+    require(pos, freq);
+    need_dims(freq, 1);
+    need(pos.dim() == 1 || pos.dim() == 2, "positions: one or two dimensions");
+    axes = pos.dim() == 1 ? 1 : to_int(pos.size(0));
+    for (int64_t n : pairs) axis_pairs.push_back(to_int(n));
+    need(axis_pairs.empty() ? axes == 1 : (int)axis_pairs.size() == axes, "axis_pairs: one number for each axis of the positions");
+  }
+  void fits(const Tensor& q, int64_t N) const {
+    need_like(freq, q, {freq.size(0)}, at::kDouble, "inv_freq");
+    if (pos.dim() == 1) need_like(pos, q, {N}, at::kInt, "positions");
+    else need_like(pos, q, {axes, N}, at::kInt, "positions");
+  }
+  const int* host_pairs() const { return axis_pairs.empty() ? nullptr : axis_pairs.data(); }
+  int R() const { return 2 * to_int(freq.size(0)); }
+};
+
+std::tuple<OptTensor, OptTensor> rotary_turn(const OptTensor& q, const OptTensor& k, const Rotation& how, bool back, const OptStream& stream) {
+  require(q, k);
+  need(q || k, "q or k");
+  const Tensor& first = q ? *q : *k;
+  const c10::OptionalDeviceGuard guard(first.device());
+  const Call call(stream);
+  need_dims(first, 3);
+  const int64_t N = first.size(0), D = first.size(2);
+  how.fits(first, N);
+  if (q && k) {
+    need_dims(*k, 3);
+    need_like(*k, first, {N, k->size(1), D}, first.scalar_type(), "k");
+  }
+  OptTensor qo, ko;
+  if (q) qo = call.make(q->sizes(), *q);
+  if (k) ko = call.make(k->sizes(), *k);
+  if ((!q || q->size(1) == 0) && (!k || k->size(1) == 0)) return {qo, ko};
+  check(back ? "moga_rotary_bwd" : "moga_rotary_fwd",
+        (back ? moga_rotary_bwd : moga_rotary_fwd)(ptr(q), ptr(k), dt(first), N, q ? to_int(q->size(1)) : 0, k ? to_int(k->size(1)) : 0, to_int(D),
+                                                   as<int32_t>(how.pos), how.axes, how.host_pairs(), as<double>(how.freq), how.R(),
+                                                   how.interleaved, (float)how.factor, ptr(qo), ptr(ko), call.stream()));
+  return {qo, ko};
+}
+
+std::tuple<Tensor, Tensor, Tensor> rotary_permute(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& perm, const Rotation& how,
+                                                  bool back, const OptStream& stream) {
+  require(q, k, v, perm);
+  const c10::OptionalDeviceGuard guard(q.device());
+  const Call call(stream);
+  need_dims(q, 3);
+  const int64_t N = q.size(back ? 1 : 0), H = q.size(back ? 0 : 1), D = q.size(2);
+  need_like(k, q, q.sizes(), q.scalar_type(), "k");
+  need_like(v, q, q.sizes(), q.scalar_type(), "v");
+  need_like(perm, q, {N}, at::kInt, "perm");
+  how.fits(q, N);
+  const std::vector<int64_t> size = back ? std::vector<int64_t>{N, H, D} : std::vector<int64_t>{H, N, D};
+  Tensor qo = call.make(size, q), ko = call.make(size, k), vo = call.make(size, v);
+  check(back ? "moga_rotary_permute_bwd" : "moga_rotary_permute_fwd",
+        (back ? moga_rotary_permute_bwd : moga_rotary_permute_fwd)(ptr(q), ptr(k), ptr(v), dt(q), N, to_int(H), to_int(D), as<int32_t>(perm),
+                                                                   as<int32_t>(how.pos), how.axes, how.host_pairs(), as<double>(how.freq), how.R(),
+                                                                   how.interleaved, (float)how.factor, ptr(qo), ptr(ko), ptr(vo), call.stream()));
+  return {qo, ko, vo};
+}
+
+struct DiffSizes {
+  int64_t H, Nq, Nk, D, G;
+};
+DiffSizes diff_sizes(const Tensor& qh, const Tensor& kh, const Tensor& vh, const Tensor& lam, const Tensor& cu_q, const Tensor& cu_k) {
+  need_dims(qh, 3);
+  need_dims(kh, 3);
+  need_dims(cu_q, 1);
+  const DiffSizes s = {qh.size(0), qh.size(1), kh.size(1), qh.size(2), cu_q.size(0) - 1};
+  need(s.G >= 1, "cu_seqlens_q: at least two entries");
+  need_like(kh, qh, {s.H, s.Nk, s.D}, qh.scalar_type(), "kh");
+  need_like(vh, qh, {s.H, s.Nk, s.D}, qh.scalar_type(), "vh");
+  need_like(lam, qh, {s.H}, at::kFloat, "lambda");
+  need_like(cu_q, qh, {s.G + 1}, at::kInt, "cu_seqlens_q");
+  need_like(cu_k, qh, {s.G + 1}, at::kInt, "cu_seqlens_k");
+  return s;
+}
+
+std::tuple<Tensor, OptTensor, Tensor> diff_attn_fwd(const Tensor& qh, const Tensor& kh, const Tensor& vh, const Tensor& lam, const Tensor& cu_q,
+                                                    const Tensor& cu_k, double scale, bool want_parts, const OptStream& stream) {
+  require(qh, kh, vh, lam, cu_q, cu_k);
+  const c10::OptionalDeviceGuard guard(qh.device());
+  const Call call(stream);
+  const DiffSizes s = diff_sizes(qh, kh, vh, lam, cu_q, cu_k);
+  Tensor oh = call.make(qh.sizes(), qh), lse = call.make({2, s.H, s.Nq}, qh, at::kFloat);
+  OptTensor parts;
+  if (want_parts) parts = call.make({2, s.H, s.Nq, s.D}, qh, at::kFloat);
+  OptTensor ws = call.attn_workspace(MOGA_OP_DIFF_ATTN_FWD, s.Nq, s.Nk, s.H, s.D, s.G, qh);
+  check("moga_diff_attn_fwd", moga_diff_attn_fwd(ptr(qh), ptr(kh), ptr(vh), dt(qh), s.Nq, s.Nk, to_int(s.H), to_int(s.D), as<float>(lam),
+                                                 as<int32_t>(cu_q), as<int32_t>(cu_k), to_int(s.G), (float)scale, ptr(oh), as<float>(parts),
+                                                 as<float>(lse), ptr(ws), bytes_of(ws), call.stream()));
+  return {oh, parts, lse};
+}
+
+std::tuple<Tensor, Tensor, Tensor, Tensor> diff_attn_bwd(const Tensor& d_oh, const Tensor& qh, const Tensor& kh, const Tensor& vh,
+                                                         const Tensor& parts, const Tensor& lse, const Tensor& lam,
+                                                         const Tensor& cu_q, const Tensor& cu_k, double scale, const OptStream& stream) {
+  require(d_oh, qh, kh, vh, parts, lse, lam, cu_q, cu_k);
+  const c10::OptionalDeviceGuard guard(qh.device());
+  const Call call(stream);
+  const DiffSizes s = diff_sizes(qh, kh, vh, lam, cu_q, cu_k);
+  need_like(d_oh, qh, qh.sizes(), qh.scalar_type(), "d_oh");
+  need_like(parts, qh, {2, s.H, s.Nq, s.D}, at::kFloat, "parts");
+  need_like(lse, qh, {2, s.H, s.Nq}, at::kFloat, "lse");
+  Tensor d_qh = call.make(qh.sizes(), qh), d_kh = call.make(kh.sizes(), kh), d_vh = call.make(vh.sizes(), vh);
+  Tensor d_lam = call.make({s.H}, qh, at::kFloat);
+  Tensor ws = call.workspace(moga_workspace_bytes(MOGA_OP_DIFF_ATTN_BWD, s.Nq, to_int(s.H), to_int(s.D), to_int(s.G), 0, dt(qh)), qh);
+  check("moga_diff_attn_bwd", moga_diff_attn_bwd(ptr(d_oh), ptr(qh), ptr(kh), ptr(vh), as<float>(parts), as<float>(lse), dt(qh), s.Nq, s.Nk,
+                                                 to_int(s.H), to_int(s.D), as<float>(lam), as<int32_t>(cu_q), as<int32_t>(cu_k), to_int(s.G),
+                                                 (float)scale, ptr(d_qh), ptr(d_kh), ptr(d_vh), as<float>(d_lam), ptr(ws), (size_t)ws.numel(),
+                                                 call.stream()));
+  return {d_qh, d_kh, d_vh, d_lam};
+}
+
 // ---- autograd: Alg. 1 with Eq. 5 and, when alpha is given, the balancing loss of Eqs. 6-8 ----
 // Parts of one allocation.  The calls of a step are made directly, with what is small in one tensor (saved for the backward) and what is only needed
 // during the pass in another: a step of 1,560 tokens, 4 heads is bound by the host, and an allocation costs 1 us, three in the engine's thread.
@@ -707,6 +893,137 @@ std::tuple<Tensor, Tensor, Tensor> attention(const Tensor& x, const Tensor& w, c
   return {r[0], r[1], r[2]};
 }
 
+// ---- autograd: layer norm, rotary positions, and Alg. 1 with differential attention in its groups ----
+using torch::autograd::AutogradContext;
+using torch::autograd::variable_list;
+
+Tensor or_empty(const OptTensor& t) { return t ? *t : Tensor(); }
+OptTensor or_none(const Tensor& t) { return t.defined() ? OptTensor(t) : std::nullopt; }
+
+struct LayerNorm : public torch::autograd::Function<LayerNorm> {
+  static Tensor forward(AutogradContext* ctx, const Tensor& x, const OptTensor& w, const OptTensor& b, double eps) {
+    require(x);
+    need(x.dim() >= 1, "x: at least one dimension");
+    const int64_t C = x.size(-1);
+    need(C >= 1, "x: an empty last dimension");
+    const Tensor rows = x.view({x.numel() / C, C});
+    auto [y, mean, rstd] = layer_norm_fwd(rows, w, b, eps, true, std::nullopt);
+    ctx->save_for_backward({rows, or_empty(w), *mean, *rstd});
+    ctx->saved_data["bias"] = b.has_value();
+    return y.view(x.sizes());
+  }
+  static variable_list backward(AutogradContext* ctx, const variable_list& grads) {
+    const auto s = ctx->get_saved_variables();
+    const bool bias = ctx->saved_data["bias"].toBool();
+    const Tensor d_y = grads[0].contiguous();
+    // inputs are counted without those that are absent
+    const bool dw = (s[1].defined() && ctx->needs_input_grad(1)) || (bias && ctx->needs_input_grad(s[1].defined() ? 2 : 1));
+    auto [d_x, d_w, d_b] = layer_norm_bwd(d_y.view(s[0].sizes()), s[0], or_none(s[1]), s[2], s[3], dw, std::nullopt);
+    return {d_x.view(d_y.sizes()), s[1].defined() ? or_empty(d_w) : Tensor(), bias ? or_empty(d_b) : Tensor(), Tensor()};
+  }
+};
+
+struct Rotary : public torch::autograd::Function<Rotary> {
+  static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& pos, const Tensor& freq,
+                               const std::vector<int64_t>& pairs, bool interleaved, double factor) {
+    auto [qo, ko] = rotary_turn(q, k, Rotation(pos, freq, pairs, interleaved, factor), false, std::nullopt);
+    ctx->save_for_backward({pos, freq});
+    ctx->saved_data["pairs"] = pairs;
+    ctx->saved_data["how"] = std::vector<double>{interleaved ? 1. : 0., factor};
+    ctx->set_materialize_grads(false);
+    return {*qo, *ko};
+  }
+  static variable_list backward(AutogradContext* ctx, const variable_list& grads) {
+    const auto s = ctx->get_saved_variables();
+    const auto how = ctx->saved_data["how"].toDoubleVector();
+    OptTensor dq, dk;
+    if (grads[0].defined()) dq = grads[0].contiguous();
+    if (grads[1].defined()) dk = grads[1].contiguous();
+    variable_list out(7);
+    if (!dq && !dk) return out;
+    auto [a, b] = rotary_turn(dq, dk, Rotation(s[0], s[1], ctx->saved_data["pairs"].toIntVector(), how[0] != 0., how[1]), true, std::nullopt);
+    out[0] = or_empty(a);
+    out[1] = or_empty(b);
+    return out;
+  }
+};
+
+struct DiffAttention : public torch::autograd::Function<DiffAttention> {
+  static variable_list forward(AutogradContext* ctx, const Tensor& x, const Tensor& w, const Tensor& q, const Tensor& k, const Tensor& v,
+                               const Tensor& lam, double scale, std::optional<double> alpha, bool grad_x, const OptTensor& pos,
+                               const OptTensor& freq, const std::vector<int64_t>& pairs, bool interleaved, double factor) {
+    require(x, w, q, k, v, lam, pos, freq);
+    need_dims(x, 2);
+    need_dims(w, 2);
+    need_dims(q, 3);
+    const c10::OptionalDeviceGuard guard(q.device());
+    const int64_t N = q.size(0), M = w.size(0);
+    need(x.size(0) == N && x.size(1) == w.size(1), "x [N, d_model] and w [M, d_model] with the N of q");
+    need_like(w, x, w.sizes(), at::kFloat, "w");
+    need_like(k, q, q.sizes(), q.scalar_type(), "k");
+    need_like(v, q, q.sizes(), q.scalar_type(), "v");
+    need_like(lam, q, {q.size(1)}, at::kFloat, "lambda");
+    need(pos.has_value() == freq.has_value(), "positions and inv_freq");
+    std::optional<Rotation> how;
+    if (pos) how.emplace(*pos, *freq, pairs, interleaved, factor);
+    auto [group, gate, probs, logits] = route(x, w, std::nullopt, true, false, std::nullopt);
+    Tensor qh, kh, vh;
+    Permuted p;
+    if (how) {
+      p = permute(group, M, std::nullopt, std::nullopt, std::nullopt, std::nullopt);
+      std::tie(qh, kh, vh) = rotary_permute(q, k, v, p.perm, *how, false, std::nullopt);
+    } else {
+      p = permute(group, M, q, k, v, std::nullopt);
+      qh = *p.qh, kh = *p.kh, vh = *p.vh;
+    }
+    auto [oh, parts, lse] = diff_attn_fwd(qh, kh, vh, lam, p.cu_seqlens, p.cu_seqlens, scale, true, std::nullopt);
+    Tensor o = unpermute(oh, p.perm, gate, std::nullopt, std::nullopt);
+    Tensor loss = alpha ? at::empty({}, x.options().dtype(at::kFloat)) : at::zeros({}, x.options().dtype(at::kFloat)), frac;
+    if (alpha) frac = std::get<0>(balance_into(loss, group, gate, M, *alpha, std::nullopt));
+    ctx->save_for_backward({x, w, group, gate, *probs, p.perm, p.cu_seqlens, qh, kh, vh, lam, oh, *parts, lse, frac, or_empty(pos), or_empty(freq)});
+    ctx->saved_data["args"] = std::vector<double>{scale, alpha.value_or(0.), alpha ? 1. : 0., grad_x ? 1. : 0., interleaved ? 1. : 0., factor};
+    ctx->saved_data["pairs"] = pairs;
+    ctx->mark_non_differentiable({group});
+    ctx->set_materialize_grads(false);
+    return {o, loss, group};
+  }
+
+  static variable_list backward(AutogradContext* ctx, const variable_list& grads) {
+    const auto s = ctx->get_saved_variables();
+    const Tensor &x = s[0], &w = s[1], &group = s[2], &gate = s[3], &probs = s[4], &perm = s[5], &cu = s[6], &qh = s[7], &kh = s[8], &vh = s[9],
+                 &lam = s[10], &oh = s[11], &parts = s[12], &lse = s[13], &frac = s[14];
+    const std::vector<double> a = ctx->saved_data["args"].toDoubleVector();
+    const c10::OptionalDeviceGuard guard(qh.device());
+    const int64_t H = qh.size(0), N = qh.size(1), D = qh.size(2);
+    Tensor d_o = grads[0].defined() ? grads[0].contiguous() : at::zeros({N, H, D}, qh.options());
+    auto [d_oh, d_gate] = unpermute_bwd(d_o, oh, perm, gate, std::nullopt);
+    auto [d_qh, d_kh, d_vh, d_lam] = diff_attn_bwd(d_oh, qh, kh, vh, parts, lse, lam, cu, cu, a[0], std::nullopt);
+    Tensor d_q, d_k, d_v;
+    if (s[15].defined())
+      std::tie(d_q, d_k, d_v) = rotary_permute(d_qh, d_kh, d_vh, perm, Rotation(s[15], s[16], ctx->saved_data["pairs"].toIntVector(), a[4] != 0., a[5]),
+                                               true, std::nullopt);
+    else
+      std::tie(d_q, d_k, d_v) = permute_bwd(d_qh, d_kh, d_vh, perm, std::nullopt);
+    const bool balanced = a[2] != 0. && grads[1].defined();
+    std::optional<at::ScalarType> dx;
+    if (a[3] != 0.) dx = x.scalar_type();
+    auto [d_w, d_x] = route_bwd_with(x, w, probs, group, gate, d_gate, balanced ? OptTensor(frac) : std::nullopt, a[1],
+                                     balanced ? OptTensor(grads[1]) : std::nullopt, dx, std::nullopt);
+    variable_list out(14);
+    out[0] = or_empty(d_x);
+    out[1] = d_w, out[2] = d_q, out[3] = d_k, out[4] = d_v, out[5] = d_lam;
+    return out;
+  }
+};
+
+std::tuple<Tensor, Tensor, Tensor> diff_attention(const Tensor& x, const Tensor& w, const Tensor& q, const Tensor& k, const Tensor& v,
+                                                  const Tensor& lam, double scale, std::optional<double> alpha, bool grad_x,
+                                                  const OptTensor& pos, const OptTensor& freq, const std::vector<int64_t>& pairs,
+                                                  bool interleaved, double factor) {
+  auto r = DiffAttention::apply(x, w, q, k, v, lam, scale, alpha, grad_x, pos, freq, pairs, interleaved, factor);
+  return {r[0], r[1], r[2]};
+}
+
 }  // namespace
 
 PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
@@ -753,4 +1070,30 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
   m.def("balance_loss", &balance_loss, nogil);
   m.def("balance_loss_bwd", &balance_loss_bwd, nogil);
   m.def("attention", &attention, nogil);
+  m.def("layer_norm_fwd", &layer_norm_fwd, nogil);
+  m.def("layer_norm_bwd", &layer_norm_bwd, nogil);
+  m.def(
+      "rotary",
+      [](const OptTensor& q, const OptTensor& k, const Tensor& pos, const Tensor& freq, const std::vector<int64_t>& pairs, bool interleaved,
+         double factor, bool back, const OptStream& stream) { return rotary_turn(q, k, Rotation(pos, freq, pairs, interleaved, factor), back, stream); },
+      nogil);
+  m.def(
+      "rotary_permute",
+      [](const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& perm, const Tensor& pos, const Tensor& freq,
+         const std::vector<int64_t>& pairs, bool interleaved, double factor, bool back, const OptStream& stream) {
+        return rotary_permute(q, k, v, perm, Rotation(pos, freq, pairs, interleaved, factor), back, stream);
+      },
+      nogil);
+  m.def("diff_attn_fwd", &diff_attn_fwd, nogil);
+  m.def("diff_attn_bwd", &diff_attn_bwd, nogil);
+  m.def(
+      "layer_norm", [](const Tensor& x, const OptTensor& w, const OptTensor& b, double eps) { return LayerNorm::apply(x, w, b, eps); }, nogil);
+  m.def(
+      "rotary_apply",
+      [](const Tensor& q, const Tensor& k, const Tensor& pos, const Tensor& freq, const std::vector<int64_t>& pairs, bool interleaved, double factor) {
+        auto r = Rotary::apply(q, k, pos, freq, pairs, interleaved, factor);
+        return std::make_tuple(r[0], r[1]);
+      },
+      nogil);
+  m.def("diff_attention", &diff_attention, nogil);
 }
