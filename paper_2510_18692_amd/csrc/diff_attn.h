@@ -51,53 +51,79 @@ __device__ __forceinline__ void diff_columns(Frag<T> (&f)[NC][D / 32], const T* 
   }
 }
 
-// Rows of a group streamed through LDS, 32 of two tensors at a time.  ready(s): tile s may be read, by all waves of the block together.
+// Rows of a group streamed through LDS, 32 of two tensors at a time.  ready(s): tile s may be read, by all waves of the block together, and
+// all of them have left tile s - KEEP.
 // nat(which, t, kb): operand t of the tile's rows (step_row), channels 32 kb ..; tr(which, dt): transposed, channels 16 dt .., all 32 rows.
-template <typename T, int D> struct DiffTiles;
+template <typename T, int D, bool ROWS = false, int KEEP = 1> struct DiffTiles;
 
-// bf16: direct-to-LDS loads into a ring of four, three tiles ahead.
-template <> struct DiffTiles<unsigned short, 128> {
-  static constexpr int kTile = 32 * kHeadDim * 2, kLoads = 2 * kDmaLoads<4, 32>, kAhead = 3;
+// With ROWS, 16 bytes of constants of every row beside them: row(i).
+// bf16: direct-to-LDS loads into a ring of four, as far ahead as the tiles that are kept allow.
+template <bool ROWS, int KEEP> struct DiffTiles<unsigned short, 128, ROWS, KEEP> {
+  static constexpr int kTile = 32 * kHeadDim * 2, kLoads = 2 * kDmaLoads<4, 32> + ROWS, kAhead = 4 - KEEP, kRowSlot = 640;
   struct Lds {
     __attribute__((aligned(1024))) unsigned short a[4][32 * kHeadDim];
     __attribute__((aligned(1024))) unsigned short b[4][32 * kHeadDim];
+    __attribute__((aligned(128))) char rows[ROWS ? 4 : 1][ROWS ? kRowSlot : 16];
   };
   PipeDma dma;
-  unsigned n_[2], t_[2][2], off;
-  __device__ __forceinline__ void start(Lds& lds, const unsigned short* a, const unsigned short* b, int n) {
+  unsigned n_[2], t_[2][2], off, rows_lds, rows_own, rows_at;
+  const void* rows_base;
+  // A wave moves 128 bytes of the 512, and the next wave's (the same bytes twice) with the lanes that are left.
+  __device__ __forceinline__ void issue(int s) {
+    pipe_issue<4, 32, false>(dma, 32 * s, (s & 3) * kTile);
+    if constexpr (ROWS) {
+      const int word = (threadIdx.x >> 6) * 32 + (threadIdx.x & 63), row = min(32 * s + (word >> 2), dma.last_row);
+      lds_dma4_soff(rows_base, (unsigned)row * 16u + (word & 3) * 4u, rows_own + (s & 3) * kRowSlot);
+    }
+  }
+  __device__ __forceinline__ void start(Lds& lds, const unsigned short* a, const unsigned short* b, int n, const floatx4_t* rows = nullptr) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     dma.kbase = uniform_ptr(a);
     dma.vbase = uniform_ptr(b);
     dma_lanes<4, 32>(dma, &lds.a[0][0], &lds.b[0][0], wave, lane);
     dma.last_row = n - 1;
+    if constexpr (ROWS) {
+      rows_base = uniform_ptr(rows);
+      rows_lds = lds_addr_uniform(&lds.rows[0][0]);
+      rows_own = rows_lds + wave * 128;
+    }
     n_[0] = nat_address(&lds.a[0][0], lane);
     n_[1] = nat_address(&lds.b[0][0], lane);
     tr_addresses(t_[0], &lds.a[0][0], lane);
     tr_addresses(t_[1], &lds.b[0][0], lane);
 #pragma unroll
-    for (int s = 0; s < kAhead; ++s) pipe_issue<4, 32, false>(dma, 32 * s, s * kTile);   // rows are clamped: always issued
+    for (int s = 0; s < kAhead; ++s) issue(s);   // rows are clamped: always issued
   }
   __device__ __forceinline__ void ready(int s) {
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(kLoads * (kAhead - 1)));
-    __syncthreads();   // tile s is here, and every wave has left tile s - 1, whose slot is filled again
-    pipe_issue<4, 32, false>(dma, 32 * (s + kAhead), ((s + kAhead) & 3) * kTile);
+    // tile s is here, and every wave has left tile s - KEEP, whose slot is filled again (kept for longer, a wave's reads of it are done)
+    if constexpr (KEEP == 1) __syncthreads();
+    else block_barrier();
+    issue(s + kAhead);
+    at(s);
+  }
+  __device__ __forceinline__ void at(int s) {   // nat, tr and row read tile s from here on
     off = (unsigned)(s & 3) * kTile;
+    if constexpr (ROWS) rows_at = rows_lds + (unsigned)(s & 3) * kRowSlot;
   }
   __device__ __forceinline__ void finish() { __builtin_amdgcn_s_waitcnt(waitcnt_vm(0)); }   // before the LDS is released
   __device__ __forceinline__ bf16x8_t nat(int which, int t, int kb) const { return read_nat<32>(n_[which] + off, t, kb); }
   __device__ __forceinline__ bf16x8_t tr(int which, int dt) const { return read_tr<32>(t_[which], off, dt); }
+  __device__ __forceinline__ floatx4_t row(int i) const { return *(const floatx4_t __attribute__((address_space(3)))*)(uintptr_t)(rows_at + 16 * i); }
 };
 
 // fp32: through registers, one tile ahead.
-template <int D> struct DiffTiles<float, D> {
+template <int D, bool ROWS> struct DiffTiles<float, D, ROWS, 1> {
   static constexpr int kPitch = D + 4, kEach = 32 * D / 4 / 256;
   struct Lds {
     float a[32][kPitch], b[32][kPitch];
+    floatx4_t rows[ROWS ? 32 : 1];
   };
   Lds* lds;
   const float *pa, *pb;
   int last;
-  floatx4_t ra[kEach], rb[kEach];
+  floatx4_t ra[kEach], rb[kEach], rr;
+  const floatx4_t* rows;
   __device__ __forceinline__ void fetch(int s) {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
@@ -106,9 +132,11 @@ template <int D> struct DiffTiles<float, D> {
       ra[i] = *(const floatx4_t*)(pa + row * D + col);
       rb[i] = *(const floatx4_t*)(pb + row * D + col);
     }
+    if (ROWS && threadIdx.x < 32) rr = rows[min(32 * s + (int)threadIdx.x, last)];
   }
-  __device__ __forceinline__ void start(Lds& l, const float* a, const float* b, int n) {
+  __device__ __forceinline__ void start(Lds& l, const float* a, const float* b, int n, const floatx4_t* r = nullptr) {
     lds = &l;
+    rows = r;
     pa = a;
     pb = b;
     last = n - 1;
@@ -122,10 +150,12 @@ template <int D> struct DiffTiles<float, D> {
       *(floatx4_t*)&lds->a[row][col] = ra[i];
       *(floatx4_t*)&lds->b[row][col] = rb[i];
     }
+    if (ROWS && threadIdx.x < 32) lds->rows[threadIdx.x] = rr;
     __syncthreads();
     fetch(s + 1);
   }
   __device__ __forceinline__ void finish() {}
+  __device__ __forceinline__ floatx4_t row(int i) const { return lds->rows[i]; }
   __device__ __forceinline__ FragF32 nat(int which, int t, int kb) const {
     const int lane = threadIdx.x & 63;
     const float* p = (which ? lds->b : lds->a)[step_row(lane & 15) + 4 * t] + 32 * kb + 8 * (lane >> 4);

@@ -8,7 +8,7 @@
 #include <algorithm>
 #include <cmath>
 
-#include "diff_attn.h"
+#include "diff_keys.h"
 
 namespace moga {
 namespace {
@@ -17,6 +17,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 template <typename T> constexpr int kCols = sizeof(T) == 4 ? 1 : 2;   // columns of 16 rows of a wave
 template <typename T> constexpr int kRows = 64 * kCols<T>;            // rows of a block of four waves
+template <typename T> constexpr int kKeyRows = sizeof(T) == 4 ? 64 : 4 * DiffKeySweep::kKeys;   // the same of dK and dV
 
 struct DiffFwd {
   const void *q, *k, *v;
@@ -371,14 +372,13 @@ __global__ __launch_bounds__(256, 2) void diff_dq_kernel(DiffBwd a) {
   }
 }
 
-// dK and dV: a wave owns 16 NC keys and sweeps the queries, with their row constants beside them in LDS.
+// fp32 dK and dV: a wave owns 16 keys and sweeps the queries, with their row constants beside them in LDS.
 template <typename T, int D>
-__global__ __launch_bounds__(256, 1) void diff_dkdv_kernel(DiffBwd a) {
-  constexpr int NC = kCols<T>, KB = D / 64, DT = D / 16;
-  __shared__ typename DiffTiles<T, D>::Lds lds;
-  __shared__ floatx4_t rows[2][32];
+__global__ __launch_bounds__(256, 1) void diff_dkdv_f32_kernel(DiffBwd a) {
+  constexpr int NC = 1, KB = D / 64, DT = D / 16;
+  __shared__ typename DiffTiles<T, D, true>::Lds lds;
   WorkTile w;
-  if (!find_work<false>(a.cu_k, a.tile_start, a.G, a.H, kRows<T>, blockIdx.x, w)) return;
+  if (!find_work<false>(a.cu_k, a.tile_start, a.G, a.H, kKeyRows<T>, blockIdx.x, w)) return;
   const int head = w.head, ge = w.ti.row_end;
   const int gs = __builtin_amdgcn_readfirstlane(a.cu_q[w.ti.group]), n = __builtin_amdgcn_readfirstlane(a.cu_q[w.ti.group + 1]) - gs;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
@@ -395,12 +395,11 @@ __global__ __launch_bounds__(256, 1) void diff_dkdv_kernel(DiffBwd a) {
     Frag<T> kf[NC][D / 32], vf[NC][D / 32];
     diff_columns<T, D, NC>(kf, (const T*)a.k, row0, ge, head_k);
     diff_columns<T, D, NC>(vf, (const T*)a.v, row0, ge, head_k);
-    DiffTiles<T, D> tiles;
-    tiles.start(lds, (const T*)a.q + (head_q + gs) * D, (const T*)a.d_o + (head_q + gs) * D, n);
+    DiffTiles<T, D, true> tiles;
+    tiles.start(lds, (const T*)a.q + (head_q + gs) * D, (const T*)a.d_o + (head_q + gs) * D, n, a.rows + head_q + gs);
     const int steps = (n + 31) >> 5;
     for (int st = 0; st < steps; ++st) {
-      if (threadIdx.x < 32) rows[st & 1][threadIdx.x] = a.rows[head_q + gs + min(32 * st + (int)threadIdx.x, n - 1)];
-      tiles.ready(st);   // its barrier is behind the store, and the other buffer's readers are a step back
+      tiles.ready(st);
       if (!active) continue;
       const int left = n - 32 * st;
       float pa[NC][8], d1[NC][8], d2[NC][8];
@@ -422,12 +421,12 @@ __global__ __launch_bounds__(256, 1) void diff_dkdv_kernel(DiffBwd a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int q = 8 * g + 4 * t + i;
-          const floatx4_t rc = rows[st & 1][q];
+          const floatx4_t rc = tiles.row(q);
 #pragma unroll
           for (int k = 0; k < NC; ++k) {
-            float p1 = fast_exp2(fmaf(s[0][k][i], c, -rc[0])), p2 = lam * fast_exp2(fmaf(s[1][k][i], c, -rc[1]));
+            float p1 = fast_exp2(fmaf(s[0][k][i], c, -rc[0])), p2 = fast_exp2(fmaf(s[1][k][i], c, -rc[1]));
             if (left < 32 && q >= left) p1 = p2 = 0.f;
-            pa[k][4 * t + i] = p1 - p2;
+            pa[k][4 * t + i] = fmaf(-lam, p2, p1);
             d1[k][4 * t + i] = p1 * (dp[k][i] - rc[2]);
             d2[k][4 * t + i] = p2 * (rc[3] - dp[k][i]);
           }
@@ -459,8 +458,55 @@ __global__ __launch_bounds__(256, 1) void diff_dkdv_kernel(DiffBwd a) {
     if (row >= ge) continue;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-      store4((T*)a.d_k + (head_k + row) * D, dt, dk[dt][k] * a.scale);
+      store4((T*)a.d_k + (head_k + row) * D, dt, dk[dt][k] * (dt < DT / 2 ? a.scale : lam * a.scale));
       store4((T*)a.d_v + (head_k + row) * D, dt, dv[dt][k]);
+    }
+  }
+}
+
+// bf16: diff_keys.h
+__global__ __launch_bounds__(256, 1) void diff_dkdv_kernel(DiffBwd a) {
+  constexpr int NC = DiffKeySweep::NC, D = kHeadDim;
+  typedef unsigned short T;
+  __shared__ typename DiffKeySweep::Tiles::Lds lds;
+  WorkTile w;
+  if (!find_work<false>(a.cu_k, a.tile_start, a.G, a.H, kKeyRows<T>, blockIdx.x, w)) return;
+  const int head = w.head, ge = w.ti.row_end;
+  const int gs = __builtin_amdgcn_readfirstlane(a.cu_q[w.ti.group]), n = __builtin_amdgcn_readfirstlane(a.cu_q[w.ti.group + 1]) - gs;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int row0 = w.ti.tile_row + DiffKeySweep::kKeys * wave;
+  const int64_t head_q = (int64_t)head * a.Nq, head_k = (int64_t)head * a.Nk;
+  const float lam = a.lambda[head];
+  DiffKeySweep k;
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) k.dk[dt][c] = k.dv[dt][c] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+  if (n > 0) {
+    k.tiles.start(lds, (const T*)a.q + (head_q + gs) * D, (const T*)a.d_o + (head_q + gs) * D, n, a.rows + head_q + gs);
+    if (row0 >= ge) {   // no keys: this wave moves its share of the tiles and keeps the barriers
+      for (int s = 0; s < (n + 31) >> 5; ++s) k.tiles.ready(s);
+      k.tiles.finish();
+      return;
+    }
+    diff_columns<T, D, NC>(k.kf, (const T*)a.k, row0, ge, head_k);
+    diff_columns<T, D, NC>(k.vf, (const T*)a.v, row0, ge, head_k);
+    settle(k.kf);
+    settle(k.vf);
+    k.c = a.scale * kLog2e;
+    k.lam = lam;
+    k.tiles.ready(0);
+    k.sweep(n);
+    k.tiles.finish();
+  }
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int row = row0 + 16 * c + (lane & 15);
+    if (row >= ge) continue;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) {
+      store4((T*)a.d_k + (head_k + row) * D, dt, k.dk[dt][c] * (dt < 4 ? a.scale : lam * a.scale));
+      store4((T*)a.d_v + (head_k + row) * D, dt, k.dv[dt][c]);
     }
   }
 }
@@ -493,7 +539,8 @@ int check_diff(int64_t Nq, int64_t Nk, int H, int D, int G, float scale, int dty
 }
 
 int rows_of(int dtype) { return dtype == MOGA_F32 ? kRows<float> : kRows<unsigned short>; }
-int64_t diff_blocks(int64_t N, int H, int G, int dtype) { return (max_tiles(N, G, rows_of(dtype)) * H + 7) / 8 * 8; }
+int key_rows_of(int dtype) { return dtype == MOGA_F32 ? kKeyRows<float> : kKeyRows<unsigned short>; }
+int64_t diff_blocks(int64_t N, int H, int G, int rows) { return (max_tiles(N, G, rows) * H + 7) / 8 * 8; }
 size_t tile_bytes(int G) { return G > MOGA_MAX_GROUPS ? round_up(((size_t)G + 1) * sizeof(int32_t), 256) : 0; }
 
 // Pieces of a forward tile's keys: where the tiles leave CUs idle, as many as fill two blocks a CU, none under 256 keys of a mean group.
@@ -531,7 +578,7 @@ extern "C" int moga_diff_attn_fwd(const void* qh, const void* kh, const void* vh
   if (need && (!ws || ws_bytes < need)) return MOGA_ERR_WORKSPACE;
   const bool room = ws && ws_bytes >= moga_diff_attn_fwd_preferred(Nq, Nk, H, D, G, dtype);
   const int pieces = room ? diff_pieces(Nq, Nk, H, G, dtype) : 1;
-  const int64_t blocks = diff_blocks(Nq, H, G, dtype), rows = Nq * H;
+  const int64_t blocks = diff_blocks(Nq, H, G, rows_of(dtype)), rows = Nq * H;
   if (!grid_fits(blocks * pieces, 256) || !grid_fits((rows + 3) / 4, 256)) return MOGA_ERR_UNSUPPORTED;
   hipStream_t st = (hipStream_t)stream;
   int32_t* ts = G > MOGA_MAX_GROUPS ? (int32_t*)ws : nullptr;
@@ -573,7 +620,7 @@ extern "C" int moga_diff_attn_bwd(const void* d_oh, const void* qh, const void* 
     return MOGA_ERR_INVALID_ARG;
   const size_t need = moga_diff_attn_bwd_ws_bytes(Nq, H, G);
   if (need && (!ws || ws_bytes < need)) return MOGA_ERR_WORKSPACE;
-  const int64_t q_blocks = diff_blocks(Nq, H, G, dtype), k_blocks = diff_blocks(Nk, H, G, dtype), rows = Nq * H;
+  const int64_t q_blocks = diff_blocks(Nq, H, G, rows_of(dtype)), k_blocks = diff_blocks(Nk, H, G, key_rows_of(dtype)), rows = Nq * H;
   if (!grid_fits(q_blocks, 256) || !grid_fits(k_blocks, 256) || !grid_fits((rows + 15) / 16, 256)) return MOGA_ERR_UNSUPPORTED;
   hipStream_t st = (hipStream_t)stream;
   int32_t *tq = nullptr, *tk = nullptr;
@@ -581,7 +628,7 @@ extern "C" int moga_diff_attn_bwd(const void* d_oh, const void* qh, const void* 
     tq = (int32_t*)ws;
     tk = (int32_t*)((char*)ws + tile_bytes(G));
     tile_start_kernel<<<1, 1024, 0, st>>>(cu_seqlens_q, G, rows_of(dtype), tq);
-    tile_start_kernel<<<1, 1024, 0, st>>>(cu_seqlens_k, G, rows_of(dtype), tk);
+    tile_start_kernel<<<1, 1024, 0, st>>>(cu_seqlens_k, G, key_rows_of(dtype), tk);
   }
   floatx4_t* rc = (floatx4_t*)((char*)ws + 2 * tile_bytes(G));
   float* share = (float*)(rc + rows);
@@ -592,7 +639,10 @@ extern "C" int moga_diff_attn_bwd(const void* d_oh, const void* qh, const void* 
   do {                                                                                                                                 \
     diff_rows_kernel<T, D><<<(unsigned)((rows + 15) / 16), 256, 0, st>>>((const T*)d_oh, parts, lse, rows, rc, share);                  \
     diff_dq_kernel<T, D><<<(unsigned)q_blocks, 256, 0, st>>>(a);                                                                       \
-    if (Nk > 0) diff_dkdv_kernel<T, D><<<(unsigned)k_blocks, 256, 0, st>>>(b);                                                          \
+    if (Nk > 0) {                                                                                                                      \
+      if constexpr (sizeof(T) == 4) diff_dkdv_f32_kernel<T, D><<<(unsigned)k_blocks, 256, 0, st>>>(b);                                  \
+      else diff_dkdv_kernel<<<(unsigned)k_blocks, 256, 0, st>>>(b);                                                                    \
+    }                                                                                                                                  \
   } while (0)
   if (Nq > 0) {
     if (dtype == MOGA_BF16) MOGA_DIFF_BWD(unsigned short, 128);
