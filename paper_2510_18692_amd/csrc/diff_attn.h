@@ -56,7 +56,7 @@ __device__ __forceinline__ void diff_columns(Frag<T> (&f)[NC][D / 32], const T* 
 // nat(which, t, kb): operand t of the tile's rows (step_row), channels 32 kb ..; tr(which, dt): transposed, channels 16 dt .., all 32 rows.
 template <typename T, int D, bool ROWS = false, int KEEP = 1> struct DiffTiles;
 
-// With ROWS, 16 bytes of constants of every row beside them: row(i).
+// With ROWS, four constants of every row beside them: rows(v, i), constant v of rows i .. i + 3.
 // bf16: direct-to-LDS loads into a ring of four, as far ahead as the tiles that are kept allow.
 template <bool ROWS, int KEEP> struct DiffTiles<unsigned short, 128, ROWS, KEEP> {
   static constexpr int kTile = 32 * kHeadDim * 2, kLoads = 2 * kDmaLoads<4, 32> + ROWS, kAhead = 4 - KEEP, kRowSlot = 640;
@@ -68,12 +68,14 @@ template <bool ROWS, int KEEP> struct DiffTiles<unsigned short, 128, ROWS, KEEP>
   PipeDma dma;
   unsigned n_[2], t_[2][2], off, rows_lds, rows_own, rows_at;
   const void* rows_base;
-  // A wave moves 128 bytes of the 512, and the next wave's (the same bytes twice) with the lanes that are left.
+  // Wave v moves constant v of the 32 rows, and v + 1 (the same bytes twice) with the lanes that are left.  Each constant by itself: the four
+  // rows that a lane group wants are one read, and the four lane groups' reads lie in different banks (as 16 bytes a row they do not,
+  // and a read takes 50 cycles).
   __device__ __forceinline__ void issue(int s) {
     pipe_issue<4, 32, false>(dma, 32 * s, (s & 3) * kTile);
     if constexpr (ROWS) {
-      const int word = (threadIdx.x >> 6) * 32 + (threadIdx.x & 63), row = min(32 * s + (word >> 2), dma.last_row);
-      lds_dma4_soff(rows_base, (unsigned)row * 16u + (word & 3) * 4u, rows_own + (s & 3) * kRowSlot);
+      const int lane = threadIdx.x & 63, v = min((int)(threadIdx.x >> 6) + (lane >> 5), 3), row = min(32 * s + (lane & 31), dma.last_row);
+      lds_dma4_soff(rows_base, (unsigned)row * 16u + v * 4u, rows_own + (s & 3) * kRowSlot);
     }
   }
   __device__ __forceinline__ void start(Lds& lds, const unsigned short* a, const unsigned short* b, int n, const floatx4_t* rows = nullptr) {
@@ -109,7 +111,9 @@ template <bool ROWS, int KEEP> struct DiffTiles<unsigned short, 128, ROWS, KEEP>
   __device__ __forceinline__ void finish() { __builtin_amdgcn_s_waitcnt(waitcnt_vm(0)); }   // before the LDS is released
   __device__ __forceinline__ bf16x8_t nat(int which, int t, int kb) const { return read_nat<32>(n_[which] + off, t, kb); }
   __device__ __forceinline__ bf16x8_t tr(int which, int dt) const { return read_tr<32>(t_[which], off, dt); }
-  __device__ __forceinline__ floatx4_t row(int i) const { return *(const floatx4_t __attribute__((address_space(3)))*)(uintptr_t)(rows_at + 16 * i); }
+  __device__ __forceinline__ floatx4_t rows(int v, int i) const {
+    return *(const floatx4_t __attribute__((address_space(3)))*)(uintptr_t)(rows_at + 128 * v + 4 * i);
+  }
 };
 
 // fp32: through registers, one tile ahead.
@@ -117,13 +121,14 @@ template <int D, bool ROWS> struct DiffTiles<float, D, ROWS, 1> {
   static constexpr int kPitch = D + 4, kEach = 32 * D / 4 / 256;
   struct Lds {
     float a[32][kPitch], b[32][kPitch];
-    floatx4_t rows[ROWS ? 32 : 1];
+    float rows[ROWS ? 4 : 1][32];
   };
   Lds* lds;
   const float *pa, *pb;
   int last;
-  floatx4_t ra[kEach], rb[kEach], rr;
-  const floatx4_t* rows;
+  floatx4_t ra[kEach], rb[kEach];
+  float rr;
+  const floatx4_t* constants;
   __device__ __forceinline__ void fetch(int s) {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
@@ -132,11 +137,11 @@ template <int D, bool ROWS> struct DiffTiles<float, D, ROWS, 1> {
       ra[i] = *(const floatx4_t*)(pa + row * D + col);
       rb[i] = *(const floatx4_t*)(pb + row * D + col);
     }
-    if (ROWS && threadIdx.x < 32) rr = rows[min(32 * s + (int)threadIdx.x, last)];
+    if (ROWS && threadIdx.x < 128) rr = ((const float*)(constants + min(32 * s + (int)(threadIdx.x & 31), last)))[threadIdx.x >> 5];
   }
   __device__ __forceinline__ void start(Lds& l, const float* a, const float* b, int n, const floatx4_t* r = nullptr) {
     lds = &l;
-    rows = r;
+    constants = r;
     pa = a;
     pb = b;
     last = n - 1;
@@ -150,12 +155,12 @@ template <int D, bool ROWS> struct DiffTiles<float, D, ROWS, 1> {
       *(floatx4_t*)&lds->a[row][col] = ra[i];
       *(floatx4_t*)&lds->b[row][col] = rb[i];
     }
-    if (ROWS && threadIdx.x < 32) lds->rows[threadIdx.x] = rr;
+    if (ROWS && threadIdx.x < 128) lds->rows[threadIdx.x >> 5][threadIdx.x & 31] = rr;
     __syncthreads();
     fetch(s + 1);
   }
   __device__ __forceinline__ void finish() {}
-  __device__ __forceinline__ floatx4_t row(int i) const { return lds->rows[i]; }
+  __device__ __forceinline__ floatx4_t rows(int v, int i) const { return *(const floatx4_t*)&lds->rows[v][i]; }
   __device__ __forceinline__ FragF32 nat(int which, int t, int kb) const {
     const int lane = threadIdx.x & 63;
     const float* p = (which ? lds->b : lds->a)[step_row(lane & 15) + 4 * t] + 32 * kb + 8 * (lane >> 4);

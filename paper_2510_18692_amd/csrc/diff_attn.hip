@@ -418,17 +418,19 @@ __global__ __launch_bounds__(256, 1) void diff_dkdv_f32_kernel(DiffBwd a) {
 #pragma unroll
           for (int k = 0; k < NC; ++k) dp[k] = mma(f, vf[k][kb], kb == 0 ? floatx4_t{0.f, 0.f, 0.f, 0.f} : dp[k]);
         }
+        floatx4_t rc[4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) rc[v] = tiles.rows(v, 8 * g + 4 * t);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int q = 8 * g + 4 * t + i;
-          const floatx4_t rc = tiles.row(q);
 #pragma unroll
           for (int k = 0; k < NC; ++k) {
-            float p1 = fast_exp2(fmaf(s[0][k][i], c, -rc[0])), p2 = fast_exp2(fmaf(s[1][k][i], c, -rc[1]));
+            float p1 = fast_exp2(fmaf(s[0][k][i], c, -rc[0][i])), p2 = fast_exp2(fmaf(s[1][k][i], c, -rc[1][i]));
             if (left < 32 && q >= left) p1 = p2 = 0.f;
             pa[k][4 * t + i] = fmaf(-lam, p2, p1);
-            d1[k][4 * t + i] = p1 * (dp[k][i] - rc[2]);
-            d2[k][4 * t + i] = p2 * (rc[3] - dp[k][i]);
+            d1[k][4 * t + i] = p1 * (dp[k][i] - rc[2][i]);
+            d2[k][4 * t + i] = p2 * (rc[3][i] - dp[k][i]);
           }
         }
       }

@@ -26,49 +26,51 @@ struct DiffKeySweep {
   bf16x8_t kf[NC][4], vf[NC][4], ahead[kWin];
   floatx4_t dk[8][NC], dv[8][NC];
   Half h0, h1;
-  float c, lam, x[3], hold[3];
+  float c, lam;
   unsigned nat, tr[2];   // the lane's addresses: rows of the newer tile, transposed of the older
   Tiles tiles;
 
   __device__ __forceinline__ void load_rows(int t, Half& h) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) h.rc[i] = tiles.row(8 * ((threadIdx.x & 63) >> 4) + 4 * t + i);
+    for (int v = 0; v < 4; ++v) h.rc[v] = tiles.rows(v, 8 * ((threadIdx.x & 63) >> 4) + 4 * t);
   }
   // queries behind the last: weights of zero
   __device__ __forceinline__ void mask_rows(int t, int left, Half& h) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (8 * (int)((threadIdx.x & 63) >> 4) + 4 * t + i >= left) h.rc[i][0] = h.rc[i][1] = INFINITY;
+      if (8 * (int)((threadIdx.x & 63) >> 4) + 4 * t + i >= left) h.rc[0][i] = h.rc[1][i] = INFINITY;
   }
 
-  // Vector work on element e = (column, row) in parts of some 12 cycles.
+  // Vector work on element e = (column, row), in parts of some 12 cycles: a weight,
   __device__ __forceinline__ void weight(Half& h, int m, int e) {
     const int k = e >> 2, i = e & 3;
-    h.s[m][k][i] = fast_exp2(fmaf(h.s[m][k][i], c, -h.rc[i][m]));
+    h.s[m][k][i] = fast_exp2(fmaf(h.s[m][k][i], c, -h.rc[m][i]));
   }
-  __device__ __forceinline__ void rest_a(Half& h, int e) {
-    const int k = e >> 2, i = e & 3;
-    x[0] = fmaf(-lam, h.s[1][k][i], h.s[0][k][i]);
-    x[1] = h.s[0][k][i] * (h.dp[k][i] - h.rc[i][2]);
-    x[2] = h.rc[i][3] - h.dp[k][i];
-  }
-  __device__ __forceinline__ void rest_b(Half& h, int t, int e, Packed& p) {
-    const int k = e >> 2, i = e & 3;
-    x[2] *= h.s[1][k][i];
-    if (i & 1) {   // to nearest even: operands of the matrix products
-      p.a[k][2 * t + (i >> 1)] = pack_bf16x2(hold[0], x[0]);
-      p.d1[k][2 * t + (i >> 1)] = pack_bf16x2(hold[1], x[1]);
-      p.d2[k][2 * t + (i >> 1)] = pack_bf16x2(hold[2], x[2]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 3; ++j) hold[j] = x[j];
-    }
-  }
-
   // PREV: there is an older tile, `cur`; NEXT: a newer one, t = 0 of it to `nxt`; MORE: and one after that, which is waited for.
   template <bool PREV, bool NEXT, bool MORE>
   __device__ __forceinline__ void body(Packed& cur, Packed& nxt, int newer, int left) {
     bf16x8_t fr[32];
+    // All else of an element, in two parts (x: its results, y: those of the row before it).
+    float xa, x1, x2, ya, y1, y2;
+    auto rest_a = [&](Half& h, int e) {
+      const int k = e >> 2, i = e & 3;
+      xa = fmaf(-lam, h.s[1][k][i], h.s[0][k][i]);
+      x1 = h.s[0][k][i] * (h.dp[k][i] - h.rc[2][i]);
+      x2 = h.rc[3][i] - h.dp[k][i];
+    };
+    auto rest_b = [&](Half& h, int t, int e, Packed& p) {
+      const int k = e >> 2, i = e & 3;
+      x2 *= h.s[1][k][i];
+      if (i & 1) {   // to nearest even: operands of the matrix products
+        p.a[k][2 * t + (i >> 1)] = pack_bf16x2(ya, xa);
+        p.d1[k][2 * t + (i >> 1)] = pack_bf16x2(y1, x1);
+        p.d2[k][2 * t + (i >> 1)] = pack_bf16x2(y2, x2);
+      } else {
+        ya = xa;
+        y1 = x1;
+        y2 = x2;
+      }
+    };
     auto load = [&](int f) {   // in the order of use
       if (!PREV && f >= 8 && f < 24) f += 16;
       if (f < 8) fr[f] = read_nat<32>(nat + (f >> 2) * 4 * Tiles::kTile, 0, f & 3);
