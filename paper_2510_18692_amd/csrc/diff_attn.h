@@ -116,6 +116,56 @@ template <bool ROWS, int KEEP> struct DiffTiles<unsigned short, 128, ROWS, KEEP>
   }
 };
 
+// The same for a wave by itself: every fourth tile of the block's, a ring of two, no barriers.
+struct DiffWaveTiles {
+  static constexpr int kTile = 32 * kHeadDim * 2, kLoads = 2 * kDmaLoads<1, 32>;
+  struct Lds {
+    __attribute__((aligned(1024))) unsigned short a[2][32 * kHeadDim];
+    __attribute__((aligned(1024))) unsigned short b[2][32 * kHeadDim];
+  };
+  PipeDma dma;
+  unsigned n_[2], t_[2][2], off;
+  __device__ __forceinline__ void start(Lds& lds, const unsigned short* a, const unsigned short* b, int n, int first) {
+    const int lane = threadIdx.x & 63;
+    dma.kbase = uniform_ptr(a);
+    dma.vbase = uniform_ptr(b);
+    dma_lanes<1, 32>(dma, &lds.a[0][0], &lds.b[0][0], 0, lane);
+    dma.last_row = n - 1;
+    n_[0] = nat_address(&lds.a[0][0], lane);
+    n_[1] = nat_address(&lds.b[0][0], lane);
+    tr_addresses(t_[0], &lds.a[0][0], lane);
+    tr_addresses(t_[1], &lds.b[0][0], lane);
+    off = kTile;
+    issue(first, 0);
+    issue(first + 4, kTile);
+  }
+  __device__ __forceinline__ void issue(int tile, unsigned slot) {   // rows are clamped: always issued
+    // 16 rows (1 KB of LDS of each quarter) at a time
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int row = 16 * h + (int)((threadIdx.x & 63) >> 2);
+      const unsigned at = (unsigned)min(32 * tile + row, dma.last_row) * (kHeadDim * 2) + ((((threadIdx.x & 3) ^ lds_swizzle(row))) << 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        lds_dma16_soff(dma.kbase, at + 64 * i, dma.lds_k + slot + h * 1024 + i * kQuarterBytes<32>);
+        lds_dma16_soff(dma.vbase, at + 64 * i, dma.lds_v + slot + h * 1024 + i * kQuarterBytes<32>);
+      }
+    }
+  }
+  __device__ __forceinline__ void next() {   // the next of the wave's tiles may be read
+    off ^= kTile;
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(kLoads));
+    asm volatile("" ::: "memory");
+  }
+  __device__ __forceinline__ void refill(int tile) {   // its slot is read no more
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    issue(tile, off);
+  }
+  __device__ __forceinline__ void finish() { __builtin_amdgcn_s_waitcnt(waitcnt_vm(0)); }
+  __device__ __forceinline__ bf16x8_t nat(int which, int t, int kb) const { return read_nat<32>(n_[which] + off, t, kb); }
+  __device__ __forceinline__ bf16x8_t tr(int which, int dt) const { return read_tr<32>(t_[which], off, dt); }
+};
+
 // fp32: through registers, one tile ahead.
 template <int D, bool ROWS> struct DiffTiles<float, D, ROWS, 1> {
   static constexpr int kPitch = D + 4, kEach = 32 * D / 4 / 256;

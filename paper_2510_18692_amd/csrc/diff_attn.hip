@@ -190,34 +190,135 @@ __global__ __launch_bounds__(256, 2) void diff_fwd_kernel(DiffFwd a) {
   }
 }
 
-// The pieces of a row put together: a wave per row, D / 64 channels of both maps per lane.
+// bf16 calls of few queries a group: the blocks go by the keys, `chunk` of a group each, and take all queries of the group, 16 at a time.  The
+// four waves share the keys out, every fourth tile each from a ring of its own without a barrier, and add up what they have.  Bound by HBM:
+// 4 x 32 KB are on their way to a CU.  Sums and maxima go to part and stat, for piece (first key / chunk) of the group.
+__global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd a, int chunk) {
+  constexpr int D = kHeadDim;
+  typedef unsigned short T;
+  __shared__ union {
+    DiffWaveTiles::Lds tiles[4];
+    struct { float o[4][2][16][D], stat[4][2][16][2]; } sums;
+  } lds;
+  WorkTile w;
+  if (!find_work<false>(a.cu_k, a.tile_start, a.G, a.H, chunk, blockIdx.x, w)) return;
+  const int head = w.head, gs = __builtin_amdgcn_readfirstlane(w.ti.tile_row);
+  const int n = __builtin_amdgcn_readfirstlane(min(w.ti.row_end, w.ti.tile_row + chunk)) - gs, piece = (gs - w.ti.row_begin) / chunk;
+  const int q_first = a.cu_q[w.ti.group], q_end = a.cu_q[w.ti.group + 1];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15;
+  const int64_t head_q = (int64_t)head * a.Nq, head_k = (int64_t)head * a.Nk;
+  const int tiles_n = (n + 31) >> 5;
+  const float c = a.scale * kLog2e;
+  for (int row0 = q_first; row0 < q_end; row0 += 16) {
+    DiffState<D, 1> st;
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      st.m[m][0] = st.l[m][0] = 0.f;
+      st.thresh[m][0] = -INFINITY;
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) st.o[m][dt][0] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    bf16x8_t qf[1][4];
+    diff_columns<T, D, 1>(qf, (const T*)a.q, row0, q_end, head_q);
+    settle(qf);
+    if (wave < tiles_n) {
+      DiffWaveTiles tiles;
+      tiles.start(lds.tiles[wave], (const T*)a.k + (head_k + gs) * D, (const T*)a.v + (head_k + gs) * D, n, wave);
+      for (int t = wave; t < tiles_n; t += 4) {
+        tiles.next();
+        diff_fwd_step<T, D, 1>(tiles, qf, st, c, n - 32 * t);
+        tiles.refill(t + 8);
+      }
+      tiles.finish();
+    }
+    __syncthreads();   // the rings are read no more
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      float l = st.l[m][0] + __shfl_xor(st.l[m][0], 16, kWave);
+      l += __shfl_xor(l, 32, kWave);
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) store4(lds.sums.o[wave][m][r], dt, st.o[m][dt][0]);
+      if (lane < 16) {
+        lds.sums.stat[wave][m][r][0] = st.thresh[m][0] == -INFINITY ? -INFINITY : st.m[m][0];
+        lds.sums.stat[wave][m][r][1] = l;
+      }
+    }
+    __syncthreads();
+    const int used = min(4, tiles_n);
+    for (int i = threadIdx.x; i < 2 * 16 * (D / 4); i += 256) {
+      const int col = i % (D / 4) * 4, m = i / (D / 4) / 16, q = i / (D / 4) % 16;
+      if (row0 + q >= q_end) continue;
+      float mx = -INFINITY, l = 0.f;
+      for (int k = 0; k < used; ++k) mx = fmaxf(mx, lds.sums.stat[k][m][q][0]);
+      floatx4_t o = {0.f, 0.f, 0.f, 0.f};
+      for (int k = 0; k < used; ++k) {
+        const float f = mx == -INFINITY ? 1.f : fast_exp2(lds.sums.stat[k][m][q][0] - mx);
+        l = fmaf(lds.sums.stat[k][m][q][1], f, l);
+        o += *(const floatx4_t*)&lds.sums.o[k][m][q][col] * f;
+      }
+      const int64_t at = ((int64_t)piece * a.H * a.Nq + head_q + row0 + q) * 2 + m;
+      *(floatx4_t*)(a.part + at * D + col) = o;
+      if (col == 0) *(floatx2_t*)(a.stat + at * 2) = floatx2_t{mx, l};
+    }
+    __syncthreads();   // the sums are read no more
+  }
+}
+
+// The pieces of a row put together: a wave per row, D / 64 channels of both maps per lane.  chunk > 0: a piece for every `chunk` keys of the
+// row's group (diff_few_kernel), else `pieces`.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void diff_merge_kernel(DiffFwd a, int pieces) {
+__global__ __launch_bounds__(256) void diff_merge_kernel(DiffFwd a, int pieces, int chunk) {
   constexpr int V = D / 64;
   const int lane = threadIdx.x & 63;
   const int64_t rows = (int64_t)a.H * a.Nq, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (row >= rows || row % a.Nq >= a.cu_q[a.G]) return;   // rows behind the last group stay as they are
-  float o[2][V], lse[2];
+  if (chunk > 0) {
+    TileInfo ti;   // tiles of one row: the entries of cu_q are their own sums
+    find_tile_presummed(a.cu_q, a.cu_q, a.G, 1, (int)(row % a.Nq), ti);
+    pieces = (a.cu_k[ti.group + 1] - a.cu_k[ti.group] + chunk - 1) / chunk;
+  }
+  float o[2][V], lse[2], mx[2], l[2];
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
-    float mx = -INFINITY, l = 0.f;
-    bool empty = true;
-    for (int p = 0; p < pieces; ++p) mx = fmaxf(mx, a.stat[((p * rows + row) * 2 + m) * 2]);
+    mx[m] = -INFINITY;
+    l[m] = 0.f;
 #pragma unroll
     for (int i = 0; i < V; ++i) o[m][i] = 0.f;
-    for (int p = 0; p < pieces; ++p) {
-      const int64_t at = (p * rows + row) * 2 + m;
-      const floatx2_t s = *(const floatx2_t*)(a.stat + at * 2);
-      if (s[1] == -1.f) continue;   // no keys
-      empty = false;
-      const float f = mx == -INFINITY ? 1.f : fast_exp2(s[0] - mx);
-      l = fmaf(s[1], f, l);
+  }
+  bool empty = true;
+  for (int p0 = 0; p0 < pieces; p0 += 64) {   // (maximum, sum) of 64 pieces at a time, a lane each; a sum of -1: no keys
+    floatx4_t s = {-INFINITY, -1.f, -INFINITY, -1.f};
+    if (p0 + lane < pieces) s = *(const floatx4_t*)(a.stat + ((p0 + lane) * rows + row) * 4);
+    const bool none = s[1] == -1.f;
+    if (__builtin_amdgcn_ballot_w64(!none) == 0) continue;
+    empty = false;
+    float f[2];
 #pragma unroll
-      for (int i = 0; i < V; ++i) o[m][i] = fmaf(a.part[at * D + lane * V + i], f, o[m][i]);
+    for (int m = 0; m < 2; ++m) {
+      const float now = fmaxf(mx[m], wave_max(s[2 * m])), before = mx[m] == now ? 1.f : fast_exp2(mx[m] - now);
+      f[m] = none ? 0.f : now == -INFINITY ? 1.f : fast_exp2(s[2 * m] - now);
+      mx[m] = now;
+      l[m] = fmaf(l[m], before, wave_sum(none ? 0.f : s[2 * m + 1] * f[m]));
+#pragma unroll
+      for (int i = 0; i < V; ++i) o[m][i] *= before;
     }
+    const int n = min(64, pieces - p0);
+#pragma unroll 4
+    for (int p = 0; p < n; ++p) {
+      const float* part = a.part + ((p0 + p) * rows + row) * 2 * D + lane * V;
 #pragma unroll
-    for (int i = 0; i < V; ++i) o[m][i] = empty ? 0.f : o[m][i] / l;
-    lse[m] = empty ? -INFINITY : logf(l) + mx * 0.6931471805599453f;
+      for (int m = 0; m < 2; ++m) {
+        const float w = __shfl(f[m], p, kWave);
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[m][i] = fmaf(part[m * D + i], w, o[m][i]);
+      }
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[m][i] = empty ? 0.f : o[m][i] / l[m];
+    lse[m] = empty ? -INFINITY : logf(l[m]) + mx[m] * 0.6931471805599453f;
   }
   const float lam = a.lambda[row / a.Nq];
   T* out = (T*)a.o + row * D + lane * V;
@@ -519,9 +620,13 @@ __global__ __launch_bounds__(1024) void diff_dlambda_kernel(const float* __restr
   __shared__ float acc[16];
   const float* p = share + blockIdx.x * Nq;
   const int n = Nq > 0 ? cu_q[G] : 0;
-  float s = 0.f;
-  for (int i = threadIdx.x; i < n; i += 1024) s += p[i];
-  s = wave_sum(s);
+  float u[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};   // eight loads on their way
+  int i = threadIdx.x;
+  for (; i + 7 * 1024 < n; i += 8 * 1024)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) u[k] += p[i + 1024 * k];
+  for (; i < n; i += 1024) u[0] += p[i];
+  float s = wave_sum(((u[0] + u[1]) + (u[2] + u[3])) + ((u[4] + u[5]) + (u[6] + u[7])));
   if ((threadIdx.x & 63) == 0) acc[threadIdx.x >> 6] = s;
   __syncthreads();
   if (threadIdx.x < 64) {
@@ -545,13 +650,23 @@ int key_rows_of(int dtype) { return dtype == MOGA_F32 ? kKeyRows<float> : kKeyRo
 int64_t diff_blocks(int64_t N, int H, int G, int rows) { return (max_tiles(N, G, rows) * H + 7) / 8 * 8; }
 size_t tile_bytes(int G) { return G > MOGA_MAX_GROUPS ? round_up(((size_t)G + 1) * sizeof(int32_t), 256) : 0; }
 
-// Pieces of a forward tile's keys: where the tiles leave CUs idle, as many as fill two blocks a CU, none under 256 keys of a mean group.
-int diff_pieces(int64_t Nq, int64_t Nk, int H, int G, int dtype) {
-  const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(max_tiles(Nq, G, rows_of(dtype)), Nq)) * H;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, 2 * kCus / blocks), Nk / G / 256));
-}
 size_t diff_piece_bytes(int64_t Nq, int H, int D) { return (size_t)Nq * H * 2 * (D + 2) * sizeof(float); }
 
+// How a forward call shares out its keys.  chunk > 0: diff_few_kernel, pieces of `chunk` keys, at most `pieces` of a group; else pieces of every
+// tile of queries (1: whole).
+struct DiffSplit { int pieces, chunk; };
+DiffSplit diff_split(int64_t Nq, int64_t Nk, int H, int D, int G, int dtype) {
+  // Up to 16 queries a group the matrix products of a tile of 128 are idle work, and three of its waves too: pieces of keys for some two rounds
+  // of blocks, one a CU, none under 256 keys, and as many as 256 MB hold (one group might have all the keys).
+  const int64_t most = (256 << 20) / (int64_t)diff_piece_bytes(Nq, H, D);
+  if (dtype == MOGA_BF16 && Nq <= 16 * (int64_t)G && Nk / G >= 128 && most >= 1) {
+    const int64_t chunk = round_up((size_t)std::max({(int64_t)256, Nk * H / (2 * kCus), (Nk + most - 1) / most}), 128);
+    return {(int)((Nk + chunk - 1) / chunk), (int)chunk};
+  }
+  // Else where the tiles leave CUs idle, as many pieces as fill two blocks a CU, none under 256 keys of a mean group.
+  const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(max_tiles(Nq, G, rows_of(dtype)), Nq)) * H;
+  return {(int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, 2 * kCus / blocks), Nk / G / 256)), 0};
+}
 }  // namespace
 }  // namespace moga
 
@@ -561,8 +676,8 @@ extern "C" size_t moga_diff_attn_fwd_ws_bytes(int G) { return tile_bytes(G); }
 // With the pieces of the keys, for calls of few tiles.
 extern "C" size_t moga_diff_attn_fwd_preferred(int64_t Nq, int64_t Nk, int H, int D, int G, int dtype) {
   if (Nq <= 0 || check_diff(Nq, Nk, H, D, G, 1.f, dtype) != MOGA_OK) return 0;
-  const int pieces = diff_pieces(Nq, Nk, H, G, dtype);
-  return tile_bytes(G) + (pieces > 1 ? pieces * diff_piece_bytes(Nq, H, D) : 0);
+  const DiffSplit s = diff_split(Nq, Nk, H, D, G, dtype);
+  return tile_bytes(G) + (s.pieces > 1 || s.chunk ? s.pieces * diff_piece_bytes(Nq, H, D) : 0);
 }
 extern "C" size_t moga_diff_attn_bwd_ws_bytes(int64_t Nq, int H, int G) {
   return Nq > 0 ? tile_bytes(G) * 2 + (size_t)Nq * H * (sizeof(floatx4_t) + sizeof(float)) : 0;
@@ -579,15 +694,22 @@ extern "C" int moga_diff_attn_fwd(const void* qh, const void* kh, const void* vh
   const size_t need = moga_diff_attn_fwd_ws_bytes(G);
   if (need && (!ws || ws_bytes < need)) return MOGA_ERR_WORKSPACE;
   const bool room = ws && ws_bytes >= moga_diff_attn_fwd_preferred(Nq, Nk, H, D, G, dtype);
-  const int pieces = room ? diff_pieces(Nq, Nk, H, G, dtype) : 1;
-  const int64_t blocks = diff_blocks(Nq, H, G, rows_of(dtype)), rows = Nq * H;
-  if (!grid_fits(blocks * pieces, 256) || !grid_fits((rows + 3) / 4, 256)) return MOGA_ERR_UNSUPPORTED;
+  const DiffSplit split = room ? diff_split(Nq, Nk, H, D, G, dtype) : DiffSplit{1, 0};
+  const int pieces = split.pieces;
+  const int64_t blocks = split.chunk ? diff_blocks(Nk, H, G, split.chunk) : diff_blocks(Nq, H, G, rows_of(dtype)), rows = Nq * H;
+  if (!grid_fits(split.chunk ? blocks : blocks * pieces, 256) || !grid_fits((rows + 3) / 4, 256)) return MOGA_ERR_UNSUPPORTED;
   hipStream_t st = (hipStream_t)stream;
   int32_t* ts = G > MOGA_MAX_GROUPS ? (int32_t*)ws : nullptr;
   DiffFwd a = {qh, kh, vh, lambda, cu_seqlens_q, cu_seqlens_k, ts, Nq, Nk, H, G, softmax_scale, oh, parts, lse, nullptr, nullptr};
-  if (pieces > 1) {
+  if (pieces > 1 || split.chunk) {
     a.part = (float*)((char*)ws + tile_bytes(G));
     a.stat = a.part + (size_t)pieces * rows * 2 * D;
+  }
+  if (split.chunk) {
+    if (ts) tile_start_kernel<<<1, 1024, 0, st>>>(cu_seqlens_k, G, split.chunk, ts);
+    diff_few_kernel<<<(unsigned)blocks, 256, 0, st>>>(a, split.chunk);
+    diff_merge_kernel<unsigned short, 128><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a, pieces, split.chunk);
+    return launch_status();
   }
   if (ts) tile_start_kernel<<<1, 1024, 0, st>>>(cu_seqlens_q, G, rows_of(dtype), ts);
   const dim3 grid((unsigned)blocks, (unsigned)pieces);
@@ -595,7 +717,7 @@ extern "C" int moga_diff_attn_fwd(const void* qh, const void* kh, const void* vh
   do {                                                                               \
     if (pieces > 1) {                                                                \
       diff_fwd_kernel<T, D, true><<<grid, 256, 0, st>>>(a);                          \
-      diff_merge_kernel<T, D><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a, pieces); \
+      diff_merge_kernel<T, D><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a, pieces, 0); \
     } else {                                                                         \
       diff_fwd_kernel<T, D, false><<<grid, 256, 0, st>>>(a);                         \
     }                                                                                \

@@ -91,6 +91,16 @@ def test_more_groups_than_the_lookup_takes(D, dtype):
     _check(_run(*t, cu_q, cu_k, 0.125), *t, cu_q, cu_k, 0.125, near=False)
 
 
+@pytest.mark.parametrize("groups,longest", [(5, 3000), (70, 700), (300, 200)])
+def test_a_few_queries_a_group(groups, longest):
+    """Groups of 0 to 40 queries, 8 on average, and 0 to `longest` keys."""
+    g = torch.Generator().manual_seed(groups)
+    cu_q = _cu([int(x) for x in torch.randint(0, 17, (groups - 1,), generator=g)] + [40])
+    cu_k = _cu([longest] + [int(x) for x in torch.randint(0, longest + 1, (groups - 1,), generator=g)])
+    t = _inputs(2, 128, torch.bfloat16, cu_q, cu_k, 31)
+    _check(_run(*t, cu_q, cu_k, 0.125), *t, cu_q, cu_k, 0.125, near=False)
+
+
 @pytest.mark.parametrize("spread", [1e-3, 12.0, 60.0])
 @pytest.mark.parametrize("D,dtype", [(128, torch.bfloat16), (128, torch.float32)])
 def test_flat_and_peaked_maps(D, dtype, spread):
