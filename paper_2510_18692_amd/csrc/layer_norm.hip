@@ -3,8 +3,9 @@
 //   mu = mean x, rstd = 1 / sqrt(mean (x - mu)^2 + eps), xh = (x - mu) rstd, y = xh w + b
 //   g = dy w, dx = rstd (g - mean g - xh mean(g xh)), dw = sum over rows of dy xh, db = sum over rows of dy
 //
-// Bound by HBM: a row is read once into registers, where both passes over it (mean, then centred squares) run, and written once.
-// A row belongs to 16 lanes, a wave or a block, so that a lane holds at most eight loads of 16 bytes.
+// Bound by HBM: a row is read once into registers, where both passes over it (mean, then centred squares) run, and written once, while the
+// next row is on its way.  A row belongs to 16 lanes, a wave, or a block of as many waves as give a lane 16 columns or fewer (of 8 waves beyond
+// 8,192): the weights, their two sums, x and dy of 16 columns leave room for three waves a SIMD.
 #include <algorithm>
 #include <cmath>
 
@@ -49,15 +50,15 @@ __device__ __forceinline__ float to_f32(unsigned short v) { return bf16_bits_to_
 __device__ __forceinline__ void from_f32(float& d, float v) { d = v; }
 __device__ __forceinline__ void from_f32(unsigned short& d, float v) { d = f32_to_bf16_bits(v); }
 
-// Columns col .. col + V - 1 of a row of C; zeros past its end.
-template <typename T, int V>
-__device__ __forceinline__ void load_part(const T* __restrict__ row, int col, int C, float (&f)[V]) {
-  if (col + V <= C) {
-    unpack(*(const Bytes16<T>*)(row + col), f);
-  } else {
+// Columns col .. col + V - 1 of a row of C, as they lie there; zeros past its end.
+template <typename T>
+__device__ __forceinline__ Bytes16<T> load_part(const T* __restrict__ row, int col, int C) {
+  constexpr int V = kPer16<T>;
+  if (col + V <= C) return *(const Bytes16<T>*)(row + col);
+  float f[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = col + i < C ? to_f32(row[col + i]) : 0.f;
-  }
+  for (int i = 0; i < V; ++i) f[i] = col + i < C ? to_f32(row[col + i]) : 0.f;
+  return pack(f);   // exact: values of T
 }
 template <typename T, int V>
 __device__ __forceinline__ void store_part(T* __restrict__ row, int col, int C, const float (&f)[V]) {
@@ -72,51 +73,87 @@ __device__ __forceinline__ void store_part(T* __restrict__ row, int col, int C, 
 // fp32 weights of the same columns; `other` where there are none.
 template <int V>
 __device__ __forceinline__ void load_weights(const float* __restrict__ w, int col, int C, float other, float (&f)[V]) {
+  if (w && col + V <= C) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) f[i] = w && col + i < C ? w[col + i] : other;
+    for (int i = 0; i < V; i += 4) {
+      const Bytes16<float> b = *(const Bytes16<float>*)(w + col + i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[i + e] = __uint_as_float(b.w[e]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = w && col + i < C ? w[col + i] : other;
+  }
 }
 
+// How the rows are dealt out: LANES = 16 or 64 to a row, four waves a block; LANES = 0: a row to a block of any number of waves.
+template <int LANES>
+struct Deal {
+  int lanes, lane;   // of the row
+  int64_t row, step;
+  __device__ __forceinline__ Deal() {
+    lanes = LANES ? LANES : blockDim.x;
+    lane = LANES ? threadIdx.x % LANES : threadIdx.x;
+    const int rows = LANES ? 256 / LANES : 1;
+    row = (int64_t)blockIdx.x * rows + (LANES ? threadIdx.x / LANES : 0);
+    step = (int64_t)gridDim.x * rows;
+  }
+};
+
 // Sums over the lanes of a row.  A row of a whole block goes through LDS: one barrier a sum, two buffers in turn.
+constexpr int kMaxWaves = 8;
 template <int LANES, int K>
 struct RowSum {
-  float (*lds)[4][K];   // [2][4 waves][K]
+  float (*lds)[kMaxWaves][K];   // [2][waves][K]
   int turn = 0;
   __device__ __forceinline__ void operator()(float (&v)[K]) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = lanes_sum<(LANES < 64 ? LANES : 64)>(v[k]);
-    if constexpr (LANES > 64) {
+    for (int k = 0; k < K; ++k) v[k] = lanes_sum<(LANES ? LANES : 64)>(v[k]);
+    if constexpr (LANES == 0) {
       if ((threadIdx.x & 63) == 0)
 #pragma unroll
         for (int k = 0; k < K; ++k) lds[turn][threadIdx.x >> 6][k] = v[k];
       __syncthreads();
+      const int waves = blockDim.x >> 6, lane = threadIdx.x & 15;
 #pragma unroll
-      for (int k = 0; k < K; ++k) v[k] = (lds[turn][0][k] + lds[turn][1][k]) + (lds[turn][2][k] + lds[turn][3][k]);
+      for (int k = 0; k < K; ++k) v[k] = lanes_sum<16>(lane < waves ? lds[turn][lane & (kMaxWaves - 1)][k] : 0.f);
       turn ^= 1;
     }
   }
 };
 
-// LANES per row, PARTS loads per lane; lane t holds the columns (part * LANES + t) * V ..
+// PARTS loads per lane; lane t holds the columns (part * lanes + t) * V ..
 template <typename T, int LANES, int PARTS>
-__global__ __launch_bounds__(256) void layer_norm_fwd_kernel(const T* __restrict__ x, const float* __restrict__ w, const float* __restrict__ b,
-                                                             int64_t N, int C, float eps, T* __restrict__ y, float* __restrict__ mean,
-                                                             float* __restrict__ rstd) {
-  constexpr int V = kPer16<T>, ROWS = 256 / LANES;
-  __shared__ float lds[2][4][1];
+__global__ __launch_bounds__(LANES ? 256 : 64 * kMaxWaves) void layer_norm_fwd_kernel(const T* __restrict__ x, const float* __restrict__ w,
+                                                                            const float* __restrict__ b, int64_t N, int C, float eps,
+                                                                            T* __restrict__ y, float* __restrict__ mean,
+                                                                            float* __restrict__ rstd) {
+  constexpr int V = kPer16<T>;
+  __shared__ float lds[2][kMaxWaves][1];
   RowSum<LANES, 1> sum{lds};
-  const int t = threadIdx.x % LANES;
+  Deal<LANES> d;
+  int col[PARTS];
+  Bytes16<T> next[PARTS];
   float wf[PARTS][V], bf[PARTS][V];
 #pragma unroll
   for (int p = 0; p < PARTS; ++p) {
-    load_weights(w, (p * LANES + t) * V, C, 1.f, wf[p]);
-    load_weights(b, (p * LANES + t) * V, C, 0.f, bf[p]);
+    col[p] = (p * d.lanes + d.lane) * V;
+    if (d.row < N) next[p] = load_part(x + d.row * C, col[p], C);
+  }
+#pragma unroll
+  for (int p = 0; p < PARTS; ++p) {
+    load_weights(w, col[p], C, 1.f, wf[p]);
+    load_weights(b, col[p], C, 0.f, bf[p]);
   }
   const float n = (float)C;   // divided by: the mean of equal values is their value
-  for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES; row < N; row += (int64_t)gridDim.x * ROWS) {
+  for (; d.row < N; d.row += d.step) {
     float f[PARTS][V];
     float s[1] = {0.f};
 #pragma unroll
-    for (int p = 0; p < PARTS; ++p) load_part(x + row * C, (p * LANES + t) * V, C, f[p]);
+    for (int p = 0; p < PARTS; ++p) unpack(next[p], f[p]);
+    if (d.row + d.step < N)
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) next[p] = load_part(x + (d.row + d.step) * C, col[p], C);
 #pragma unroll
     for (int p = 0; p < PARTS; ++p)
 #pragma unroll
@@ -128,7 +165,7 @@ __global__ __launch_bounds__(256) void layer_norm_fwd_kernel(const T* __restrict
     for (int p = 0; p < PARTS; ++p)
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        f[p][i] = (p * LANES + t) * V + i < C ? f[p][i] - mu : 0.f;
+        f[p][i] = col[p] + i < C ? f[p][i] - mu : 0.f;
         s[0] = fmaf(f[p][i], f[p][i], s[0]);
       }
     sum(s);
@@ -137,11 +174,11 @@ __global__ __launch_bounds__(256) void layer_norm_fwd_kernel(const T* __restrict
     for (int p = 0; p < PARTS; ++p) {
 #pragma unroll
       for (int i = 0; i < V; ++i) f[p][i] = fmaf(f[p][i] * r, wf[p][i], bf[p][i]);
-      store_part(y + row * C, (p * LANES + t) * V, C, f[p]);
+      store_part(y + d.row * C, col[p], C, f[p]);
     }
-    if (mean && t == 0) {
-      mean[row] = mu;
-      rstd[row] = r;
+    if (mean && d.lane == 0) {
+      mean[d.row] = mu;
+      rstd[d.row] = r;
     }
   }
 }
@@ -149,30 +186,47 @@ __global__ __launch_bounds__(256) void layer_norm_fwd_kernel(const T* __restrict
 // dx, and this block's share of dw and db at part[block][2][C] (DW).  The shares of the rows that run beside each other in a block are
 // added in a fixed order, and so are the blocks': results repeat bit by bit.
 template <typename T, int LANES, int PARTS, bool DW>
-__global__ __launch_bounds__(256) void layer_norm_bwd_kernel(const T* __restrict__ dy, const T* __restrict__ x, const float* __restrict__ w,
-                                                             const float* __restrict__ mean, const float* __restrict__ rstd, int64_t N, int C,
-                                                             T* __restrict__ dx, float* __restrict__ part) {
+__global__ __launch_bounds__(LANES ? 256 : 64 * kMaxWaves) void layer_norm_bwd_kernel(const T* __restrict__ dy, const T* __restrict__ x,
+                                                                            const float* __restrict__ w, const float* __restrict__ mean,
+                                                                            const float* __restrict__ rstd, int64_t N, int C,
+                                                                            T* __restrict__ dx, float* __restrict__ part) {
 #pragma clang fp contract(off)   // g is one value in its mean and in what the mean is taken from
-  constexpr int V = kPer16<T>, ROWS = 256 / LANES;
-  __shared__ float lds[2][4][2];
+  constexpr int V = kPer16<T>;
+  __shared__ float lds[2][kMaxWaves][2];
   RowSum<LANES, 2> sum{lds};
-  const int t = threadIdx.x % LANES;
+  Deal<LANES> d;
+  int col[PARTS];
+  Bytes16<T> next_x[PARTS], next_g[PARTS];
+  float next_mu = 0.f, next_r = 0.f;
+  auto fetch = [&](int64_t row) {
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) {
+      next_x[p] = load_part(x + row * C, col[p], C);
+      next_g[p] = load_part(dy + row * C, col[p], C);
+    }
+    next_mu = mean[row];
+    next_r = rstd[row];
+  };
+#pragma unroll
+  for (int p = 0; p < PARTS; ++p) col[p] = (p * d.lanes + d.lane) * V;
+  if (d.row < N) fetch(d.row);
   float wf[PARTS][V], dw[PARTS][V], db[PARTS][V];
 #pragma unroll
   for (int p = 0; p < PARTS; ++p) {
-    load_weights(w, (p * LANES + t) * V, C, 1.f, wf[p]);
+    load_weights(w, col[p], C, 1.f, wf[p]);
 #pragma unroll
     for (int i = 0; i < V; ++i) dw[p][i] = db[p][i] = 0.f;
   }
   const float n = (float)C;
-  for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES; row < N; row += (int64_t)gridDim.x * ROWS) {
+  for (; d.row < N; d.row += d.step) {
     float f[PARTS][V], g[PARTS][V];
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) {
-      load_part(x + row * C, (p * LANES + t) * V, C, f[p]);
-      load_part(dy + row * C, (p * LANES + t) * V, C, g[p]);
+      unpack(next_x[p], f[p]);
+      unpack(next_g[p], g[p]);
     }
-    const float mu = mean[row], r = rstd[row];
+    const float mu = next_mu, r = next_r;
+    if (d.row + d.step < N) fetch(d.row + d.step);
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int p = 0; p < PARTS; ++p)
@@ -193,22 +247,20 @@ __global__ __launch_bounds__(256) void layer_norm_bwd_kernel(const T* __restrict
     for (int p = 0; p < PARTS; ++p) {
 #pragma unroll
       for (int i = 0; i < V; ++i) f[p][i] = r * (g[p][i] - m0 - f[p][i] * m1);
-      store_part(dx + row * C, (p * LANES + t) * V, C, f[p]);
+      store_part(dx + d.row * C, col[p], C, f[p]);
     }
   }
   if constexpr (DW) {
     float* out = part + (size_t)blockIdx.x * 2 * C;
-    if constexpr (LANES == 256) {
+    if constexpr (LANES == 0) {
 #pragma unroll
       for (int p = 0; p < PARTS; ++p)
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const int col = (p * LANES + t) * V + i;
-          if (col < C) {
-            out[col] = dw[p][i];
-            out[C + col] = db[p][i];
+        for (int i = 0; i < V; ++i)
+          if (col[p] + i < C) {
+            out[col[p] + i] = dw[p][i];
+            out[C + col[p] + i] = db[p][i];
           }
-        }
     } else {
       __shared__ float acc[2][LANES * PARTS * V];
       const int wave = threadIdx.x >> 6;
@@ -227,16 +279,15 @@ __global__ __launch_bounds__(256) void layer_norm_bwd_kernel(const T* __restrict
           for (int p = 0; p < PARTS; ++p)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-              const int col = (p * LANES + t) * V + i;
-              acc[0][col] = k == 0 ? dw[p][i] : acc[0][col] + dw[p][i];
-              acc[1][col] = k == 0 ? db[p][i] : acc[1][col] + db[p][i];
+              acc[0][col[p] + i] = k == 0 ? dw[p][i] : acc[0][col[p] + i] + dw[p][i];
+              acc[1][col[p] + i] = k == 0 ? db[p][i] : acc[1][col[p] + i] + db[p][i];
             }
         }
         __syncthreads();
       }
-      for (int col = threadIdx.x; col < C; col += 256) {
-        out[col] = acc[0][col];
-        out[C + col] = acc[1][col];
+      for (int c = threadIdx.x; c < C; c += 256) {
+        out[c] = acc[0][c];
+        out[C + c] = acc[1][c];
       }
     }
   }
@@ -270,41 +321,46 @@ __global__ __launch_bounds__(256) void layer_norm_dw_kernel(const float* __restr
   }
 }
 
-// Lanes per row: 16 up to two loads a lane, a wave up to four, else a block.
-int norm_lanes(int C, int dtype) {
-  const int v = dtype == MOGA_F32 ? 4 : 8;
-  return C <= 2 * 16 * v ? 16 : C <= 4 * 64 * v ? 64 : 256;
+// 16 columns a lane at most: a row goes to 16 lanes up to 256 columns, to a wave up to 1,024, else to a block of a wave per 1,024; beyond 8,192
+// columns to 8 waves, which have registers for 32 a lane.
+struct NormShape {
+  int lanes, parts, waves, rows;   // lanes of a row (0: the block), loads a lane; waves and rows of a block
+};
+NormShape norm_shape(int C, int dtype) {
+  const int v = dtype == MOGA_F32 ? 4 : 8, waves = std::min(kMaxWaves, (C + 1023) / 1024);
+  auto parts = [&](int lanes) { return (C + lanes * v - 1) / (lanes * v); };
+  if (C <= 256) return {16, parts(16), 4, 16};
+  if (C <= 1024) return {64, parts(64), 4, 4};
+  return {0, parts(64 * waves), waves, 1};
 }
-int64_t norm_blocks(int64_t N, int C, int dtype, int64_t rows_each, int64_t most) {
-  const int64_t rows = 256 / norm_lanes(C, dtype);
-  return std::max<int64_t>(1, std::min(most, (N + rows * rows_each - 1) / (rows * rows_each)));
+// Blocks for rows_each rows a lane group, up to what fills the chip `fill` waves deep a CU.
+int64_t norm_blocks(int64_t N, int C, int dtype, int64_t rows_each, int fill) {
+  const NormShape s = norm_shape(C, dtype);
+  return std::max<int64_t>(1, std::min<int64_t>(256 * std::max(1, fill / s.waves), (N + s.rows * rows_each - 1) / (s.rows * rows_each)));
 }
-int64_t norm_bwd_blocks(int64_t N, int C, int dtype) { return norm_blocks(N, C, dtype, 8, 1024); }
+int64_t norm_bwd_blocks(int64_t N, int C, int dtype) { return norm_blocks(N, C, dtype, 8, 16); }
 
 // f(lanes, parts) with both as constants.
 template <typename T, typename F>
-void with_shape(int C, int dtype, F&& f) {
-  const int lanes = norm_lanes(C, dtype), per = lanes * kPer16<T>, parts = (C + per - 1) / per;
+void with_shape(const NormShape& s, F&& f) {
 #define MOGA_SHAPE(L, P) f(std::integral_constant<int, L>{}, std::integral_constant<int, P>{})
-  if (lanes == 16) {
-    if (parts == 1) MOGA_SHAPE(16, 1);
-    else MOGA_SHAPE(16, 2);
-  } else if (lanes == 64) {
-    if (parts == 1) MOGA_SHAPE(64, 1);
-    else if (parts == 2) MOGA_SHAPE(64, 2);
-    else if (parts == 3) MOGA_SHAPE(64, 3);
-    else MOGA_SHAPE(64, 4);
-  } else {
-    if (parts <= 2) MOGA_SHAPE(256, 2);
-    else if (parts == 3) MOGA_SHAPE(256, 3);
-    else if (parts == 4) MOGA_SHAPE(256, 4);
-    else if (parts <= 6) MOGA_SHAPE(256, 6);
-    else if (parts <= 8) MOGA_SHAPE(256, 8);
-    else if constexpr (sizeof(T) == 4) {
-      if (parts <= 12) MOGA_SHAPE(256, 12);
-      else MOGA_SHAPE(256, 16);
-    }
-  }
+#define MOGA_SHAPES(L)                                        \
+  do {                                                        \
+    if (s.parts == 1) MOGA_SHAPE(L, 1);                       \
+    else if (s.parts == 2) MOGA_SHAPE(L, 2);                  \
+    else if constexpr (L == 0 || sizeof(T) == 4) {            \
+      if (s.parts == 3) MOGA_SHAPE(L, 3);                     \
+      else if (s.parts == 4) MOGA_SHAPE(L, 4);                \
+      else if constexpr (L == 0 && sizeof(T) == 4) {          \
+        if (s.parts <= 6) MOGA_SHAPE(L, 6);                   \
+        else MOGA_SHAPE(L, 8);                                \
+      }                                                       \
+    }                                                         \
+  } while (0)
+  if (s.lanes == 16) MOGA_SHAPES(16);
+  else if (s.lanes == 64) MOGA_SHAPES(64);
+  else MOGA_SHAPES(0);
+#undef MOGA_SHAPES
 #undef MOGA_SHAPE
 }
 
@@ -318,20 +374,24 @@ int check_norm(int64_t N, int C, int dtype) {
 template <typename T>
 void launch_fwd(const void* x, const float* w, const float* b, int64_t N, int C, float eps, void* y, float* mean, float* rstd, int dtype,
                 hipStream_t st) {
-  const unsigned blocks = (unsigned)norm_blocks(N, C, dtype, 1, 2048);
-  with_shape<T>(C, dtype, [&](auto lanes, auto parts) {
-    layer_norm_fwd_kernel<T, lanes.value, parts.value><<<blocks, 256, 0, st>>>((const T*)x, w, b, N, C, eps, (T*)y, mean, rstd);
+  const NormShape s = norm_shape(C, dtype);
+  const unsigned blocks = (unsigned)norm_blocks(N, C, dtype, 1, 32);
+  with_shape<T>(s, [&](auto lanes, auto parts) {
+    layer_norm_fwd_kernel<T, lanes.value, parts.value><<<blocks, 64 * s.waves, 0, st>>>((const T*)x, w, b, N, C, eps, (T*)y, mean, rstd);
   });
 }
 
 template <typename T>
 void launch_bwd(const void* dy, const void* x, const float* w, const float* mean, const float* rstd, int64_t N, int C, void* dx, float* part,
                 int dtype, unsigned blocks, hipStream_t st) {
-  with_shape<T>(C, dtype, [&](auto lanes, auto parts) {
+  const NormShape s = norm_shape(C, dtype);
+  with_shape<T>(s, [&](auto lanes, auto parts) {
     if (part)
-      layer_norm_bwd_kernel<T, lanes.value, parts.value, true><<<blocks, 256, 0, st>>>((const T*)dy, (const T*)x, w, mean, rstd, N, C, (T*)dx, part);
+      layer_norm_bwd_kernel<T, lanes.value, parts.value, true><<<blocks, 64 * s.waves, 0, st>>>((const T*)dy, (const T*)x, w, mean, rstd, N, C,
+                                                                                                (T*)dx, part);
     else
-      layer_norm_bwd_kernel<T, lanes.value, parts.value, false><<<blocks, 256, 0, st>>>((const T*)dy, (const T*)x, w, mean, rstd, N, C, (T*)dx, part);
+      layer_norm_bwd_kernel<T, lanes.value, parts.value, false><<<blocks, 64 * s.waves, 0, st>>>((const T*)dy, (const T*)x, w, mean, rstd, N, C,
+                                                                                                 (T*)dx, part);
   });
 }
 
