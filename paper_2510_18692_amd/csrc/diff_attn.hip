@@ -303,15 +303,25 @@ __global__ __launch_bounds__(256) void diff_merge_kernel(DiffFwd a, int pieces, 
       for (int i = 0; i < V; ++i) o[m][i] *= before;
     }
     const int n = min(64, pieces - p0);
-#pragma unroll 4
-    for (int p = 0; p < n; ++p) {
-      const float* part = a.part + ((p0 + p) * rows + row) * 2 * D + lane * V;
+    for (int p = 0; p < n; p += 4) {   // four on their way
+      float v[4][2][V], w[4][2];
 #pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        const float w = __shfl(f[m], p, kWave);
+      for (int u = 0; u < 4; ++u) {
+        const float* part = a.part + ((p0 + min(p + u, n - 1)) * rows + row) * 2 * D + lane * V;
 #pragma unroll
-        for (int i = 0; i < V; ++i) o[m][i] = fmaf(part[m * D + i], w, o[m][i]);
+        for (int m = 0; m < 2; ++m) {
+          w[u][m] = __shfl(f[m], min(p + u, n - 1), kWave);
+#pragma unroll
+          for (int i = 0; i < V; ++i) v[u][m][i] = part[m * D + i];
+        }
       }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (p + u < n)
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int i = 0; i < V; ++i) o[m][i] = fmaf(v[u][m][i], w[u][m], o[m][i]);
     }
   }
 #pragma unroll

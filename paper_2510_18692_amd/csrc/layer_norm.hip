@@ -299,15 +299,20 @@ __global__ __launch_bounds__(256) void layer_norm_dw_kernel(const float* __restr
   __shared__ float acc[16][17];
   const int c = threadIdx.x & 15, k = threadIdx.x >> 4;
   const int64_t col = (int64_t)blockIdx.x * 16 + c;
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
-  if (col < 2 * C) {
-    int b = k;
-    for (; b + 48 < blocks; b += 64)
+  constexpr int U = 16;   // loads on their way
+  float s[U];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) s[u] += part[(size_t)(b + 16 * u) * 2 * C + col];
-    for (; b < blocks; b += 16) s[0] += part[(size_t)b * 2 * C + col];
+  for (int u = 0; u < U; ++u) s[u] = 0.f;
+  if (col < 2 * C) {
+    for (int b = k; b < blocks; b += 16 * U)
+#pragma unroll
+      for (int u = 0; u < U; ++u) s[u] += b + 16 * u < blocks ? part[(size_t)(b + 16 * u) * 2 * C + col] : 0.f;
   }
-  acc[k][c] = (s[0] + s[1]) + (s[2] + s[3]);
+#pragma unroll
+  for (int h = U / 2; h > 0; h /= 2)
+#pragma unroll
+    for (int u = 0; u < h; ++u) s[u] += s[u + h];
+  acc[k][c] = s[0];
   __syncthreads();
   if (k == 0 && col < 2 * C) {
     float t = 0.f;
