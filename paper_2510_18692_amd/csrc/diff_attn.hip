@@ -39,12 +39,13 @@ template <int D, int NC> struct DiffState {
   float m[2][NC], l[2][NC], thresh[2][NC];
 };
 
-// One step: 32 keys.  left: keys of the tile that exist.
-template <typename T, int D, int NC, typename Tiles>
+// One step: 32 keys, of which `left` exist (MASK).
+template <bool MASK, typename T, int D, int NC, typename Tiles>
 __device__ __forceinline__ void diff_fwd_step(const Tiles& tiles, const Frag<T> (&qf)[NC][D / 32], DiffState<D, NC>& st, float c, int left) {
   constexpr int KB = D / 64;   // k blocks of a map
   const int g = (threadIdx.x & 63) >> 4;
-  Frag<T> pf[2][NC];
+  float x[2][NC][8], mx[2][NC];
+  bool up = false;
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
     floatx4_t s[2][NC];
@@ -56,24 +57,25 @@ __device__ __forceinline__ void diff_fwd_step(const Tiles& tiles, const Frag<T> 
 #pragma unroll
         for (int q = 0; q < NC; ++q) s[t][q] = mma(a, qf[q][m * KB + kb], kb == 0 ? floatx4_t{0.f, 0.f, 0.f, 0.f} : s[t][q]);
       }
-    float x[NC][8], mx[NC];
-    bool up = false;
 #pragma unroll
     for (int q = 0; q < NC; ++q) {
-      mx[q] = -INFINITY;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        x[q][i] = fmaf(s[i >> 2][q][i & 3], c, -st.m[m][q]);
-        if (left < 32 && 8 * g + i >= left) x[q][i] = -INFINITY;
-        mx[q] = fmaxf(mx[q], x[q][i]);
+        x[m][q][i] = fmaf(s[i >> 2][q][i & 3], c, -st.m[m][q]);
+        if (MASK && 8 * g + i >= left) x[m][q][i] = -INFINITY;
       }
-      up = up || mx[q] > st.thresh[m][q];
+      const float(&y)[8] = x[m][q];
+      mx[m][q] = fmaxf(max3(max3(max3(y[0], y[1], y[2]), y[3], y[4]), y[5], y[6]), y[7]);
+      up = up || mx[m][q] > st.thresh[m][q];
     }
-    // The maximum is raised when a weight would exceed 2^8 only: rare after the first step.
-    if (__builtin_amdgcn_ballot_w64(up) != 0) {
+  }
+  // The maximum is raised when a weight would exceed 2^8 only: rare after the first step.
+  if (__builtin_amdgcn_ballot_w64(up) != 0) {
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
       for (int q = 0; q < NC; ++q) {
-        float all = fmaxf(mx[q], __shfl_xor(mx[q], 16, kWave));
+        float all = fmaxf(mx[m][q], __shfl_xor(mx[m][q], 16, kWave));
         all = fmaxf(all, __shfl_xor(all, 32, kWave));
         const bool first = st.thresh[m][q] == -INFINITY;
         const float by = first ? (all == -INFINITY ? 0.f : all) : fmaxf(all, 0.f);
@@ -82,20 +84,23 @@ __device__ __forceinline__ void diff_fwd_step(const Tiles& tiles, const Frag<T> 
         st.m[m][q] += by;
         st.l[m][q] *= alpha;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[q][i] -= by;
+        for (int i = 0; i < 8; ++i) x[m][q][i] -= by;
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) st.o[m][dt][q] *= alpha;
       }
-    }
+  }
+  Frag<T> pf[2][NC];
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
 #pragma unroll
     for (int q = 0; q < NC; ++q) {
+      float(&y)[8] = x[m][q];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[q][i] = fast_exp2(x[q][i]);
+      for (int i = 0; i < 8; ++i) y[i] = fast_exp2(y[i]);
       // sums of the weights in 32 bits, before they are rounded: the log-sum-exp is exact enough for the gradient of lambda
-      st.l[m][q] += ((x[q][0] + x[q][1]) + (x[q][2] + x[q][3])) + ((x[q][4] + x[q][5]) + (x[q][6] + x[q][7]));
-      make_frag(pf[m][q], x[q]);
+      st.l[m][q] += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
+      make_frag(pf[m][q], y);
     }
-  }
 #pragma unroll
   for (int dt = 0; dt < D / 16; ++dt) {
     const Frag<T> a = tiles.tr(1, dt);
@@ -145,10 +150,14 @@ __global__ __launch_bounds__(256, 2) void diff_fwd_kernel(DiffFwd a) {
     const float c = a.scale * kLog2e;
     DiffTiles<T, D> tiles;
     tiles.start(lds, (const T*)a.k + (head_k + gs) * D, (const T*)a.v + (head_k + gs) * D, n);
-    const int steps = (n + 31) >> 5;
-    for (int s = 0; s < steps; ++s) {
+    const int full = n >> 5;
+    for (int s = 0; s < full; ++s) {
       tiles.ready(s);
-      if (active) diff_fwd_step<T, D, NC>(tiles, qf, st, c, n - 32 * s);
+      if (active) diff_fwd_step<false, T, D, NC>(tiles, qf, st, c, 32);
+    }
+    if (n & 31) {
+      tiles.ready(full);
+      if (active) diff_fwd_step<true, T, D, NC>(tiles, qf, st, c, n & 31);
     }
     tiles.finish();
   }
@@ -226,7 +235,8 @@ __global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd a, int chunk) 
       tiles.start(lds.tiles[wave], (const T*)a.k + (head_k + gs) * D, (const T*)a.v + (head_k + gs) * D, n, wave);
       for (int t = wave; t < tiles_n; t += 4) {
         tiles.next();
-        diff_fwd_step<T, D, 1>(tiles, qf, st, c, n - 32 * t);
+        if (n - 32 * t >= 32) diff_fwd_step<false, T, D, 1>(tiles, qf, st, c, 32);
+        else diff_fwd_step<true, T, D, 1>(tiles, qf, st, c, n - 32 * t);
         tiles.refill(t + 8);
       }
       tiles.finish();
@@ -423,11 +433,8 @@ __global__ __launch_bounds__(256, 2) void diff_dq_kernel(DiffBwd a) {
     for (int q = 0; q < NC; ++q) rc[q] = a.rows[head_q + min(row0 + 16 * q + r, ge - 1)];
     DiffTiles<T, D> tiles;
     tiles.start(lds, (const T*)a.k + (head_k + gs) * D, (const T*)a.v + (head_k + gs) * D, n);
-    const int steps = (n + 31) >> 5;
-    for (int st = 0; st < steps; ++st) {
-      tiles.ready(st);
-      if (!active) continue;
-      const int left = n - 32 * st;
+    auto step = [&](auto mask, int left) {
+      constexpr bool kMask = mask.value;
       float d1[NC][8], d2[NC][8];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -449,7 +456,7 @@ __global__ __launch_bounds__(256, 2) void diff_dq_kernel(DiffBwd a) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             float p1 = fast_exp2(fmaf(s[0][q][i], c, -rc[q][0])), p2 = fast_exp2(fmaf(s[1][q][i], c, -rc[q][1]));
-            if (left < 32 && 8 * g + 4 * t + i >= left) p1 = p2 = 0.f;
+            if (kMask && 8 * g + 4 * t + i >= left) p1 = p2 = 0.f;
             if constexpr (sizeof(T) == 2) share[q] = fmaf(p2, dp[q][i], share[q]);
             d1[q][4 * t + i] = p1 * (dp[q][i] - rc[q][2]);
             d2[q][4 * t + i] = p2 * (dp[q][i] - rc[q][3]);
@@ -467,6 +474,15 @@ __global__ __launch_bounds__(256, 2) void diff_dq_kernel(DiffBwd a) {
 #pragma unroll
         for (int q = 0; q < NC; ++q) dq[dt][q] = mma(f, dt < DT / 2 ? f1[q] : f2[q], dq[dt][q]);
       }
+    };
+    const int full = n >> 5;
+    for (int s = 0; s < full; ++s) {
+      tiles.ready(s);
+      if (active) step(std::false_type{}, 32);
+    }
+    if (n & 31) {
+      tiles.ready(full);
+      if (active) step(std::true_type{}, n & 31);
     }
     tiles.finish();
   }
