@@ -54,16 +54,16 @@ __device__ __forceinline__ void diff_columns(Frag<T> (&f)[NC][D / 32], const T* 
 // Rows of a group streamed through LDS, 32 of two tensors at a time.  ready(s): tile s may be read, by all waves of the block together, and
 // all of them have left tile s - KEEP.
 // nat(which, t, kb): operand t of the tile's rows (step_row), channels 32 kb ..; tr(which, dt): transposed, channels 16 dt .., all 32 rows.
-template <typename T, int D, bool ROWS = false, int KEEP = 1> struct DiffTiles;
+template <typename T, int D, bool ROWS = false, int KEEP = 1, int SLOTS = 4> struct DiffTiles;
 
 // With ROWS, four constants of every row beside them: rows(v, i), constant v of rows i .. i + 3.
-// bf16: direct-to-LDS loads into a ring of four, as far ahead as the tiles that are kept allow.
-template <bool ROWS, int KEEP> struct DiffTiles<unsigned short, 128, ROWS, KEEP> {
-  static constexpr int kTile = 32 * kHeadDim * 2, kLoads = 2 * kDmaLoads<4, 32> + ROWS, kAhead = 4 - KEEP, kRowSlot = 640;
+// bf16: direct-to-LDS loads into a ring of SLOTS, as far ahead as the tiles that are kept allow.
+template <bool ROWS, int KEEP, int SLOTS> struct DiffTiles<unsigned short, 128, ROWS, KEEP, SLOTS> {
+  static constexpr int kSlots = SLOTS, kTile = 32 * kHeadDim * 2, kLoads = 2 * kDmaLoads<4, 32> + ROWS, kAhead = SLOTS - KEEP, kRowSlot = 640;
   struct Lds {
-    __attribute__((aligned(1024))) unsigned short a[4][32 * kHeadDim];
-    __attribute__((aligned(1024))) unsigned short b[4][32 * kHeadDim];
-    __attribute__((aligned(128))) char rows[ROWS ? 4 : 1][ROWS ? kRowSlot : 16];
+    __attribute__((aligned(1024))) unsigned short a[SLOTS][32 * kHeadDim];
+    __attribute__((aligned(1024))) unsigned short b[SLOTS][32 * kHeadDim];
+    __attribute__((aligned(128))) char rows[ROWS ? SLOTS : 1][ROWS ? kRowSlot : 16];
   };
   PipeDma dma;
   unsigned n_[2], t_[2][2], off, rows_lds, rows_own, rows_at;
@@ -72,10 +72,10 @@ template <bool ROWS, int KEEP> struct DiffTiles<unsigned short, 128, ROWS, KEEP>
   // rows that a lane group wants are one read, and the four lane groups' reads lie in different banks (as 16 bytes a row they do not,
   // and a read takes 50 cycles).
   __device__ __forceinline__ void issue(int s) {
-    pipe_issue<4, 32, false>(dma, 32 * s, (s & 3) * kTile);
+    pipe_issue<4, 32, false>(dma, 32 * s, (s & (SLOTS - 1)) * kTile);
     if constexpr (ROWS) {
       const int lane = threadIdx.x & 63, v = min((int)(threadIdx.x >> 6) + (lane >> 5), 3), row = min(32 * s + (lane & 31), dma.last_row);
-      lds_dma4_soff(rows_base, (unsigned)row * 16u + v * 4u, rows_own + (s & 3) * kRowSlot);
+      lds_dma4_soff(rows_base, (unsigned)row * 16u + v * 4u, rows_own + (s & (SLOTS - 1)) * kRowSlot);
     }
   }
   __device__ __forceinline__ void start(Lds& lds, const unsigned short* a, const unsigned short* b, int n, const floatx4_t* rows = nullptr) {
@@ -105,8 +105,8 @@ template <bool ROWS, int KEEP> struct DiffTiles<unsigned short, 128, ROWS, KEEP>
     at(s);
   }
   __device__ __forceinline__ void at(int s) {   // nat, tr and row read tile s from here on
-    off = (unsigned)(s & 3) * kTile;
-    if constexpr (ROWS) rows_at = rows_lds + (unsigned)(s & 3) * kRowSlot;
+    off = (unsigned)(s & (SLOTS - 1)) * kTile;
+    if constexpr (ROWS) rows_at = rows_lds + (unsigned)(s & (SLOTS - 1)) * kRowSlot;
   }
   __device__ __forceinline__ void finish() { __builtin_amdgcn_s_waitcnt(waitcnt_vm(0)); }   // before the LDS is released
   __device__ __forceinline__ bf16x8_t nat(int which, int t, int kb) const { return read_nat<32>(n_[which] + off, t, kb); }
@@ -167,7 +167,7 @@ struct DiffWaveTiles {
 };
 
 // fp32: through registers, one tile ahead.
-template <int D, bool ROWS> struct DiffTiles<float, D, ROWS, 1> {
+template <int D, bool ROWS> struct DiffTiles<float, D, ROWS, 1, 4> {
   static constexpr int kPitch = D + 4, kEach = 32 * D / 4 / 256;
   struct Lds {
     float a[32][kPitch], b[32][kPitch];

@@ -9,6 +9,7 @@
 #include <cmath>
 
 #include "diff_keys.h"
+#include "diff_steps.h"
 
 namespace moga {
 namespace {
@@ -37,6 +38,17 @@ struct DiffFwd {
 template <int D, int NC> struct DiffState {
   floatx4_t o[2][D / 16][NC];
   float m[2][NC], l[2][NC], thresh[2][NC];
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int q = 0; q < NC; ++q) {
+        m[k][q] = l[k][q] = 0.f;
+        thresh[k][q] = -INFINITY;
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) o[k][dt][q] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+      }
+  }
 };
 
 // One step: 32 keys, of which `left` exist (MASK).
@@ -111,11 +123,32 @@ __device__ __forceinline__ void diff_fwd_step(const Tiles& tiles, const Frag<T> 
   }
 }
 
+// fp32: step by step.
+template <typename T, int D>
+struct DiffPlainSweep : DiffState<D, 1> {
+  typedef DiffTiles<T, D> Tiles;
+  Frag<T> qf[1][D / 32];
+  float c;
+  Tiles tiles;
+  __device__ __forceinline__ void sweep(int n) {
+    const int full = n >> 5;
+    for (int s = 0; s < full; ++s) {
+      if (s > 0) tiles.ready(s);
+      diff_fwd_step<false, T, D, 1>(tiles, qf, *this, c, 32);
+    }
+    if (n & 31) {
+      if (full > 0) tiles.ready(full);
+      diff_fwd_step<true, T, D, 1>(tiles, qf, *this, c, n & 31);
+    }
+  }
+};
+
 // A tile of kRows queries, or (SPLIT) blockIdx.y's share of its keys.
 template <typename T, int D, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void diff_fwd_kernel(DiffFwd a) {
   constexpr int NC = kCols<T>;
-  __shared__ typename DiffTiles<T, D>::Lds lds;
+  typedef std::conditional_t<sizeof(T) == 4, DiffPlainSweep<float, D>, DiffFwdSweep> Sweep;
+  __shared__ typename Sweep::Tiles::Lds lds;
   WorkTile w;
   if (!find_work<false>(a.cu_q, a.tile_start, a.G, a.H, kRows<T>, blockIdx.x, w)) return;
   const int head = w.head, ge = w.ti.row_end;
@@ -132,36 +165,24 @@ __global__ __launch_bounds__(256, 2) void diff_fwd_kernel(DiffFwd a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
   const int row0 = w.ti.tile_row + 16 * NC * wave;
   const int64_t head_q = (int64_t)head * a.Nq, head_k = (int64_t)head * a.Nk;
-  const bool active = row0 < ge;
 
-  DiffState<D, NC> st;
-#pragma unroll
-  for (int m = 0; m < 2; ++m)
-#pragma unroll
-    for (int q = 0; q < NC; ++q) {
-      st.m[m][q] = st.l[m][q] = 0.f;
-      st.thresh[m][q] = -INFINITY;
-#pragma unroll
-      for (int dt = 0; dt < D / 16; ++dt) st.o[m][dt][q] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-    }
+  Sweep st;
+  st.init();
   if (n > 0) {
-    Frag<T> qf[NC][D / 32];
-    diff_columns<T, D, NC>(qf, (const T*)a.q, row0, ge, head_q);
-    const float c = a.scale * kLog2e;
-    DiffTiles<T, D> tiles;
-    tiles.start(lds, (const T*)a.k + (head_k + gs) * D, (const T*)a.v + (head_k + gs) * D, n);
-    const int full = n >> 5;
-    for (int s = 0; s < full; ++s) {
-      tiles.ready(s);
-      if (active) diff_fwd_step<false, T, D, NC>(tiles, qf, st, c, 32);
+    st.tiles.start(lds, (const T*)a.k + (head_k + gs) * D, (const T*)a.v + (head_k + gs) * D, n);
+    if (row0 >= ge) {   // no queries: this wave moves its share of the tiles and keeps the barriers
+      for (int s = 0; s < (n + 31) >> 5; ++s) st.tiles.ready(s);
+      st.tiles.finish();
+      return;
     }
-    if (n & 31) {
-      tiles.ready(full);
-      if (active) diff_fwd_step<true, T, D, NC>(tiles, qf, st, c, n & 31);
-    }
-    tiles.finish();
+    diff_columns<T, D, NC>(st.qf, (const T*)a.q, row0, ge, head_q);
+    if constexpr (sizeof(T) == 2) settle(st.qf);
+    st.c = uniform_float(a.scale * kLog2e);
+    st.tiles.ready(0);
+    st.sweep(n);
+    st.tiles.finish();
   }
-  if (!active) return;
+  if (row0 >= ge) return;
 #pragma unroll
   for (int q = 0; q < NC; ++q) {
     const int row = row0 + 16 * q + r;
@@ -220,13 +241,7 @@ __global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd a, int chunk) 
   const float c = a.scale * kLog2e;
   for (int row0 = q_first; row0 < q_end; row0 += 16) {
     DiffState<D, 1> st;
-#pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      st.m[m][0] = st.l[m][0] = 0.f;
-      st.thresh[m][0] = -INFINITY;
-#pragma unroll
-      for (int dt = 0; dt < D / 16; ++dt) st.o[m][dt][0] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-    }
+    st.init();
     bf16x8_t qf[1][4];
     diff_columns<T, D, 1>(qf, (const T*)a.q, row0, q_end, head_q);
     settle(qf);
@@ -360,7 +375,7 @@ struct DiffBwd {
   const void *d_o, *q, *k, *v;
   const float* lambda;
   const int32_t *cu_q, *cu_k, *tile_start;   // tiles of the side that the blocks own
-  const floatx4_t* rows;                     // [H][Nq]: lse_1, lse_2 in powers of two, delta_1, delta_2
+  const floatx4_t* rows;                     // [H][Nq]: lse_1, lse_2 in powers of two, -delta_1, delta_2 - delta_1
   int64_t Nq, Nk;
   int H, G;
   float scale;
@@ -397,7 +412,7 @@ __global__ __launch_bounds__(256) void diff_rows_kernel(const T* __restrict__ d_
   a = lanes_sum<16>(a);
   b = lanes_sum<16>(b);
   if (t == 0) {
-    out[row] = floatx4_t{lse[row] * kLog2e, lse[rows + row] * kLog2e, a, b};
+    out[row] = floatx4_t{lse[row] * kLog2e, lse[rows + row] * kLog2e, -a, b - a};
     if constexpr (sizeof(T) == 4) share[row] = b;
   }
 }
@@ -417,10 +432,10 @@ __global__ __launch_bounds__(256, 2) void diff_dq_kernel(DiffBwd a) {
   const bool active = row0 < ge;
   const float c = a.scale * kLog2e, lam = a.lambda[head];
   floatx4_t dq[DT][NC];
-  float share[NC];
+  float share[NC], delta2[NC];   // share: sum of P_2 (dP - delta_2); the weights' sum is 1
 #pragma unroll
   for (int q = 0; q < NC; ++q) {
-    share[q] = 0.f;
+    share[q] = delta2[q] = 0.f;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) dq[dt][q] = floatx4_t{0.f, 0.f, 0.f, 0.f};
   }
@@ -428,9 +443,12 @@ __global__ __launch_bounds__(256, 2) void diff_dq_kernel(DiffBwd a) {
     Frag<T> qf[NC][D / 32], df[NC][D / 32];
     diff_columns<T, D, NC>(qf, (const T*)a.q, row0, ge, head_q);
     diff_columns<T, D, NC>(df, (const T*)a.d_o, row0, ge, head_q);
-    floatx4_t rc[NC];
+    floatx4_t rc[NC], by[NC];
 #pragma unroll
-    for (int q = 0; q < NC; ++q) rc[q] = a.rows[head_q + min(row0 + 16 * q + r, ge - 1)];
+    for (int q = 0; q < NC; ++q) {
+      rc[q] = a.rows[head_q + min(row0 + 16 * q + r, ge - 1)];
+      by[q] = floatx4_t{rc[q][2], rc[q][2], rc[q][2], rc[q][2]};   // dP - delta_1: where its sums start
+    }
     DiffTiles<T, D> tiles;
     tiles.start(lds, (const T*)a.k + (head_k + gs) * D, (const T*)a.v + (head_k + gs) * D, n);
     auto step = [&](auto mask, int left) {
@@ -449,7 +467,7 @@ __global__ __launch_bounds__(256, 2) void diff_dq_kernel(DiffBwd a) {
         for (int kb = 0; kb < 2 * KB; ++kb) {
           const Frag<T> f = tiles.nat(1, t, kb);
 #pragma unroll
-          for (int q = 0; q < NC; ++q) dp[q] = mma(f, df[q][kb], kb == 0 ? floatx4_t{0.f, 0.f, 0.f, 0.f} : dp[q]);
+          for (int q = 0; q < NC; ++q) dp[q] = mma(f, df[q][kb], kb == 0 ? by[q] : dp[q]);
         }
 #pragma unroll
         for (int q = 0; q < NC; ++q)
@@ -457,9 +475,9 @@ __global__ __launch_bounds__(256, 2) void diff_dq_kernel(DiffBwd a) {
           for (int i = 0; i < 4; ++i) {
             float p1 = fast_exp2(fmaf(s[0][q][i], c, -rc[q][0])), p2 = fast_exp2(fmaf(s[1][q][i], c, -rc[q][1]));
             if (kMask && 8 * g + 4 * t + i >= left) p1 = p2 = 0.f;
-            if constexpr (sizeof(T) == 2) share[q] = fmaf(p2, dp[q][i], share[q]);
-            d1[q][4 * t + i] = p1 * (dp[q][i] - rc[q][2]);
+            d1[q][4 * t + i] = p1 * dp[q][i];
             d2[q][4 * t + i] = p2 * (dp[q][i] - rc[q][3]);
+            if constexpr (sizeof(T) == 2) share[q] += d2[q][4 * t + i];
           }
       }
       Frag<T> f1[NC], f2[NC];
@@ -485,6 +503,8 @@ __global__ __launch_bounds__(256, 2) void diff_dq_kernel(DiffBwd a) {
       if (active) step(std::true_type{}, n & 31);
     }
     tiles.finish();
+#pragma unroll
+    for (int q = 0; q < NC; ++q) delta2[q] = rc[q][3] - rc[q][2];
   }
   if (!active) return;
 #pragma unroll
@@ -495,7 +515,7 @@ __global__ __launch_bounds__(256, 2) void diff_dq_kernel(DiffBwd a) {
     if (row >= ge) continue;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) store4((T*)a.d_q + (head_q + row) * D, dt, dq[dt][q] * (dt < DT / 2 ? a.scale : -lam * a.scale));
-    if (sizeof(T) == 2 && g == 0) a.share[head_q + row] = sh;
+    if (sizeof(T) == 2 && g == 0) a.share[head_q + row] = sh + delta2[q];
   }
 }
 
@@ -556,8 +576,9 @@ __global__ __launch_bounds__(256, 1) void diff_dkdv_f32_kernel(DiffBwd a) {
             float p1 = fast_exp2(fmaf(s[0][k][i], c, -rc[0][i])), p2 = fast_exp2(fmaf(s[1][k][i], c, -rc[1][i]));
             if (left < 32 && q >= left) p1 = p2 = 0.f;
             pa[k][4 * t + i] = fmaf(-lam, p2, p1);
-            d1[k][4 * t + i] = p1 * (dp[k][i] - rc[2][i]);
-            d2[k][4 * t + i] = p2 * (rc[3][i] - dp[k][i]);
+            const float d = dp[k][i] + rc[2][i];
+            d1[k][4 * t + i] = p1 * d;
+            d2[k][4 * t + i] = p2 * (rc[3][i] - d);
           }
         }
       }
@@ -594,10 +615,10 @@ __global__ __launch_bounds__(256, 1) void diff_dkdv_f32_kernel(DiffBwd a) {
 }
 
 // bf16: diff_keys.h
-__global__ __launch_bounds__(256, 1) void diff_dkdv_kernel(DiffBwd a) {
+__global__ __launch_bounds__(256, 2) void diff_dkdv_kernel(DiffBwd a) {
   constexpr int NC = DiffKeySweep::NC, D = kHeadDim;
   typedef unsigned short T;
-  __shared__ typename DiffKeySweep::Tiles::Lds lds;
+  __shared__ DiffKeySweep::Lds lds;
   WorkTile w;
   if (!find_work<false>(a.cu_k, a.tile_start, a.G, a.H, kKeyRows<T>, blockIdx.x, w)) return;
   const int head = w.head, ge = w.ti.row_end;
@@ -612,16 +633,19 @@ __global__ __launch_bounds__(256, 1) void diff_dkdv_kernel(DiffBwd a) {
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) k.dk[dt][c] = k.dv[dt][c] = floatx4_t{0.f, 0.f, 0.f, 0.f};
   if (n > 0) {
-    k.tiles.start(lds, (const T*)a.q + (head_q + gs) * D, (const T*)a.d_o + (head_q + gs) * D, n, a.rows + head_q + gs);
+    k.tiles.start(lds.tiles, (const T*)a.q + (head_q + gs) * D, (const T*)a.d_o + (head_q + gs) * D, n, a.rows + head_q + gs);
     if (row0 >= ge) {   // no keys: this wave moves its share of the tiles and keeps the barriers
       for (int s = 0; s < (n + 31) >> 5; ++s) k.tiles.ready(s);
       k.tiles.finish();
       return;
     }
     diff_columns<T, D, NC>(k.kf, (const T*)a.k, row0, ge, head_k);
-    diff_columns<T, D, NC>(k.vf, (const T*)a.v, row0, ge, head_k);
+    {
+      bf16x8_t vf[NC][4];
+      diff_columns<T, D, NC>(vf, (const T*)a.v, row0, ge, head_k);
+      k.keep_values(lds, vf);
+    }
     settle(k.kf);
-    settle(k.vf);
     k.c = a.scale * kLog2e;
     k.lam = lam;
     k.tiles.ready(0);

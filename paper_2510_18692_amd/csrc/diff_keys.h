@@ -1,16 +1,4 @@
-// dK and dV of the differential attention, bf16: four waves a block, one per SIMD, 48 keys a wave.
-//
-// A wave keeps 48 keys (K and V fragments) and their dK^T and dV^T, 288 registers, and sweeps the queries of its group, 32 a step, in LDS beside
-// their row constants.  Per 16 queries (t = 0, 1) of a step: scores of both maps and dP, 24 products; from them
-//   a = P_1 - lambda P_2, d_1 = P_1 (dP - delta_1), d_2 = P_2 (delta_2 - dP)        (dK_2 is multiplied by lambda at the end)
-// and with 32 queries of a, d_1 and d_2 the 48 products of dV^T += dO^T a and dK_m^T += Q_m^T d_m.  A fragment read from LDS feeds three products.
-//
-// One wave has to fill both pipes: a product takes 16 cycles and leaves 12 of them to vector instructions, and a step has 96 products and
-// some 1,200 cycles of vector work.  So the work of tile s lies between the products of tile s + 1 and its own last ones, a few vector
-// instructions behind every product:
-//   scores, dP (t = 0) of s + 1   |  a, d_1, d_2 of s, t = 1
-//   dV, dK of s                   |  all of s + 1, t = 0
-//   scores, dP (t = 1) of s + 1   |  P_1, P_2 of s + 1, t = 1
+// dK and dV of the differential attention, bf16: four waves a block, 32 keys a wave, two blocks a CU.
 #pragma once
 
 #include "diff_attn.h"
@@ -18,177 +6,150 @@
 namespace moga {
 
 struct DiffKeySweep {
-  static constexpr int NC = 3, kKeys = 16 * NC, kWin = 2;   // kWin: fragments read ahead
-  typedef DiffTiles<unsigned short, 128, true, 2> Tiles;
-  struct Half { floatx4_t s[2][NC], dp[NC], rc[4]; };       // scores, then weights, and dP of 16 queries; their row constants
-  struct Packed { uintx4_t a[NC], d1[NC], d2[NC]; };        // of 32 queries: t = 0 in words 0, 1
-
-  bf16x8_t kf[NC][4], vf[NC][4], ahead[kWin];
+  static constexpr int NC = 2, kKeys = 16 * NC, kRows = 4 * kKeys;
+  typedef DiffTiles<unsigned short, 128, true, 1, 2> Tiles;
+  struct Lds {
+    Tiles::Lds tiles;
+    __attribute__((aligned(1024))) unsigned short v[kRows * kHeadDim];
+  };
+  bf16x8_t kf[NC][4];
   floatx4_t dk[8][NC], dv[8][NC];
-  Half h0, h1;
   float c, lam;
-  unsigned nat, tr[2];   // the lane's addresses: rows of the newer tile, transposed of the older
+  unsigned v_at;   // the lane's address of the wave's first 16 values' rows
   Tiles tiles;
 
-  __device__ __forceinline__ void load_rows(int t, Half& h) {
+  // The wave's own rows of V: operands of dP, which 32 registers more would be needed for, so they wait in LDS.
+  __device__ __forceinline__ void keep_values(Lds& lds, const bf16x8_t (&vf)[NC][4]) {
+    const int lane = threadIdx.x & 63, row = (threadIdx.x >> 6) * kKeys + (lane & 15);
+    v_at = (unsigned)(uintptr_t)&lds.v[0] + row * 64 + (((lane >> 4) ^ lds_swizzle(row & 31)) << 4);
 #pragma unroll
-    for (int v = 0; v < 4; ++v) h.rc[v] = tiles.rows(v, 8 * ((threadIdx.x & 63) >> 4) + 4 * t);
-  }
-  // queries behind the last: weights of zero
-  __device__ __forceinline__ void mask_rows(int t, int left, Half& h) {
+    for (int k = 0; k < NC; ++k)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (8 * (int)((threadIdx.x & 63) >> 4) + 4 * t + i >= left) h.rc[0][i] = h.rc[1][i] = INFINITY;
+      for (int kb = 0; kb < 4; ++kb) *(bf16x8_t __attribute__((address_space(3)))*)(uintptr_t)value_at(k, kb) = vf[k][kb];
   }
+  // rows 16 .. 31 have the other swizzle bit
+  __device__ __forceinline__ unsigned value_at(int k, int kb) const { return (v_at ^ (k << 4)) + k * 1024 + kb * kQuarterBytes<kRows>; }
 
-  // Vector work on element e = (column, row), in parts of some 12 cycles: a weight,
-  __device__ __forceinline__ void weight(Half& h, int m, int e) {
-    const int k = e >> 2, i = e & 3;
-    h.s[m][k][i] = fast_exp2(fmaf(h.s[m][k][i], c, -h.rc[m][i]));
-  }
-  // PREV: there is an older tile, `cur`; NEXT: a newer one, t = 0 of it to `nxt`; MORE: and one after that, which is waited for.
-  template <bool PREV, bool NEXT, bool MORE>
-  __device__ __forceinline__ void body(Packed& cur, Packed& nxt, int newer, int left) {
-    bf16x8_t fr[32];
-    // All else of an element, in two parts (x: its results, y: those of the row before it).
-    float xa, x1, x2, ya, y1, y2;
-    auto rest_a = [&](Half& h, int e) {
-      const int k = e >> 2, i = e & 3;
-      xa = fmaf(-lam, h.s[1][k][i], h.s[0][k][i]);
-      x1 = h.s[0][k][i] * (h.dp[k][i] - h.rc[2][i]);
-      x2 = h.rc[3][i] - h.dp[k][i];
+  template <bool MASK>
+  __device__ __forceinline__ void step(int left) {
+    constexpr int kKeep = 0x2 | 0x4 | 0x400;
+    const int g = (threadIdx.x & 63) >> 4;
+    const unsigned nat = in_register(tiles.n_[0] + tiles.off);
+    const unsigned tr[2] = {in_register(tiles.t_[0][0] + tiles.off), in_register(tiles.t_[0][1] + tiles.off)};
+    constexpr unsigned kB = Tiles::kSlots * Tiles::kTile;   // from Q to dO
+    floatx4_t s[2][NC], dp[2][NC], lse[2], by;
+    uintx4_t pa[NC], p1[NC], p2[NC];
+    bf16x8_t fd[2][4], fv[NC][4], fq[2][4], ft[16];
+    auto load_d = [&](int kb) {   // dO rows of both operands, V
+#pragma unroll
+      for (int t = 0; t < 2; ++t) fd[t][kb] = read_nat<32>(nat + kB, t, kb);
+#pragma unroll
+      for (int k = 0; k < NC; ++k) fv[k][kb] = lds_read_b128(value_at(k, kb));
     };
-    auto rest_b = [&](Half& h, int t, int e, Packed& p) {
-      const int k = e >> 2, i = e & 3;
-      x2 *= h.s[1][k][i];
-      if (i & 1) {   // to nearest even: operands of the matrix products
-        p.a[k][2 * t + (i >> 1)] = pack_bf16x2(ya, xa);
-        p.d1[k][2 * t + (i >> 1)] = pack_bf16x2(y1, x1);
-        p.d2[k][2 * t + (i >> 1)] = pack_bf16x2(y2, x2);
-      } else {
-        ya = xa;
-        y1 = x1;
-        y2 = x2;
-      }
+    auto load_q = [&](int f) { fq[f >> 2][f & 3] = read_nat<32>(nat, f >> 2, f & 3); };
+    auto load_t = [&](int f) { ft[f] = read_tr<32>(tr, (f & 1 ? 0 : kB), f >> 1); };
+    load_d(0);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {   // dP - delta_1
+      const floatx4_t d = tiles.rows(2, 8 * g + 4 * t);
+#pragma unroll
+      for (int k = 0; k < NC; ++k) dp[t][k] = d;
+    }
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) {
+      __builtin_amdgcn_sched_barrier(kKeep);
+      if (kb < 3) load_d(kb + 1);
+      else load_q(0), load_q(1);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int k = 0; k < NC; ++k) dp[t][k] = mfma16(fd[t][kb], fv[k][kb], dp[t][k]);
+    }
+    auto scores = [&](int t, int kb) {
+#pragma unroll
+      for (int k = 0; k < NC; ++k) s[kb >> 1][k] = mfma16(fq[t][kb], kf[k][kb], (kb & 1) == 0 ? floatx4_t{0.f, 0.f, 0.f, 0.f} : s[kb >> 1][k]);
     };
-    auto load = [&](int f) {   // in the order of use
-      if (!PREV && f >= 8 && f < 24) f += 16;
-      if (f < 8) fr[f] = read_nat<32>(nat + (f >> 2) * 4 * Tiles::kTile, 0, f & 3);
-      else if (f < 24) fr[f] = read_tr<32>(tr, (f & 1 ? 0 : 4 * Tiles::kTile), (f - 8) >> 1);
-      else if (f < 32) fr[f] = NEXT ? read_nat<32>(nat + ((f - 24) >> 2) * 4 * Tiles::kTile, 1, f & 3) : fr[f - 1];
+    auto work = [&](const floatx4_t (&w)[2][NC], int t) {
+      floatx4_t p[2][NC];
+#pragma unroll
+      for (int k = 0; k < NC; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int m = 0; m < 2; ++m) p[m][k][i] = fast_exp2(fmaf(w[m][k][i], c, -lse[m][i]));
+#pragma unroll
+      for (int k = 0; k < NC; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+          float x[2], y[2], z[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            x[e] = fmaf(-lam, p[1][k][i + e], p[0][k][i + e]);
+            y[e] = p[0][k][i + e] * dp[t][k][i + e];
+            z[e] = p[1][k][i + e] * (by[i + e] - dp[t][k][i + e]);
+          }
+          pa[k][2 * t + (i >> 1)] = pack_bf16x2(x[0], x[1]);
+          p1[k][2 * t + (i >> 1)] = pack_bf16x2(y[0], y[1]);
+          p2[k][2 * t + (i >> 1)] = pack_bf16x2(z[0], z[1]);
+        }
     };
-    auto products = [&](int f, Half& h, auto&& vec) {   // the three of a row fragment, and vector work behind each
+    auto constants = [&](int t) {
+#pragma unroll
+      for (int m = 0; m < 2; ++m) lse[m] = tiles.rows(m, 8 * g + 4 * t);
+      by = tiles.rows(3, 8 * g + 4 * t);
+      if (MASK)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (8 * g + 4 * t + i >= left) lse[0][i] = lse[1][i] = INFINITY;
+    };
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) {
+      __builtin_amdgcn_sched_barrier(kKeep);
+      load_q(kb + 2);
+      scores(0, kb);
+    }
+    constants(0);
+    floatx4_t w[2][NC];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int k = 0; k < NC; ++k) w[m][k] = s[m][k];
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) {
+      if (kb < 2) load_q(kb + 6);
+      else load_t(kb - 2);
+      scores(1, kb);
+    }
+    work(w, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    constants(1);
+    work(s, 1);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int f = 0; f < 16; ++f) {
+      __builtin_amdgcn_sched_barrier(kKeep);
+      if (f < 14) load_t(f + 2);
+      const int dt = f >> 1;
 #pragma unroll
       for (int k = 0; k < NC; ++k) {
-        const int kb = f & 3;
-        floatx4_t& d = f & 4 ? h.dp[k] : h.s[kb >> 1][k];
-        d = mfma16(fr[f], f & 4 ? vf[k][kb] : kf[k][kb], kb == 0 || (!(f & 4) && kb == 2) ? floatx4_t{0.f, 0.f, 0.f, 0.f} : d);
-        vec(3 * (f & 7) + k);
-        __builtin_amdgcn_sched_barrier(0);
+        if (f & 1) dk[dt][k] = mfma16(ft[f], __builtin_bit_cast(bf16x8_t, dt < 4 ? p1[k] : p2[k]), dk[dt][k]);
+        else dv[dt][k] = mfma16(ft[f], __builtin_bit_cast(bf16x8_t, pa[k]), dv[dt][k]);
       }
-    };
-    if constexpr (NEXT) {
-#pragma unroll
-      for (int f = 0; f < kWin; ++f) fr[f] = ahead[f];
-#pragma unroll
-      for (int f = 0; f < 8; ++f) {
-        load(f + kWin);
-        if (f == 4) load_rows(0, h0);
-        products(f, h0, [&](int slot) {
-          if constexpr (PREV) {
-            if (slot & 1) rest_b(h1, 1, slot >> 1, cur);
-            else rest_a(h1, slot >> 1);
-          }
-        });
-      }
-      if constexpr (!MORE) mask_rows(0, left, h0);
-    } else {
-      load(8);
-      load(9);
-#pragma unroll
-      for (int e = 0; e < 4 * NC; ++e) {
-        rest_a(h1, e);
-        rest_b(h1, 1, e, cur);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-    auto first_half = [&](int slot) {
-      const int e = slot >> 2;
-      if ((slot & 3) == 0) weight(h0, 0, e);
-      if ((slot & 3) == 1) weight(h0, 1, e);
-      if ((slot & 3) == 2) rest_a(h0, e);
-      if ((slot & 3) == 3) rest_b(h0, 0, e, nxt);
-    };
-    if constexpr (PREV) {
-#pragma unroll
-      for (int f = 8; f < 24; ++f) {
-        if (NEXT || f < 22) load(f + kWin);
-        if (NEXT && f == 20) load_rows(1, h1);
-        const int dt = (f - 8) >> 1;
-#pragma unroll
-        for (int k = 0; k < NC; ++k) {
-          if (f & 1) dk[dt][k] = mfma16(fr[f], __builtin_bit_cast(bf16x8_t, dt < 4 ? cur.d1[k] : cur.d2[k]), dk[dt][k]);
-          else dv[dt][k] = mfma16(fr[f], __builtin_bit_cast(bf16x8_t, cur.a[k]), dv[dt][k]);
-          if constexpr (NEXT) first_half(3 * (f - 8) + k);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int slot = 0; slot < 48; ++slot) {
-        first_half(slot);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      load_rows(1, h1);
-    }
-    if constexpr (NEXT) {
-      if constexpr (!MORE) mask_rows(1, left, h1);
-      const unsigned own = nat;
-#pragma unroll
-      for (int f = 24; f < 32; ++f) {
-        if (f < 30) {
-          load(PREV ? f + kWin : f - 16 + kWin);
-        } else if constexpr (MORE) {
-          if (f == 30) {
-            tiles.ready(newer + 1);
-            nat = in_register(tiles.n_[0] + tiles.off);
-          }
-          ahead[f - 30] = read_nat<32>(nat, 0, f - 30);
-        }
-        products(f, h1, [&](int slot) {
-          if (slot >= 6 && slot < 18) weight(h1, 0, slot - 6);
-          if (slot >= 12) weight(h1, 1, slot - 12);
-        });
-      }
-      // the newer tile is the older one from here on
-      const unsigned by = own - tiles.n_[0];
-#pragma unroll
-      for (int p = 0; p < 2; ++p) tr[p] = in_register(tiles.t_[0][p] + by);
     }
   }
 
+  // Tile 0 is ready.
   __device__ __forceinline__ void sweep(int n) {
-    const int steps = (n + 31) >> 5;
-    Packed p0, p1;
-    nat = tiles.n_[0] + tiles.off;
-#pragma unroll
-    for (int f = 0; f < kWin; ++f) ahead[f] = read_nat<32>(nat, 0, f);
-    if (steps > 1) body<false, true, true>(p1, p0, 0, 32);
-    else body<false, true, false>(p1, p0, 0, n);
-    int s = 0;
-    for (; s + 3 < steps; s += 2) {
-      body<true, true, true>(p0, p1, s + 1, 32);
-      body<true, true, true>(p1, p0, s + 2, 32);
+    const int full = n >> 5;
+    for (int s = 0; s < full; ++s) {
+      if (s > 0) tiles.ready(s);
+      step<false>(32);
     }
-    if (s + 2 < steps) {
-      body<true, true, true>(p0, p1, s + 1, 32);
-      p0 = p1;
+    if (n & 31) {
+      if (full > 0) tiles.ready(full);
+      step<true>(n & 31);
     }
-    if (steps > 1) {
-      body<true, true, false>(p0, p1, steps - 1, n - 32 * (steps - 1));
-      p0 = p1;
-    }
-    body<true, false, false>(p0, p1, 0, 0);
   }
 };
 
