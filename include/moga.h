@@ -630,7 +630,8 @@ int moga_diff_attn_fwd(const void* qh, const void* kh, const void* vh, int dtype
  *   delta_m = rowsum(d_oh * (P_m vh));  dS_1 = P_1 * (dP - delta_1);  dS_2 = -lambda * P_2 * (dP - delta_2)
  *   d_qh_m = scale * dS_m K_m;  d_kh_m = scale * dS_m^T Q_m;  d_vh = (P_1 - lambda P_2)^T d_oh;  d_lambda[h] = -sum P_2 * dP     [H] fp32
  * Keys of a group without queries, and queries of a group without keys, get zero gradients.  Sums in a fixed order: results repeat bit
- * by bit.  Workspace: MOGA_OP_DIFF_ATTN_BWD.
+ * by bit between calls that both have moga_workspace_preferred_bytes, or both less.  Workspace: MOGA_OP_DIFF_ATTN_BWD; with the preferred
+ * bytes the sweeps of calls of few tiles are split over the chip.
  */
 int moga_diff_attn_bwd(const void* d_oh, const void* qh, const void* kh, const void* vh, const float* parts,
                        const float* lse, int dtype, int64_t Nq, int64_t Nk, int H, int D, const float* lambda,

@@ -777,10 +777,12 @@ extern "C" int moga_fused_attn_bwd(const void* d_o, const void* q, const void* k
 }
 
 extern "C" size_t moga_diff_attn_fwd_preferred(int64_t Nq, int64_t Nk, int H, int D, int G, int dtype);
+extern "C" size_t moga_diff_attn_bwd_preferred(int64_t Nq, int64_t Nk, int H, int D, int G, int dtype);
 
 extern "C" size_t moga_workspace_preferred_bytes(int op, int64_t N, int64_t Nk, int H, int D, int M, int d_model, int dtype) {
   const size_t need = moga_workspace_bytes(op, N, H, D, M, d_model, dtype);
   if (op == MOGA_OP_DIFF_ATTN_FWD) return std::max(need, moga_diff_attn_fwd_preferred(N, Nk, H, D, M, dtype));
+  if (op == MOGA_OP_DIFF_ATTN_BWD) return std::max(need, moga_diff_attn_bwd_preferred(N, Nk, H, D, M, dtype));
   if (dtype != MOGA_BF16 || D != 128 || N <= 0 || Nk <= 0 || H < 1 || M < 1) return need;
   const bool fwd = op == MOGA_OP_ATTN_FWD || op == MOGA_OP_VARLEN_ATTN_FWD;
   const bool bwd = op == MOGA_OP_ATTN_BWD || op == MOGA_OP_VARLEN_ATTN_BWD || op == MOGA_OP_ATTN_BWD_JOINT;

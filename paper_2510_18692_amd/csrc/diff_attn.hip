@@ -143,6 +143,15 @@ struct DiffPlainSweep : DiffState<D, 1> {
   }
 };
 
+// (SPLIT kernels) blockIdx.y's share of n rows from `first` on: whole steps of 32, as evenly as they go.
+__device__ __forceinline__ void piece_range(int& first, int& n) {
+  const int64_t steps = (n + 31) >> 5;
+  const int t0 = (int)(steps * blockIdx.y / gridDim.y), t1 = (int)(steps * (blockIdx.y + 1) / gridDim.y);
+  const int end = min(n, 32 * t1);
+  first += 32 * t0;
+  n = end - 32 * t0;
+}
+
 // A tile of kRows queries, or (SPLIT) blockIdx.y's share of its keys.
 template <typename T, int D, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void diff_fwd_kernel(DiffFwd a) {
@@ -153,13 +162,7 @@ __global__ __launch_bounds__(256, 2) void diff_fwd_kernel(DiffFwd a) {
   if (!find_work<false>(a.cu_q, a.tile_start, a.G, a.H, kRows<T>, blockIdx.x, w)) return;
   const int head = w.head, ge = w.ti.row_end;
   int gs = a.cu_k[w.ti.group], n = a.cu_k[w.ti.group + 1] - gs;
-  if constexpr (SPLIT) {   // whole tiles of 32 keys, as evenly as they go
-    const int64_t tiles = (n + 31) >> 5;
-    const int t0 = (int)(tiles * blockIdx.y / gridDim.y), t1 = (int)(tiles * (blockIdx.y + 1) / gridDim.y);
-    const int end = min(n, 32 * t1);
-    gs += 32 * t0;
-    n = end - 32 * t0;
-  }
+  if constexpr (SPLIT) piece_range(gs, n);
   gs = __builtin_amdgcn_readfirstlane(gs);
   n = __builtin_amdgcn_readfirstlane(n);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
@@ -381,6 +384,8 @@ struct DiffBwd {
   float scale;
   void *d_q, *d_k, *d_v;
   float* share;   // [H][Nq]: a row's part of -dlambda
+  // split: pieces of the other side's rows, [piece] of d_q and of share as they are above, and of d_k, then d_v, in fp32
+  float *part_q, *part_share, *part_k;
 };
 
 // The row constants: 16 lanes per row.  delta is made of the unrounded O_m: from rounded ones the gradients of groups of some hundred keys and
@@ -418,14 +423,17 @@ __global__ __launch_bounds__(256) void diff_rows_kernel(const T* __restrict__ d_
 }
 
 // dQ and the rows' shares of dlambda: a wave owns 16 NC queries and sweeps the keys.
-template <typename T, int D>
+template <typename T, int D, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void diff_dq_kernel(DiffBwd a) {
   constexpr int NC = kCols<T>, KB = D / 64, DT = D / 16;
   __shared__ typename DiffTiles<T, D>::Lds lds;
   WorkTile w;
   if (!find_work<false>(a.cu_q, a.tile_start, a.G, a.H, kRows<T>, blockIdx.x, w)) return;
   const int head = w.head, ge = w.ti.row_end;
-  const int gs = __builtin_amdgcn_readfirstlane(a.cu_k[w.ti.group]), n = __builtin_amdgcn_readfirstlane(a.cu_k[w.ti.group + 1]) - gs;
+  int gs = a.cu_k[w.ti.group], n = a.cu_k[w.ti.group + 1] - gs;
+  if constexpr (SPLIT) piece_range(gs, n);
+  gs = __builtin_amdgcn_readfirstlane(gs);
+  n = __builtin_amdgcn_readfirstlane(n);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
   const int row0 = w.ti.tile_row + 16 * NC * wave;
   const int64_t head_q = (int64_t)head * a.Nq, head_k = (int64_t)head * a.Nk;
@@ -513,21 +521,33 @@ __global__ __launch_bounds__(256, 2) void diff_dq_kernel(DiffBwd a) {
     float sh = share[q] + __shfl_xor(share[q], 16, kWave);
     sh += __shfl_xor(sh, 32, kWave);
     if (row >= ge) continue;
+    auto store = [&](auto* out) {
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) store4((T*)a.d_q + (head_q + row) * D, dt, dq[dt][q] * (dt < DT / 2 ? a.scale : -lam * a.scale));
-    if (sizeof(T) == 2 && g == 0) a.share[head_q + row] = sh + delta2[q];
+      for (int dt = 0; dt < DT; ++dt) store4(out, dt, dq[dt][q] * (dt < DT / 2 ? a.scale : -lam * a.scale));
+    };
+    if constexpr (SPLIT) {
+      const int64_t at = (int64_t)blockIdx.y * a.H * a.Nq + head_q + row;
+      store(a.part_q + at * D);
+      if (sizeof(T) == 2 && g == 0) a.part_share[at] = sh;
+    } else {
+      store((T*)a.d_q + (head_q + row) * D);
+      if (sizeof(T) == 2 && g == 0) a.share[head_q + row] = sh + delta2[q];
+    }
   }
 }
 
 // fp32 dK and dV: a wave owns 16 keys and sweeps the queries, with their row constants beside them in LDS.
-template <typename T, int D>
+template <typename T, int D, bool SPLIT>
 __global__ __launch_bounds__(256, 1) void diff_dkdv_f32_kernel(DiffBwd a) {
   constexpr int NC = 1, KB = D / 64, DT = D / 16;
   __shared__ typename DiffTiles<T, D, true>::Lds lds;
   WorkTile w;
   if (!find_work<false>(a.cu_k, a.tile_start, a.G, a.H, kKeyRows<T>, blockIdx.x, w)) return;
   const int head = w.head, ge = w.ti.row_end;
-  const int gs = __builtin_amdgcn_readfirstlane(a.cu_q[w.ti.group]), n = __builtin_amdgcn_readfirstlane(a.cu_q[w.ti.group + 1]) - gs;
+  int gs = a.cu_q[w.ti.group], n = a.cu_q[w.ti.group + 1] - gs;
+  if constexpr (SPLIT) piece_range(gs, n);
+  gs = __builtin_amdgcn_readfirstlane(gs);
+  n = __builtin_amdgcn_readfirstlane(n);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
   const int row0 = w.ti.tile_row + 16 * NC * wave;
   const int64_t head_q = (int64_t)head * a.Nq, head_k = (int64_t)head * a.Nk;
@@ -606,15 +626,24 @@ __global__ __launch_bounds__(256, 1) void diff_dkdv_f32_kernel(DiffBwd a) {
   for (int k = 0; k < NC; ++k) {
     const int row = row0 + 16 * k + r;
     if (row >= ge) continue;
+    auto store = [&](auto* d_k, auto* d_v) {
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      store4((T*)a.d_k + (head_k + row) * D, dt, dk[dt][k] * (dt < DT / 2 ? a.scale : lam * a.scale));
-      store4((T*)a.d_v + (head_k + row) * D, dt, dv[dt][k]);
+      for (int dt = 0; dt < DT; ++dt) {
+        store4(d_k, dt, dk[dt][k] * (dt < DT / 2 ? a.scale : lam * a.scale));
+        store4(d_v, dt, dv[dt][k]);
+      }
+    };
+    if constexpr (SPLIT) {
+      float* part = a.part_k + ((int64_t)blockIdx.y * 2 * a.H * a.Nk + head_k + row) * D;
+      store(part, part + (int64_t)a.H * a.Nk * D);
+    } else {
+      store((T*)a.d_k + (head_k + row) * D, (T*)a.d_v + (head_k + row) * D);
     }
   }
 }
 
 // bf16: diff_keys.h
+template <bool SPLIT>
 __global__ __launch_bounds__(256, 2) void diff_dkdv_kernel(DiffBwd a) {
   constexpr int NC = DiffKeySweep::NC, D = kHeadDim;
   typedef unsigned short T;
@@ -622,7 +651,10 @@ __global__ __launch_bounds__(256, 2) void diff_dkdv_kernel(DiffBwd a) {
   WorkTile w;
   if (!find_work<false>(a.cu_k, a.tile_start, a.G, a.H, kKeyRows<T>, blockIdx.x, w)) return;
   const int head = w.head, ge = w.ti.row_end;
-  const int gs = __builtin_amdgcn_readfirstlane(a.cu_q[w.ti.group]), n = __builtin_amdgcn_readfirstlane(a.cu_q[w.ti.group + 1]) - gs;
+  int gs = a.cu_q[w.ti.group], n = a.cu_q[w.ti.group + 1] - gs;
+  if constexpr (SPLIT) piece_range(gs, n);
+  gs = __builtin_amdgcn_readfirstlane(gs);
+  n = __builtin_amdgcn_readfirstlane(n);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int row0 = w.ti.tile_row + DiffKeySweep::kKeys * wave;
   const int64_t head_q = (int64_t)head * a.Nq, head_k = (int64_t)head * a.Nk;
@@ -656,12 +688,49 @@ __global__ __launch_bounds__(256, 2) void diff_dkdv_kernel(DiffBwd a) {
   for (int c = 0; c < NC; ++c) {
     const int row = row0 + 16 * c + (lane & 15);
     if (row >= ge) continue;
+    auto store = [&](auto* d_k, auto* d_v) {
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt) {
-      store4((T*)a.d_k + (head_k + row) * D, dt, k.dk[dt][c] * (dt < 4 ? a.scale : lam * a.scale));
-      store4((T*)a.d_v + (head_k + row) * D, dt, k.dv[dt][c]);
+      for (int dt = 0; dt < 8; ++dt) {
+        store4(d_k, dt, k.dk[dt][c] * (dt < 4 ? a.scale : lam * a.scale));
+        store4(d_v, dt, k.dv[dt][c]);
+      }
+    };
+    if constexpr (SPLIT) {
+      float* part = a.part_k + ((int64_t)blockIdx.y * 2 * a.H * a.Nk + head_k + row) * D;
+      store(part, part + (int64_t)a.H * a.Nk * D);
+    } else {
+      store((T*)a.d_k + (head_k + row) * D, (T*)a.d_v + (head_k + row) * D);
     }
   }
+}
+
+// Sums of the pieces, four channels a thread: d_q and share (pq != 1), d_k and d_v (pk != 1; 0: zeros).  Rows behind the last group stay.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void diff_sum_kernel(DiffBwd a, int pq, int pk) {
+  constexpr int kEach = D / 4;
+  const int64_t q_rows = pq == 1 ? 0 : a.H * a.Nq, k_rows = pk == 1 ? 0 : a.H * a.Nk;
+  const int col = threadIdx.x % kEach * 4;
+  int64_t row = (int64_t)blockIdx.x * (256 / kEach) + threadIdx.x / kEach;
+  auto sum = [&](const float* part, int pieces, int64_t stride, T* out) {
+    floatx4_t v = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < pieces; ++p) v += *(const floatx4_t*)(part + p * stride * D + col);
+    if constexpr (sizeof(T) == 4) *(floatx4_t*)(out + col) = v;
+    else *(uintx2_t*)(out + col) = pack4(v, 1.f);
+  };
+  if (row < q_rows) {
+    if (row % a.Nq >= a.cu_q[a.G]) return;
+    sum(a.part_q + row * D, pq, q_rows, (T*)a.d_q + row * D);
+    if (sizeof(T) == 2 && col == 0) {
+      float s = a.rows[row][3] - a.rows[row][2];   // delta_2
+      for (int p = 0; p < pq; ++p) s += a.part_share[p * q_rows + row];
+      a.share[row] = s;
+    }
+    return;
+  }
+  row -= q_rows;
+  if (row >= 2 * k_rows || row % a.Nk >= a.cu_k[a.G]) return;
+  T* out = (T*)(row < k_rows ? a.d_k : a.d_v) + (row < k_rows ? row : row - k_rows) * D;
+  sum(a.part_k + row * D, pk, 2 * k_rows, out);
 }
 
 // A block per head, in a fixed order.
@@ -700,6 +769,14 @@ int key_rows_of(int dtype) { return dtype == MOGA_F32 ? kKeyRows<float> : kKeyRo
 int64_t diff_blocks(int64_t N, int H, int G, int rows) { return (max_tiles(N, G, rows) * H + 7) / 8 * 8; }
 size_t tile_bytes(int G) { return G > MOGA_MAX_GROUPS ? round_up(((size_t)G + 1) * sizeof(int32_t), 256) : 0; }
 
+// Pieces of the rows that a tile sweeps: where tiles of `rows` rows leave CUs idle, as many as fill two blocks a CU, none under 256 rows of a mean
+// group (fp32, whose steps take ten times as long: 128).  Backward, whole and in pieces: bf16 1,000 x 3 heads 86 and 51 us, 4,096 x 3 286
+// and 149, fp32 1,000 x 2 x 64 172 and 66; with pieces of 128 rows bf16 4,096 x 3, 8 groups 70 instead of 61.
+int diff_pieces(int64_t N, int64_t other, int H, int G, int rows, int dtype) {
+  const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(max_tiles(N, G, rows), N)) * H;
+  return (int)std::max<int64_t>(1, std::min({(int64_t)16, 2 * kCus / blocks, other / G / (dtype == MOGA_F32 ? 128 : 256)}));
+}
+
 size_t diff_piece_bytes(int64_t Nq, int H, int D) { return (size_t)Nq * H * 2 * (D + 2) * sizeof(float); }
 
 // How a forward call shares out its keys.  chunk > 0: diff_few_kernel, pieces of `chunk` keys, at most `pieces` of a group; else pieces of every
@@ -713,9 +790,19 @@ DiffSplit diff_split(int64_t Nq, int64_t Nk, int H, int D, int G, int dtype) {
     const int64_t chunk = round_up((size_t)std::max({(int64_t)256, Nk * H / (2 * kCus), (Nk + most - 1) / most}), 128);
     return {(int)((Nk + chunk - 1) / chunk), (int)chunk};
   }
-  // Else where the tiles leave CUs idle, as many pieces as fill two blocks a CU, none under 256 keys of a mean group.
-  const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(max_tiles(Nq, G, rows_of(dtype)), Nq)) * H;
-  return {(int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, 2 * kCus / blocks), Nk / G / 256)), 0};
+  return {diff_pieces(Nq, Nk, H, G, rows_of(dtype), dtype), 0};
+}
+
+struct DiffBwdSplit {
+  int q, k;
+  size_t q_bytes, share_bytes, k_bytes;
+  size_t bytes() const { return q_bytes + share_bytes + k_bytes; }
+};
+DiffBwdSplit diff_bwd_split(int64_t Nq, int64_t Nk, int H, int D, int G, int dtype) {
+  DiffBwdSplit s = {diff_pieces(Nq, Nk, H, G, rows_of(dtype), dtype), diff_pieces(Nk, Nq, H, G, key_rows_of(dtype), dtype), 0, 0, 0};
+  if (s.q > 1) s.q_bytes = (size_t)s.q * H * Nq * D * sizeof(float), s.share_bytes = round_up((size_t)s.q * H * Nq * sizeof(float), 256);
+  if (s.k > 1) s.k_bytes = (size_t)s.k * 2 * H * Nk * D * sizeof(float);
+  return s;
 }
 }  // namespace
 }  // namespace moga
@@ -730,7 +817,11 @@ extern "C" size_t moga_diff_attn_fwd_preferred(int64_t Nq, int64_t Nk, int H, in
   return tile_bytes(G) + (s.pieces > 1 || s.chunk ? s.pieces * diff_piece_bytes(Nq, H, D) : 0);
 }
 extern "C" size_t moga_diff_attn_bwd_ws_bytes(int64_t Nq, int H, int G) {
-  return Nq > 0 ? tile_bytes(G) * 2 + (size_t)Nq * H * (sizeof(floatx4_t) + sizeof(float)) : 0;
+  return Nq > 0 ? tile_bytes(G) * 2 + round_up((size_t)Nq * H * (sizeof(floatx4_t) + sizeof(float)), 256) : 0;
+}
+extern "C" size_t moga_diff_attn_bwd_preferred(int64_t Nq, int64_t Nk, int H, int D, int G, int dtype) {
+  if (Nq <= 0 || check_diff(Nq, Nk, H, D, G, 1.f, dtype) != MOGA_OK) return 0;
+  return moga_diff_attn_bwd_ws_bytes(Nq, H, G) + diff_bwd_split(Nq, Nk, H, D, G, dtype).bytes();
 }
 
 extern "C" int moga_diff_attn_fwd(const void* qh, const void* kh, const void* vh, int dtype, int64_t Nq, int64_t Nk, int H, int D,
@@ -795,7 +886,13 @@ extern "C" int moga_diff_attn_bwd(const void* d_oh, const void* qh, const void* 
   const size_t need = moga_diff_attn_bwd_ws_bytes(Nq, H, G);
   if (need && (!ws || ws_bytes < need)) return MOGA_ERR_WORKSPACE;
   const int64_t q_blocks = diff_blocks(Nq, H, G, rows_of(dtype)), k_blocks = diff_blocks(Nk, H, G, key_rows_of(dtype)), rows = Nq * H;
-  if (!grid_fits(q_blocks, 256) || !grid_fits(k_blocks, 256) || !grid_fits((rows + 15) / 16, 256)) return MOGA_ERR_UNSUPPORTED;
+  DiffBwdSplit split = {1, 1, 0, 0, 0};
+  if (Nq > 0 && ws_bytes >= moga_diff_attn_bwd_preferred(Nq, Nk, H, D, G, dtype)) split = diff_bwd_split(Nq, Nk, H, D, G, dtype);
+  if (Nq == 0) split.k = 0;   // keys without queries: zeros
+  const int64_t sum_blocks = ((split.q != 1 ? rows : 0) + (split.k != 1 ? 2 * Nk * H : 0) + 1024 / D - 1) / (1024 / D);
+  if (!grid_fits(q_blocks * split.q, 256) || !grid_fits(k_blocks * std::max(1, split.k), 256) || !grid_fits((rows + 15) / 16, 256) ||
+      !grid_fits(sum_blocks, 256))
+    return MOGA_ERR_UNSUPPORTED;
   hipStream_t st = (hipStream_t)stream;
   int32_t *tq = nullptr, *tk = nullptr;
   if (G > MOGA_MAX_GROUPS && need) {
@@ -806,26 +903,38 @@ extern "C" int moga_diff_attn_bwd(const void* d_oh, const void* qh, const void* 
   }
   floatx4_t* rc = (floatx4_t*)((char*)ws + 2 * tile_bytes(G));
   float* share = (float*)(rc + rows);
-  DiffBwd a = {d_oh, qh, kh, vh, lambda, cu_seqlens_q, cu_seqlens_k, tq, rc, Nq, Nk, H, G, softmax_scale, d_qh, d_kh, d_vh, share};
+  DiffBwd a = {d_oh, qh, kh, vh, lambda, cu_seqlens_q, cu_seqlens_k, tq, rc, Nq, Nk, H, G, softmax_scale, d_qh, d_kh, d_vh, share, nullptr, nullptr, nullptr};
+  if (split.q > 1 || split.k > 1) {
+    char* room = (char*)ws + need;
+    a.part_q = (float*)room;
+    a.part_share = (float*)(room + split.q_bytes);
+    a.part_k = (float*)(room + split.q_bytes + split.share_bytes);
+  }
   DiffBwd b = a;
   b.tile_start = tk;
 #define MOGA_DIFF_BWD(T, D)                                                                                                            \
   do {                                                                                                                                 \
     diff_rows_kernel<T, D><<<(unsigned)((rows + 15) / 16), 256, 0, st>>>((const T*)d_oh, parts, lse, rows, rc, share);                  \
-    diff_dq_kernel<T, D><<<(unsigned)q_blocks, 256, 0, st>>>(a);                                                                       \
-    if (Nk > 0) {                                                                                                                      \
-      if constexpr (sizeof(T) == 4) diff_dkdv_f32_kernel<T, D><<<(unsigned)k_blocks, 256, 0, st>>>(b);                                  \
-      else diff_dkdv_kernel<<<(unsigned)k_blocks, 256, 0, st>>>(b);                                                                    \
+    if (split.q > 1) diff_dq_kernel<T, D, true><<<dim3((unsigned)q_blocks, split.q), 256, 0, st>>>(a);                                   \
+    else diff_dq_kernel<T, D, false><<<(unsigned)q_blocks, 256, 0, st>>>(a);                                                           \
+    const dim3 grid((unsigned)k_blocks, std::max(1, split.k));                                                                         \
+    if constexpr (sizeof(T) == 4) {                                                                                                    \
+      if (Nk > 0 && split.k > 1) diff_dkdv_f32_kernel<T, D, true><<<grid, 256, 0, st>>>(b);                                             \
+      else if (Nk > 0) diff_dkdv_f32_kernel<T, D, false><<<grid, 256, 0, st>>>(b);                                                      \
+    } else {                                                                                                                           \
+      if (Nk > 0 && split.k > 1) diff_dkdv_kernel<true><<<grid, 256, 0, st>>>(b);                                                       \
+      else if (Nk > 0) diff_dkdv_kernel<false><<<grid, 256, 0, st>>>(b);                                                                \
     }                                                                                                                                  \
   } while (0)
   if (Nq > 0) {
     if (dtype == MOGA_BF16) MOGA_DIFF_BWD(unsigned short, 128);
     else if (D == 64) MOGA_DIFF_BWD(float, 64);
     else MOGA_DIFF_BWD(float, 128);
-  } else if (Nk > 0) {   // keys without queries
-    const int64_t floats = Nk * H * D * (int64_t)elem_size(dtype) / 4;
-    launch_fill_zero((float*)d_kh, floats, st);
-    launch_fill_zero((float*)d_vh, floats, st);
+  }
+  if (sum_blocks > 0) {
+    if (dtype == MOGA_BF16) diff_sum_kernel<unsigned short, 128><<<(unsigned)sum_blocks, 256, 0, st>>>(a, split.q, split.k);
+    else if (D == 64) diff_sum_kernel<float, 64><<<(unsigned)sum_blocks, 256, 0, st>>>(a, split.q, split.k);
+    else diff_sum_kernel<float, 128><<<(unsigned)sum_blocks, 256, 0, st>>>(a, split.q, split.k);
   }
 #undef MOGA_DIFF_BWD
   diff_dlambda_kernel<<<H, 1024, 0, st>>>(share, cu_seqlens_q, G, Nq, d_lambda);

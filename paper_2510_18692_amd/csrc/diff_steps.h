@@ -139,30 +139,26 @@ struct DiffFwdSweep {
     for (int p = 0; p < 2; ++p) tr[p] = in_register(tiles.t_[0][p] + (unsigned)(s & 3) * Tiles::kTile);
   }
 
-  // Tile 0 is ready.
+  // Tile 0 is ready.  The last tile's scores are masked whether it is whole or not.
   __device__ __forceinline__ void sweep(int n) {
-    const int steps = (n + 31) >> 5, tail = n & 31;
+    const int steps = (n + 31) >> 5, left = n - 32 * (steps - 1);
     auto nothing = []() {};
     Half x, y;
     nat = in_register(tiles.n_[0] + tiles.off);
-    {
 #pragma unroll
-      for (int f = 0; f < 4; ++f) {
-        const bf16x8_t a = row_frag(0, f);
+    for (int f = 0; f < 4; ++f) {
+      __builtin_amdgcn_sched_barrier(0);
+      const bf16x8_t a = row_frag(0, f);
 #pragma unroll
-        for (int q = 0; q < NC; ++q) x[f >> 1][q] = mfma16(a, qf[q][f & 1], (f & 1) == 0 ? floatx4_t{0.f, 0.f, 0.f, 0.f} : x[f >> 1][q]);
-      }
-#pragma unroll
-      for (int q = 0; q < NC; ++q)
-        if (n < 32) exponents<true>(0, x, q, n);
-        else exponents<false>(0, x, q, 32);
-      raise(0, x);
-#pragma unroll
-      for (int f = 0; f < kAheadFrags; ++f) ahead[f] = row_frag(1, f);
+      for (int q = 0; q < NC; ++q) x[f >> 1][q] = mfma16(a, qf[q][f & 1], (f & 1) == 0 ? floatx4_t{0.f, 0.f, 0.f, 0.f} : x[f >> 1][q]);
     }
+#pragma unroll
+    for (int q = 0; q < NC; ++q) exponents<true>(0, x, q, min(n, 32));
+    raise(0, x);
+#pragma unroll
+    for (int f = 0; f < kAheadFrags; ++f) ahead[f] = row_frag(1, f);
     int s = 0;
-    const int plain = steps - 1 - (tail != 0);   // tiles whose successor is there and whole
-    for (; s < plain; ++s) {
+    for (; s < steps - 2; ++s) {   // tiles whose successor is not the last
       value_tile(s);
       half<true, false, true>(1, x, y, 32, [&]() { next_tile(s + 1); });
       half<true, false, true>(0, y, x, 32, nothing);
@@ -170,12 +166,11 @@ struct DiffFwdSweep {
     if (s < steps - 1) {
       value_tile(s);
       half<true, false, true>(1, x, y, 32, [&]() { next_tile(s + 1); });
-      half<true, true, true>(0, y, x, tail, nothing);
+      half<true, true, true>(0, y, x, left, nothing);
       ++s;
     }
     value_tile(s);
-    if (tail) half<true, true, false>(1, x, y, tail, nothing);
-    else half<true, false, false>(1, x, y, 32, nothing);
+    half<true, true, false>(1, x, y, left, nothing);
     half<false, false, false>(1, y, x, 32, nothing);
   }
 };

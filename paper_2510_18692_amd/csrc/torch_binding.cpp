@@ -771,10 +771,10 @@ std::tuple<Tensor, Tensor, Tensor, Tensor> diff_attn_bwd(const Tensor& d_oh, con
   need_like(lse, qh, {2, s.H, s.Nq}, at::kFloat, "lse");
   Tensor d_qh = call.make(qh.sizes(), qh), d_kh = call.make(kh.sizes(), kh), d_vh = call.make(vh.sizes(), vh);
   Tensor d_lam = call.make({s.H}, qh, at::kFloat);
-  Tensor ws = call.workspace(moga_workspace_bytes(MOGA_OP_DIFF_ATTN_BWD, s.Nq, to_int(s.H), to_int(s.D), to_int(s.G), 0, dt(qh)), qh);
+  OptTensor ws = call.attn_workspace(MOGA_OP_DIFF_ATTN_BWD, s.Nq, s.Nk, s.H, s.D, s.G, qh);
   check("moga_diff_attn_bwd", moga_diff_attn_bwd(ptr(d_oh), ptr(qh), ptr(kh), ptr(vh), as<float>(parts), as<float>(lse), dt(qh), s.Nq, s.Nk,
                                                  to_int(s.H), to_int(s.D), as<float>(lam), as<int32_t>(cu_q), as<int32_t>(cu_k), to_int(s.G),
-                                                 (float)scale, ptr(d_qh), ptr(d_kh), ptr(d_vh), as<float>(d_lam), ptr(ws), (size_t)ws.numel(),
+                                                 (float)scale, ptr(d_qh), ptr(d_kh), ptr(d_vh), as<float>(d_lam), ptr(ws), bytes_of(ws),
                                                  call.stream()));
   return {d_qh, d_kh, d_vh, d_lam};
 }

@@ -149,6 +149,35 @@ def test_split_keys(sq, sk, H, D, dtype):
         ref.within(lse.nan_to_num(neginf=0.0), want["lse"][0].nan_to_num(neginf=0.0), want["lse"][1], "lse")
 
 
+@pytest.mark.parametrize("H,D,dtype", [(2, 128, torch.bfloat16), (2, 64, torch.float32), (1, 128, torch.float32)])
+@pytest.mark.parametrize("sq,sk", [([700], [900]), ([1500, 3], [2, 1100]), ([40, 0, 1300], [2000, 300, 0]), ([1], [3000]), ([2600], [1])])
+def test_split_backward(sq, sk, H, D, dtype):
+    """Few tiles: with room either sweep is shared out over the chip, without it neither is; bits repeat with as much room."""
+    cu_q, cu_k = _cu(sq), _cu(sk)
+    q, k, v, do, lam = _inputs(H, D, dtype, cu_q, cu_k, 25)
+    code, Nq, Nk, G = {torch.float32: 0, torch.bfloat16: 1}[dtype], cu_q[-1], cu_k[-1], len(sq)
+    need = mg.workspace_bytes(mg.OP_DIFF_ATTN_BWD, Nq, H, D, G, 0, code)
+    room = mg.load().moga_workspace_preferred_bytes(mg.OP_DIFF_ATTN_BWD, Nq, Nk, H, D, G, 0, code)
+    assert room > need
+    want = ref.diff_all(q.double(), k.double(), v.double(), lam.double(), do.double(), cu_q, cu_k, 0.1, ref.HALF_STEP[dtype])
+    dcq, dck = _dev(cu_q), _dev(cu_k)
+    _, parts, lse = mg.moga_diff_attn_fwd(q, k, v, lam, dcq, dck, 0.1)
+    p = lambda x: ctypes.c_void_p(x.data_ptr())
+    for size in (need, room):
+        seen = []
+        for _ in range(2):
+            out = {"dq": torch.empty_like(q), "dk": torch.empty_like(k), "dv": torch.empty_like(v), "dlam": torch.empty_like(lam)}
+            ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+            st = mg.load().moga_diff_attn_bwd(p(do), p(q), p(k), p(v), p(parts), p(lse), code, Nq, Nk, H, D, p(lam), p(dcq), p(dck), G, 0.1,
+                                              *(p(out[n]) for n in ("dq", "dk", "dv", "dlam")), p(ws), size,
+                                              ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+            assert st == 0
+            for name, t in out.items():
+                ref.within(t, *want[name], f"{name}, {size} bytes")
+            seen.append(out)
+        assert all(torch.equal(seen[0][n], seen[1][n]) for n in seen[0])
+
+
 @pytest.mark.parametrize("D,dtype", [(128, torch.bfloat16), (64, torch.float32)])
 def test_other_groups_values_never_leak(D, dtype):
     """Infinities and NaN in one group's rows: the other groups keep their bits."""
@@ -201,6 +230,18 @@ def test_repeated_calls_give_the_same_bits():
     for _ in range(3):
         b = _run(*t, cu, cu, 0.125)
         assert all(torch.equal(a[n], b[n]) for n in a)
+
+
+def test_keys_without_queries_leave_the_rows_behind_them():
+    k = torch.randn((2, 9, 128), device="cuda").bfloat16()
+    dk, dv, dlam = torch.full_like(k, 5), torch.full_like(k, 5), torch.full((2,), 5.0, device="cuda")
+    lam, cq, ck = torch.ones(2, device="cuda"), _dev([0, 0]), _dev([0, 6])
+    p = lambda x: ctypes.c_void_p(x.data_ptr())
+    st = mg.load().moga_diff_attn_bwd(None, None, p(k), p(k), None, None, 1, 0, 9, 2, 128, p(lam), p(cq), p(ck), 1, 0.1, None, p(dk), p(dv), p(dlam), None,
+                                      0, ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+    assert st == 0 and (dlam == 0).all()
+    for t in (dk, dv):
+        assert (t[:, :6] == 0).all() and (t[:, 6:] == 5).all()
 
 
 def test_nothing_on_a_side():
