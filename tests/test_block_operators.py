@@ -197,3 +197,13 @@ def test_pieces_need_room_only_where_tiles_are_few():
     assert pref(99840, 99840, 40, 16) == 0
     assert pref(4, 4 * 100, 12, 4) == 0           # too few keys to share out
     assert pref(0, 100000, 12, 4) == 0
+
+
+def test_pieces_of_many_heads_and_long_lists_fit_their_types():
+    """Room grows with what is split, never past a gigabyte, and no product of sizes wraps."""
+    for Nq, Nk, H, G in ((1, (1 << 24) - 1, 60000, 1), (16, (1 << 24) - 1, 4000, 1), (1 << 20, 1 << 23, 64, 1 << 16), ((1 << 24) - 1, 4096, 1, 1),
+                         (3000, (1 << 24) - 1, 1, 300)):
+        for op in (mg.OP_DIFF_ATTN_FWD, mg.OP_DIFF_ATTN_BWD):
+            need = mg.workspace_bytes(op, Nq, H, 128, G, 0, 1)
+            room = mg.load().moga_workspace_preferred_bytes(op, Nq, Nk, H, 128, G, 0, 1)
+            assert need <= room <= need + (1 << 30), (Nq, Nk, H, G, op)

@@ -223,6 +223,22 @@ def test_rows_behind_the_last_group_stay(D, dtype):
     ref.within(dlam, *want["dlam"], "dlam")
 
 
+def test_gradient_of_lambda_over_many_rows():
+    """60,000 rows whose parts have either sign: errors of single rows average out, a common one adds up.  An eighth of u a row, common to all, is
+    60,000 u / 8 of a sum of some 0.4 sqrt(60,000): 4.6e-6."""
+    H, D, n, G = 3, 128, 5000, 12
+    cu = _cu([n] * G)
+    q, k, v, do, lam = _inputs(H, D, torch.bfloat16, cu, cu, 77)
+    got = _run(q, k, v, do, lam, cu, cu, 0.125)["dlam"]
+    want = torch.zeros(H, dtype=torch.float64, device="cuda")
+    for g in range(G):
+        r = slice(cu[g], cu[g + 1])
+        for h in range(H):
+            p = torch.softmax(0.125 * q[h, r, 64:].double() @ k[h, r, 64:].double().t(), 1)
+            want[h] -= (p * (do[h, r].double() @ v[h, r].double().t())).sum()
+    ref.near(got, want, 4.6e-6, "dlam")
+
+
 def test_repeated_calls_give_the_same_bits():
     cu = _cu([500, 120, 900])
     t = _inputs(4, 128, torch.bfloat16, cu, cu, 17)

@@ -170,6 +170,18 @@ def test_two_calls_at_once():
         assert all(torch.equal(p, q) for p, q in zip(x, want[0])) and all(torch.equal(p, q) for p, q in zip(y, want[1]))
 
 
+def test_no_tokens():
+    e = lambda *s: torch.empty(s, device="cuda", requires_grad=True)
+    lam = torch.full((2,), 0.3, device="cuda", requires_grad=True)
+    q, k, v = e(0, 2, 64), e(0, 2, 64), e(0, 2, 64)
+    o, loss, _ = moga_diff_attention(torch.empty((0, 32), device="cuda"), torch.randn((3, 32), device="cuda"), q, k, v, lam, 0.125)
+    assert o.shape == (0, 2, 64)
+    grads = torch.autograd.grad(o, [q, k, v, lam], torch.empty_like(o))
+    assert all(g.shape == t.shape for g, t in zip(grads, (q, k, v, lam))) and (grads[3] == 0).all()
+    y = layer_norm(torch.empty((0, 3, 16), device="cuda", requires_grad=True))
+    assert y.shape == (0, 3, 16)
+
+
 def test_unrouted_gradients_and_no_grad():
     N, H, D = 64, 2, 64
     rnd = lambda s, *shape: torch.randn(shape, generator=torch.Generator(device="cuda").manual_seed(s), device="cuda")
