@@ -143,10 +143,10 @@ struct DiffPlainSweep : DiffState<D, 1> {
   }
 };
 
-// (SPLIT kernels) blockIdx.y's share of n rows from `first` on: whole steps of 32, as evenly as they go.
-__device__ __forceinline__ void piece_range(int& first, int& n) {
+// Piece `piece` of n rows from `first` on: whole steps of 32, as evenly as they go.
+__device__ __forceinline__ void piece_range(int piece, int pieces, int& first, int& n) {
   const int64_t steps = (n + 31) >> 5;
-  const int t0 = (int)(steps * blockIdx.y / gridDim.y), t1 = (int)(steps * (blockIdx.y + 1) / gridDim.y);
+  const int t0 = (int)(steps * piece / pieces), t1 = (int)(steps * (piece + 1) / pieces);
   const int end = min(n, 32 * t1);
   first += 32 * t0;
   n = end - 32 * t0;
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(256, 2) void diff_fwd_kernel(DiffFwd a) {
   if (!find_work<false>(a.cu_q, a.tile_start, a.G, a.H, kRows<T>, blockIdx.x, w)) return;
   const int head = w.head, ge = w.ti.row_end;
   int gs = a.cu_k[w.ti.group], n = a.cu_k[w.ti.group + 1] - gs;
-  if constexpr (SPLIT) piece_range(gs, n);
+  if constexpr (SPLIT) piece_range(blockIdx.y, gridDim.y, gs, n);
   gs = __builtin_amdgcn_readfirstlane(gs);
   n = __builtin_amdgcn_readfirstlane(n);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
@@ -386,6 +386,7 @@ struct DiffBwd {
   float* share;   // [H][Nq]: a row's part of -dlambda
   // split: pieces of the other side's rows, [piece] of d_q and of share as they are above, and of d_k, then d_v, in fp32
   float *part_q, *part_share, *part_k;
+  int q_pieces, k_pieces;
 };
 
 // The row constants: 16 lanes per row.  delta is made of the unrounded O_m: from rounded ones the gradients of groups of some hundred keys and
@@ -423,15 +424,14 @@ __global__ __launch_bounds__(256) void diff_rows_kernel(const T* __restrict__ d_
 }
 
 // dQ and the rows' shares of dlambda: a wave owns 16 NC queries and sweeps the keys.
-template <typename T, int D, bool SPLIT>
-__global__ __launch_bounds__(256, 2) void diff_dq_kernel(DiffBwd a) {
+template <typename T, int D>
+__device__ __forceinline__ void diff_dq_block(DiffBwd a, int block, int piece, typename DiffTiles<T, D>::Lds& lds) {
   constexpr int NC = kCols<T>, KB = D / 64, DT = D / 16;
-  __shared__ typename DiffTiles<T, D>::Lds lds;
   WorkTile w;
-  if (!find_work<false>(a.cu_q, a.tile_start, a.G, a.H, kRows<T>, blockIdx.x, w)) return;
+  if (!find_work<false>(a.cu_q, a.tile_start, a.G, a.H, kRows<T>, block, w)) return;
   const int head = w.head, ge = w.ti.row_end;
   int gs = a.cu_k[w.ti.group], n = a.cu_k[w.ti.group + 1] - gs;
-  if constexpr (SPLIT) piece_range(gs, n);
+  if (a.q_pieces > 1) piece_range(piece, a.q_pieces, gs, n);
   gs = __builtin_amdgcn_readfirstlane(gs);
   n = __builtin_amdgcn_readfirstlane(n);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
@@ -524,8 +524,8 @@ __global__ __launch_bounds__(256, 2) void diff_dq_kernel(DiffBwd a) {
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) store4(out, dt, dq[dt][q] * (dt < DT / 2 ? a.scale : -lam * a.scale));
     };
-    if constexpr (SPLIT) {
-      const int64_t at = (int64_t)blockIdx.y * a.H * a.Nq + head_q + row;
+    if (a.q_pieces > 1) {
+      const int64_t at = (int64_t)piece * a.H * a.Nq + head_q + row;
       store(a.part_q + at * D);
       if (sizeof(T) == 2 && g == 0) a.part_share[at] = sh;
     } else {
@@ -536,7 +536,7 @@ __global__ __launch_bounds__(256, 2) void diff_dq_kernel(DiffBwd a) {
 }
 
 // fp32 dK and dV: a wave owns 16 keys and sweeps the queries, with their row constants beside them in LDS.
-template <typename T, int D, bool SPLIT>
+template <typename T, int D>
 __global__ __launch_bounds__(256, 1) void diff_dkdv_f32_kernel(DiffBwd a) {
   constexpr int NC = 1, KB = D / 64, DT = D / 16;
   __shared__ typename DiffTiles<T, D, true>::Lds lds;
@@ -544,7 +544,7 @@ __global__ __launch_bounds__(256, 1) void diff_dkdv_f32_kernel(DiffBwd a) {
   if (!find_work<false>(a.cu_k, a.tile_start, a.G, a.H, kKeyRows<T>, blockIdx.x, w)) return;
   const int head = w.head, ge = w.ti.row_end;
   int gs = a.cu_q[w.ti.group], n = a.cu_q[w.ti.group + 1] - gs;
-  if constexpr (SPLIT) piece_range(gs, n);
+  if (a.k_pieces > 1) piece_range(blockIdx.y, a.k_pieces, gs, n);
   gs = __builtin_amdgcn_readfirstlane(gs);
   n = __builtin_amdgcn_readfirstlane(n);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
@@ -632,7 +632,7 @@ __global__ __launch_bounds__(256, 1) void diff_dkdv_f32_kernel(DiffBwd a) {
         store4(d_v, dt, dv[dt][k]);
       }
     };
-    if constexpr (SPLIT) {
+    if (a.k_pieces > 1) {
       float* part = a.part_k + ((int64_t)blockIdx.y * 2 * a.H * a.Nk + head_k + row) * D;
       store(part, part + (int64_t)a.H * a.Nk * D);
     } else {
@@ -641,17 +641,15 @@ __global__ __launch_bounds__(256, 1) void diff_dkdv_f32_kernel(DiffBwd a) {
   }
 }
 
-// bf16: diff_keys.h
-template <bool SPLIT>
-__global__ __launch_bounds__(256, 2) void diff_dkdv_kernel(DiffBwd a) {
+// bf16 dK and dV: diff_keys.h.
+__device__ __forceinline__ void diff_dkdv_block(DiffBwd a, int block, int piece, DiffKeySweep::Lds& lds) {
   constexpr int NC = DiffKeySweep::NC, D = kHeadDim;
   typedef unsigned short T;
-  __shared__ DiffKeySweep::Lds lds;
   WorkTile w;
-  if (!find_work<false>(a.cu_k, a.tile_start, a.G, a.H, kKeyRows<T>, blockIdx.x, w)) return;
+  if (!find_work<false>(a.cu_k, a.tile_start, a.G, a.H, kKeyRows<T>, block, w)) return;
   const int head = w.head, ge = w.ti.row_end;
   int gs = a.cu_q[w.ti.group], n = a.cu_q[w.ti.group + 1] - gs;
-  if constexpr (SPLIT) piece_range(gs, n);
+  if (a.k_pieces > 1) piece_range(piece, a.k_pieces, gs, n);
   gs = __builtin_amdgcn_readfirstlane(gs);
   n = __builtin_amdgcn_readfirstlane(n);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -694,12 +692,34 @@ __global__ __launch_bounds__(256, 2) void diff_dkdv_kernel(DiffBwd a) {
         store4(d_v, dt, k.dv[dt][c]);
       }
     };
-    if constexpr (SPLIT) {
-      float* part = a.part_k + ((int64_t)blockIdx.y * 2 * a.H * a.Nk + head_k + row) * D;
+    if (a.k_pieces > 1) {
+      float* part = a.part_k + ((int64_t)piece * 2 * a.H * a.Nk + head_k + row) * D;
       store(part, part + (int64_t)a.H * a.Nk * D);
     } else {
       store((T*)a.d_k + (head_k + row) * D, (T*)a.d_v + (head_k + row) * D);
     }
+  }
+}
+
+// fp32 dQ.
+template <int D>
+__global__ __launch_bounds__(256, 2) void diff_dq_f32_kernel(DiffBwd a) {
+  __shared__ typename DiffTiles<float, D>::Lds lds;
+  diff_dq_block<float, D>(a, blockIdx.x, blockIdx.y, lds);
+}
+
+// bf16, both: blocks of keys (first of their pieces, then the next), then blocks of queries, which fill the others' last rounds.
+__global__ __launch_bounds__(256, 2) void diff_bwd_kernel(DiffBwd a, const int32_t* __restrict__ q_tiles, int q_blocks, int k_blocks) {
+  __shared__ union {
+    DiffTiles<unsigned short, kHeadDim>::Lds q;
+    DiffKeySweep::Lds k;
+  } lds;
+  const int b = blockIdx.x, keys = k_blocks * a.k_pieces;
+  if (b < keys) {
+    diff_dkdv_block(a, b % k_blocks, b / k_blocks, lds.k);
+  } else {
+    a.tile_start = q_tiles;
+    diff_dq_block<unsigned short, kHeadDim>(a, (b - keys) % q_blocks, (b - keys) / q_blocks, lds.q);
   }
 }
 
@@ -884,13 +904,14 @@ extern "C" int moga_diff_attn_bwd(const void* d_oh, const void* qh, const void* 
     return MOGA_ERR_INVALID_ARG;
   const size_t need = moga_diff_attn_bwd_ws_bytes(Nq, H, G);
   if (need && (!ws || ws_bytes < need)) return MOGA_ERR_WORKSPACE;
-  const int64_t q_blocks = diff_blocks(Nq, H, G, rows_of(dtype)), k_blocks = diff_blocks(Nk, H, G, key_rows_of(dtype)), rows = Nq * H;
+  const int64_t q_blocks = diff_blocks(Nq, H, G, rows_of(dtype)), k_blocks = Nk > 0 ? diff_blocks(Nk, H, G, key_rows_of(dtype)) : 0,
+                rows = Nq * H;
   DiffBwdSplit split = {1, 1, 0, 0, 0};
   if (Nq > 0 && ws_bytes >= moga_diff_attn_bwd_preferred(Nq, Nk, H, D, G, dtype)) split = diff_bwd_split(Nq, Nk, H, D, G, dtype);
   if (Nq == 0) split.k = 0;   // keys without queries: zeros
   const int64_t sum_blocks = ((split.q != 1 ? rows : 0) + (split.k != 1 ? 2 * Nk * H : 0) + 1024 / D - 1) / (1024 / D);
-  if (!grid_fits(q_blocks * split.q, 256) || !grid_fits(k_blocks * std::max(1, split.k), 256) || !grid_fits((rows + 15) / 16, 256) ||
-      !grid_fits(sum_blocks, 256))
+  const int64_t joint = q_blocks * split.q + k_blocks * split.k;
+  if (!grid_fits(joint, 256) || !grid_fits((rows + 15) / 16, 256) || !grid_fits(sum_blocks, 256))
     return MOGA_ERR_UNSUPPORTED;
   hipStream_t st = (hipStream_t)stream;
   int32_t *tq = nullptr, *tk = nullptr;
@@ -902,7 +923,8 @@ extern "C" int moga_diff_attn_bwd(const void* d_oh, const void* qh, const void* 
   }
   floatx4_t* rc = (floatx4_t*)((char*)ws + 2 * tile_bytes(G));
   float* share = (float*)(rc + rows);
-  DiffBwd a = {d_oh, qh, kh, vh, lambda, cu_seqlens_q, cu_seqlens_k, tq, rc, Nq, Nk, H, G, softmax_scale, d_qh, d_kh, d_vh, share, nullptr, nullptr, nullptr};
+  DiffBwd a = {d_oh, qh, kh, vh, lambda, cu_seqlens_q, cu_seqlens_k, tq, rc, Nq, Nk, H, G, softmax_scale, d_qh, d_kh, d_vh, share, nullptr, nullptr, nullptr,
+               split.q, split.k};
   if (split.q > 1 || split.k > 1) {
     char* room = (char*)ws + need;
     a.part_q = (float*)room;
@@ -914,15 +936,11 @@ extern "C" int moga_diff_attn_bwd(const void* d_oh, const void* qh, const void* 
 #define MOGA_DIFF_BWD(T, D)                                                                                                            \
   do {                                                                                                                                 \
     diff_rows_kernel<T, D><<<(unsigned)((rows + 15) / 16), 256, 0, st>>>((const T*)d_oh, parts, lse, rows, rc, share);                  \
-    if (split.q > 1) diff_dq_kernel<T, D, true><<<dim3((unsigned)q_blocks, split.q), 256, 0, st>>>(a);                                   \
-    else diff_dq_kernel<T, D, false><<<(unsigned)q_blocks, 256, 0, st>>>(a);                                                           \
-    const dim3 grid((unsigned)k_blocks, std::max(1, split.k));                                                                         \
     if constexpr (sizeof(T) == 4) {                                                                                                    \
-      if (Nk > 0 && split.k > 1) diff_dkdv_f32_kernel<T, D, true><<<grid, 256, 0, st>>>(b);                                             \
-      else if (Nk > 0) diff_dkdv_f32_kernel<T, D, false><<<grid, 256, 0, st>>>(b);                                                      \
+      diff_dq_f32_kernel<D><<<dim3((unsigned)q_blocks, split.q), 256, 0, st>>>(a);                                                     \
+      if (Nk > 0) diff_dkdv_f32_kernel<T, D><<<dim3((unsigned)k_blocks, split.k), 256, 0, st>>>(b);                                     \
     } else {                                                                                                                           \
-      if (Nk > 0 && split.k > 1) diff_dkdv_kernel<true><<<grid, 256, 0, st>>>(b);                                                       \
-      else if (Nk > 0) diff_dkdv_kernel<false><<<grid, 256, 0, st>>>(b);                                                                \
+      diff_bwd_kernel<<<(unsigned)joint, 256, 0, st>>>(b, tq, (int)q_blocks, (int)k_blocks);                                            \
     }                                                                                                                                  \
   } while (0)
   if (Nq > 0) {
