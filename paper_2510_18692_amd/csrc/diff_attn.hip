@@ -802,11 +802,14 @@ size_t diff_piece_bytes(int64_t Nq, int H, int D) { return (size_t)Nq * H * 2 * 
 // tile of queries (1: whole).
 struct DiffSplit { int pieces, chunk; };
 DiffSplit diff_split(int64_t Nq, int64_t Nk, int H, int D, int G, int dtype) {
-  // Up to 16 queries a group the matrix products of a tile of 128 are idle work, and three of its waves too: pieces of keys for some two rounds
-  // of blocks, one a CU, none under 256 keys, and as many as 256 MB hold (one group might have all the keys).
+  // Up to 16 queries a group the matrix products of a tile of 128 are idle work, and three of its waves too: pieces of keys for two rounds of
+  // blocks, one a CU (or one round more than what the groups' last pieces make), none under 256 keys, and as many as 256 MB hold (one group
+  // might have all the keys).  A group's last piece is half a piece on average.
   const int64_t most = (256 << 20) / (int64_t)diff_piece_bytes(Nq, H, D);
   if (dtype == MOGA_BF16 && Nq <= 16 * (int64_t)G && Nk / G >= 128 && most >= 1) {
-    const int64_t chunk = round_up((size_t)std::min(Nk, std::max({(int64_t)256, Nk * H / (2 * kCus), (Nk + most - 1) / most})), 128);
+    const int64_t ends = (int64_t)G * H / 2, rounds = std::max<int64_t>(2, (ends + 2 * kCus - 1) / kCus);
+    const int64_t even = Nk * H / std::max<int64_t>(1, rounds * kCus * 49 / 50 - ends);
+    const int64_t chunk = round_up((size_t)std::min(Nk, std::max({(int64_t)256, even, (Nk + most - 1) / most})), 128);
     return {(int)((Nk + chunk - 1) / chunk), (int)chunk};
   }
   return {diff_pieces(Nq, Nk, H, G, rows_of(dtype), dtype), 0};

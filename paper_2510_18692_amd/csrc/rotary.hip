@@ -82,10 +82,19 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
   const int h0 = blockIdx.y * a.heads_each, nh = min(a.heads_each, a.first[3] - h0);
   // items of a head: a chunk each, or (same places of two chunks) a pair of chunks or one that is only copied
   const int pairs = half / V, items = WHOLE && !INTERLEAVED ? chunks - pairs : chunks;
+  // (row, head, item) of a thread's pieces of work, 256 apart, by carries: a division each would cost as much as the rest.  Heads of a token lie
+  // beside each other in token order, rows of a head in sorted order: the side that is written is walked.
+  const int inner = LAYOUT == 1 ? rows : nh;
+  int item = threadIdx.x % items, in = threadIdx.x / items % inner, out = threadIdx.x / items / inner;
+  const int item_step = 256 % items, in_step = 256 / items % inner, out_step = 256 / items / inner;
   for (int i = threadIdx.x; i < rows * nh * items; i += 256) {
-    const int item = i % items, rest = i / items;
-    // heads of a token lie beside each other in token order, rows of a head in sorted order: the side that is written is walked
-    const int r = LAYOUT == 1 ? rest % rows : rest / nh, hh = h0 + (LAYOUT == 1 ? rest / rows : rest % nh);
+    const int r = LAYOUT == 1 ? in : out, hh = h0 + (LAYOUT == 1 ? out : in);
+    const int at = item;
+    item += item_step;
+    in += in_step;
+    out += out_step;
+    if (item >= items) item -= items, ++in;
+    if (in >= inner) in -= inner, ++out;
     const int which = (hh >= a.first[1]) + (hh >= a.first[2]);
     const int head = hh - a.first[which], H = a.heads[which];
     const int64_t slot = row0 + r, tok = LAYOUT == 0 ? slot : a.perm[slot];
@@ -95,9 +104,9 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
     const floatx2_t* t = turn + r * half;
     const bool copied = which == 2;
     if constexpr (WHOLE && !INTERLEAVED) {
-      const int c = item < pairs ? item : item + pairs;   // the chunk, or the first of two
+      const int c = at < pairs ? at : at + pairs;   // the chunk, or the first of two
       const uintx4_t w1 = *(const uintx4_t*)(src + c * V);
-      if (item >= pairs) {
+      if (at >= pairs) {
         *(uintx4_t*)(dst + c * V) = w1;
         continue;
       }
@@ -119,9 +128,9 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
       *(uintx4_t*)(dst + c * V) = Chunk<T>::put(y1);
       *(uintx4_t*)(dst + half + c * V) = Chunk<T>::put(y2);
     } else {
-      const uintx4_t w = *(const uintx4_t*)(src + item * V);
-      if (copied || item * V >= a.R) {
-        *(uintx4_t*)(dst + item * V) = w;
+      const uintx4_t w = *(const uintx4_t*)(src + at * V);
+      if (copied || at * V >= a.R) {
+        *(uintx4_t*)(dst + at * V) = w;
         continue;
       }
       float f[V], y[V];
@@ -129,7 +138,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
       if constexpr (INTERLEAVED) {
 #pragma unroll
         for (int e = 0; e < V; e += 2) {
-          const int p = (item * V + e) / 2;
+          const int p = (at * V + e) / 2;
           if (p < half) {
             const floatx2_t cs = t[p];
             y[e] = f[e] * cs[0] - f[e + 1] * cs[1];
@@ -142,7 +151,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
       } else {   // partners anywhere: read one by one
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          const int d = item * V + e;
+          const int d = at * V + e;
           if (d < a.R) {
             const bool low = d < half;
             const floatx2_t cs = t[low ? d : d - half];
@@ -153,7 +162,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
           }
         }
       }
-      *(uintx4_t*)(dst + item * V) = Chunk<T>::put(y);
+      *(uintx4_t*)(dst + at * V) = Chunk<T>::put(y);
     }
   }
 }
