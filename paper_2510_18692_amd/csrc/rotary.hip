@@ -6,7 +6,13 @@
 // With several axes a token has a position on each, and every axis a run of pairs.
 //
 // Angles: the product and its reduction to a part of a turn in 64 bits (at position 500,000 a product in 32 bits is 0.03 radians off), then
-// sine and cosine in 32 bits, once per token and pair, in LDS, for all heads of q and k.  Bound by HBM.
+// sine and cosine in 32 bits, once per token and pair, in LDS, for all heads of q and k.
+//
+// Bound by HBM: every chunk of 16 bytes is read and written once, by a lane of its own, so that loads and stores are whole rows.  A lane of the
+// half layout reads its partner's chunk too, from L1; one lane for both partners halves those loads but splits every row's traffic in two:
+// 32,760 x 12 heads of 128, 96 channels turned, bf16, into sorted order 139 us against 128, back 149 against 139 (4.3 TB/s; gathering
+// rows without turning them takes 111).  Three chunks of a lane in flight together were slower everywhere (149, 156; fewer waves fit).
+// 62,400 x 32 heads in token order, neighbours, bf16: 0.75 ms.
 #include <algorithm>
 #include <cmath>
 
@@ -80,20 +86,18 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
   __syncthreads();
 
   const int h0 = blockIdx.y * a.heads_each, nh = min(a.heads_each, a.first[3] - h0);
-  // items of a head: a chunk each, or (same places of two chunks) a pair of chunks or one that is only copied
-  const int pairs = half / V, items = WHOLE && !INTERLEAVED ? chunks - pairs : chunks;
-  // (row, head, item) of a thread's pieces of work, 256 apart, by carries: a division each would cost as much as the rest.  Heads of a token lie
-  // beside each other in token order, rows of a head in sorted order: the side that is written is walked.
-  const int inner = LAYOUT == 1 ? rows : nh;
-  int item = threadIdx.x % items, in = threadIdx.x / items % inner, out = threadIdx.x / items / inner;
-  const int item_step = 256 % items, in_step = 256 / items % inner, out_step = 256 / items / inner;
-  for (int i = threadIdx.x; i < rows * nh * items; i += 256) {
+  // A lane a chunk: (row, head, chunk) of a thread's pieces of work, 256 apart, by carries: a division each would cost as much as the rest.
+  // Heads of a token lie beside each other in token order, rows of a head in sorted order: the side that is written is walked.
+  const int pairs = half / V, inner = LAYOUT == 1 ? rows : nh;
+  int chunk = threadIdx.x % chunks, in = threadIdx.x / chunks % inner, out = threadIdx.x / chunks / inner;
+  const int chunk_step = 256 % chunks, in_step = 256 / chunks % inner, out_step = 256 / chunks / inner;
+  for (int i = threadIdx.x; i < rows * nh * chunks; i += 256) {
     const int r = LAYOUT == 1 ? in : out, hh = h0 + (LAYOUT == 1 ? out : in);
-    const int at = item;
-    item += item_step;
+    const int at = chunk;
+    chunk += chunk_step;
     in += in_step;
     out += out_step;
-    if (item >= items) item -= items, ++in;
+    if (chunk >= chunks) chunk -= chunks, ++in;
     if (in >= inner) in -= inner, ++out;
     const int which = (hh >= a.first[1]) + (hh >= a.first[2]);
     const int head = hh - a.first[which], H = a.heads[which];
@@ -102,68 +106,51 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
     const T* __restrict__ src = (const T*)a.src[which] + (LAYOUT == 2 ? in_sorted : in_tokens);
     T* __restrict__ dst = (T*)a.dst[which] + (LAYOUT == 1 ? in_sorted : in_tokens);
     const floatx2_t* t = turn + r * half;
-    const bool copied = which == 2;
-    if constexpr (WHOLE && !INTERLEAVED) {
-      const int c = at < pairs ? at : at + pairs;   // the chunk, or the first of two
-      const uintx4_t w1 = *(const uintx4_t*)(src + c * V);
-      if (at >= pairs) {
-        *(uintx4_t*)(dst + c * V) = w1;
-        continue;
+    const uintx4_t w = *(const uintx4_t*)(src + at * V);
+    if (which == 2 || at * V >= a.R) {
+      *(uintx4_t*)(dst + at * V) = w;
+      continue;
+    }
+    float f[V], y[V];
+    Chunk<T>::get(w, f);
+    if constexpr (INTERLEAVED) {
+#pragma unroll
+      for (int e = 0; e < V; e += 2) {
+        const int p = (at * V + e) / 2;
+        if (p < half) {
+          const floatx2_t cs = t[p];
+          y[e] = f[e] * cs[0] - f[e + 1] * cs[1];
+          y[e + 1] = f[e + 1] * cs[0] + f[e] * cs[1];
+        } else {
+          y[e] = f[e];
+          y[e + 1] = f[e + 1];
+        }
       }
-      const uintx4_t w2 = *(const uintx4_t*)(src + half + c * V);
-      if (copied) {
-        *(uintx4_t*)(dst + c * V) = w1;
-        *(uintx4_t*)(dst + half + c * V) = w2;
-        continue;
-      }
-      float f1[V], f2[V], y1[V], y2[V];
-      Chunk<T>::get(w1, f1);
-      Chunk<T>::get(w2, f2);
+    } else if constexpr (WHOLE) {
+      const bool low = at < pairs;
+      const int c = low ? at : at - pairs;
+      float o[V];   // the partners, which their own lane loads too: the second read is from L1
+      Chunk<T>::get(*(const uintx4_t*)(src + (low ? at + pairs : c) * V), o);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const floatx2_t cs = t[c * V + e];
-        y1[e] = f1[e] * cs[0] - f2[e] * cs[1];
-        y2[e] = f2[e] * cs[0] + f1[e] * cs[1];
+        y[e] = f[e] * cs[0] + o[e] * (low ? -cs[1] : cs[1]);
       }
-      *(uintx4_t*)(dst + c * V) = Chunk<T>::put(y1);
-      *(uintx4_t*)(dst + half + c * V) = Chunk<T>::put(y2);
-    } else {
-      const uintx4_t w = *(const uintx4_t*)(src + at * V);
-      if (copied || at * V >= a.R) {
-        *(uintx4_t*)(dst + at * V) = w;
-        continue;
-      }
-      float f[V], y[V];
-      Chunk<T>::get(w, f);
-      if constexpr (INTERLEAVED) {
+    } else {   // partners anywhere: read one by one
 #pragma unroll
-        for (int e = 0; e < V; e += 2) {
-          const int p = (at * V + e) / 2;
-          if (p < half) {
-            const floatx2_t cs = t[p];
-            y[e] = f[e] * cs[0] - f[e + 1] * cs[1];
-            y[e + 1] = f[e + 1] * cs[0] + f[e] * cs[1];
-          } else {
-            y[e] = f[e];
-            y[e + 1] = f[e + 1];
-          }
-        }
-      } else {   // partners anywhere: read one by one
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const int d = at * V + e;
-          if (d < a.R) {
-            const bool low = d < half;
-            const floatx2_t cs = t[low ? d : d - half];
-            const float other = value(src[low ? d + half : d - half]);
-            y[e] = low ? f[e] * cs[0] - other * cs[1] : f[e] * cs[0] + other * cs[1];
-          } else {
-            y[e] = f[e];
-          }
+      for (int e = 0; e < V; ++e) {
+        const int d = at * V + e;
+        if (d < a.R) {
+          const bool low = d < half;
+          const floatx2_t cs = t[low ? d : d - half];
+          const float other = value(src[low ? d + half : d - half]);
+          y[e] = low ? f[e] * cs[0] - other * cs[1] : f[e] * cs[0] + other * cs[1];
+        } else {
+          y[e] = f[e];
         }
       }
-      *(uintx4_t*)(dst + at * V) = Chunk<T>::put(y);
     }
+    *(uintx4_t*)(dst + at * V) = Chunk<T>::put(y);
   }
 }
 
