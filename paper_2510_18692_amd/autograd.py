@@ -34,7 +34,9 @@ def moga_diff_attention(x, w, q, k, v, lam, softmax_scale, balance_alpha=None, g
                         interleaved=False, factor=1.0):
     """moga_attention with differential attention in the groups: the two halves of a head's channels are two maps, lam f32 [H] the weight of
     the second (moga_diff_attn_fwd); gradients flow to lam as well.  With positions and inv_freq (binding.moga_rotary_freqs) q and k are
-    rotated on their way into the groups.  -> (o [N, H, D], balancing loss or None, group [N])."""
+    rotated on their way into the groups.  -> (o [N, H, D], balancing loss or None, group [N]).
+    A step whose backward is captured into a graph: let go of the eager results of the same leaves before the capture (torch keeps the stream
+    on which a leaf was first used, and a capture may not join work of another)."""
     o, loss, group = mg._nat.diff_attention(x, w, q, k, v, lam, softmax_scale, balance_alpha, grad_x, positions, inv_freq, axis_pairs or [],
                                             interleaved, factor)
     return o, (loss if balance_alpha is not None else None), group

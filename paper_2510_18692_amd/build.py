@@ -22,9 +22,6 @@ FLAGS = [
     "-Wno-unused-command-line-argument", "-Wno-deprecated-volatile",
     "-I", os.path.join(ROOT, "include"), "-I", CSRC,
 ]
-# diff_attn: results of matrix instructions in vector registers, accumulators moved to the others afterwards.  Without, the scores of the dK/dV
-# kernel, which has more than 256 registers, are moved one by one before they can be used.
-FLAGS_OF = {"diff_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def _hipcc() -> str:
@@ -68,7 +65,7 @@ def build(verbose: bool = False, extra_flags=()) -> str:
 
     def compile_one(src):
         obj = os.path.join(objdir, src.replace(".hip", ".o"))
-        cmd = [hipcc, *FLAGS, *FLAGS_OF.get(src, ()), *extra_flags, "-c", os.path.join(CSRC, src), "-o", obj]
+        cmd = [hipcc, *FLAGS, *extra_flags, "-c", os.path.join(CSRC, src), "-o", obj]
         r = subprocess.run(cmd, capture_output=True, text=True)
         out = "\n".join(l for l in (r.stdout + r.stderr).splitlines()
                         if "packed-fp32-ops" not in l and l.strip())

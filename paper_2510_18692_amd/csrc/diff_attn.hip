@@ -5,6 +5,9 @@
 //   dS_1 = P_1 * (dP - delta_1), dS_2 = -lambda P_2 * (dP - delta_2), dQ_m = s dS_m K_m, dK_m = s dS_m^T Q_m
 //   dV = (P_1 - lambda P_2)^T dO, dlambda = -sum P_2 * dP
 // so that a backward has the matrix products of plain attention, and a forward one and a half times them (two weighted sums of V).
+//
+// bf16 calls are bound by the matrix cores (diff_steps.h, diff_keys.h, dQ below), those of few queries by HBM, fp32 calls by products of 1 / 8
+// of bf16's rate and, at the sizes of gradient checks, by launches and by the length of a group's sweep.
 #include <algorithm>
 #include <cmath>
 
@@ -123,7 +126,7 @@ __device__ __forceinline__ void diff_fwd_step(const Tiles& tiles, const Frag<T> 
   }
 }
 
-// fp32: step by step.
+// fp32: step by step.  4,096 x 2 heads of 64, 8 groups: 34 us in pieces of the keys and 7 to join them.
 template <typename T, int D>
 struct DiffPlainSweep : DiffState<D, 1> {
   typedef DiffTiles<T, D> Tiles;
@@ -152,7 +155,8 @@ __device__ __forceinline__ void piece_range(int piece, int pieces, int& first, i
   n = end - 32 * t0;
 }
 
-// A tile of kRows queries, or (SPLIT) blockIdx.y's share of its keys.
+// A tile of kRows queries, or (SPLIT) blockIdx.y's share of its keys.  32,760 x 12 heads, bf16, 8 groups 1.27 ms; 10,007 x 12, 20 groups of unequal
+// length 105 us.
 template <typename T, int D, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void diff_fwd_kernel(DiffFwd a) {
   constexpr int NC = kCols<T>;
@@ -225,7 +229,8 @@ __global__ __launch_bounds__(256, 2) void diff_fwd_kernel(DiffFwd a) {
 
 // bf16 calls of few queries a group: the blocks go by the keys, `chunk` of a group each, and take all queries of the group, 16 at a time.  The
 // four waves share the keys out, every fourth tile each from a ring of its own without a barrier, and add up what they have.  Bound by HBM:
-// 4 x 32 KB are on their way to a CU.  Sums and maxima go to part and stat, for piece (first key / chunk) of the group.
+// 4 x 32 KB are on their way to a CU.  4 queries, 65,536 keys, 12 heads: 77 us, 5.2 TB/s (a call 84 us; by tiles of 128 queries with split keys 247).
+// Sums and maxima go to part and stat, for piece (first key / chunk) of the group.
 __global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd a, int chunk) {
   constexpr int D = kHeadDim;
   typedef unsigned short T;
@@ -389,7 +394,7 @@ struct DiffBwd {
   int q_pieces, k_pieces;
 };
 
-// The row constants: 16 lanes per row.  delta is made of the unrounded O_m: from rounded ones the gradients of groups of some hundred keys and
+// The row constants: 16 lanes per row, bound by HBM (62,400 x 12 heads, bf16: 0.17 ms, 5.8 TB/s).  delta is made of the unrounded O_m: from rounded ones the gradients of groups of some hundred keys and
 // fewer are a tenth further off.  share (fp32): the rows' parts of -dlambda, which are delta_2; of bf16 calls, whose O_2 comes from
 // rounded weights, the dQ kernel makes them from the unrounded ones.
 template <typename T, int D>
@@ -423,7 +428,9 @@ __global__ __launch_bounds__(256) void diff_rows_kernel(const T* __restrict__ d_
   }
 }
 
-// dQ and the rows' shares of dlambda: a wave owns 16 NC queries and sweeps the keys.
+// dQ and the rows' shares of dlambda: a wave owns 16 NC queries and sweeps the keys.  Three products of a step, with Q and dO in registers: the
+// compiler's order of a step was as fast as one written out like the forward's, and raised wave priorities were slower.  fp32, 4,096 x 2 heads
+// of 64, 8 groups: 32 us.
 template <typename T, int D>
 __device__ __forceinline__ void diff_dq_block(DiffBwd a, int block, int piece, typename DiffTiles<T, D>::Lds& lds) {
   constexpr int NC = kCols<T>, KB = D / 64, DT = D / 16;
@@ -535,9 +542,10 @@ __device__ __forceinline__ void diff_dq_block(DiffBwd a, int block, int piece, t
   }
 }
 
-// fp32 dK and dV: a wave owns 16 keys and sweeps the queries, with their row constants beside them in LDS.
-template <typename T, int D>
+// fp32 dK and dV: a wave owns 16 keys and sweeps the queries, with their row constants beside them in LDS.  4,096 x 2 heads of 64, 8 groups: 43 us.
+template <int D>
 __global__ __launch_bounds__(256, 1) void diff_dkdv_f32_kernel(DiffBwd a) {
+  typedef float T;
   constexpr int NC = 1, KB = D / 64, DT = D / 16;
   __shared__ typename DiffTiles<T, D, true>::Lds lds;
   WorkTile w;
@@ -708,7 +716,8 @@ __global__ __launch_bounds__(256, 2) void diff_dq_f32_kernel(DiffBwd a) {
   diff_dq_block<float, D>(a, blockIdx.x, blockIdx.y, lds);
 }
 
-// bf16, both: blocks of keys (first of their pieces, then the next), then blocks of queries, which fill the others' last rounds.
+// bf16, both: blocks of keys (first of their pieces, then the next), then blocks of queries, which fill the others' last rounds: 10,007 x 12
+// heads, 20 unequal groups 206 us, 62,400 x 12, 8 groups 10.5 ms.
 __global__ __launch_bounds__(256, 2) void diff_bwd_kernel(DiffBwd a, const int32_t* __restrict__ q_tiles, int q_blocks, int k_blocks) {
   __shared__ union {
     DiffTiles<unsigned short, kHeadDim>::Lds q;
@@ -941,7 +950,7 @@ extern "C" int moga_diff_attn_bwd(const void* d_oh, const void* qh, const void* 
     diff_rows_kernel<T, D><<<(unsigned)((rows + 15) / 16), 256, 0, st>>>((const T*)d_oh, parts, lse, rows, rc, share);                  \
     if constexpr (sizeof(T) == 4) {                                                                                                    \
       diff_dq_f32_kernel<D><<<dim3((unsigned)q_blocks, split.q), 256, 0, st>>>(a);                                                     \
-      if (Nk > 0) diff_dkdv_f32_kernel<T, D><<<dim3((unsigned)k_blocks, split.k), 256, 0, st>>>(b);                                     \
+      if (Nk > 0) diff_dkdv_f32_kernel<D><<<dim3((unsigned)k_blocks, split.k), 256, 0, st>>>(b);                                        \
     } else {                                                                                                                           \
       diff_bwd_kernel<<<(unsigned)joint, 256, 0, st>>>(b, tq, (int)q_blocks, (int)k_blocks);                                            \
     }                                                                                                                                  \

@@ -607,7 +607,7 @@ void need_like(const Tensor& t, const Tensor& first, at::IntArrayRef size, at::S
 void need_like(const OptTensor& t, const Tensor& first, at::IntArrayRef size, at::ScalarType type, const char* name) {
   if (t) need_like(*t, first, size, type, name);
 }
-// A vector of 64-bit results' own size is an int in the C calls.
+// Sizes that the C calls take as int.
 int to_int(int64_t n) {
   need(n >= 0 && n <= INT32_MAX, "size beyond 32 bits");
   return (int)n;
@@ -959,6 +959,7 @@ struct DiffAttention : public torch::autograd::Function<DiffAttention> {
     const c10::OptionalDeviceGuard guard(q.device());
     const int64_t N = q.size(0), M = w.size(0);
     need(x.size(0) == N && x.size(1) == w.size(1), "x [N, d_model] and w [M, d_model] with the N of q");
+    need(x.device() == q.device(), "x: on another device");
     need_like(w, x, w.sizes(), at::kFloat, "w");
     need_like(k, q, q.sizes(), q.scalar_type(), "k");
     need_like(v, q, q.sizes(), q.scalar_type(), "v");

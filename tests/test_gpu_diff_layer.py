@@ -118,6 +118,45 @@ def test_forward_and_backward_in_a_graph_match_eager_on_every_replay():
         assert all(torch.equal(a, b) for a, b in zip(again, eager)), rep
 
 
+def test_captured_training_step():
+    """Forward and backward through the autograd functions in one graph, of leaves that no eager graph holds."""
+    N, H, D, M = 700, 3, 128, 4
+    rnd = lambda s, *shape: torch.randn(shape, generator=torch.Generator(device="cuda").manual_seed(s), device="cuda")
+    x, w, g = rnd(1, N, 64).bfloat16(), rnd(2, M, 64), rnd(6, N, H, D).bfloat16()
+    pos = torch.arange(N, dtype=torch.int32, device="cuda")
+    freq, _ = mg.moga_rotary_freqs(D)
+
+    def leaves():
+        t = [w, rnd(3, N, H, D).bfloat16(), rnd(4, N, H, D).bfloat16(), rnd(5, N, H, D).bfloat16(), torch.full((H,), 0.3, device="cuda"),
+             torch.ones(D, device="cuda")]
+        return [a.clone().requires_grad_() for a in t]
+
+    def step(t):
+        q = layer_norm(t[1], t[5])
+        o, loss, _ = moga_diff_attention(x, t[0], q, t[2], t[3], t[4], 0.125, balance_alpha=0.1, positions=pos, inv_freq=freq)
+        return [o.detach(), *torch.autograd.grad([o, loss], t, [g, torch.ones_like(loss)])]
+
+    want = [a.clone() for a in step(leaves())]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step(leaves())
+    torch.cuda.synchronize()
+    own = leaves()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step(own)
+    for rep in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(captured, want)), rep
+        again = step(leaves())
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(again, want)), rep
+        del again
+
+
 def test_on_another_stream():
     """Given a stream that is not the current one: inputs made there, outputs in its order, temporaries not reused too early."""
     side = torch.cuda.Stream()
