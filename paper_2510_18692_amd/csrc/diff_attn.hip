@@ -797,12 +797,29 @@ int key_rows_of(int dtype) { return dtype == MOGA_F32 ? kKeyRows<float> : kKeyRo
 int64_t diff_blocks(int64_t N, int H, int G, int rows) { return (max_tiles(N, G, rows) * H + 7) / 8 * 8; }
 size_t tile_bytes(int G) { return G > MOGA_MAX_GROUPS ? round_up(((size_t)G + 1) * sizeof(int32_t), 256) : 0; }
 
-// Pieces of the rows that a tile sweeps: where tiles of `rows` rows leave CUs idle, as many as fill two blocks a CU, none under 256 rows of a mean
-// group (fp32, whose steps take ten times as long: 128).  Backward, whole and in pieces: bf16 1,000 x 3 heads 86 and 51 us, 4,096 x 3 286
-// and 149, fp32 1,000 x 2 x 64 172 and 66; with pieces of 128 rows bf16 4,096 x 3, 8 groups 70 instead of 61.
-int diff_pieces(int64_t N, int64_t other, int H, int G, int rows, int dtype) {
-  const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(max_tiles(N, G, rows), N)) * H;
-  return (int)std::max<int64_t>(1, std::min({(int64_t)16, 2 * kCus / blocks, other / G / (dtype == MOGA_F32 ? 128 : 256)}));
+// Pieces of the rows that a tile sweeps, where tiles of `rows` rows leave CUs idle.  bf16: as many as fill two blocks a CU, none under 256 rows of a
+// mean group.  Backward, whole and in pieces: 1,000 x 3 heads 86 and 40 us, 4,096 x 3 286 and 151; with pieces of 128 rows 4,096 x 3,
+// 8 groups 70 instead of 61.
+// fp32, whose steps take ten times as long: none under 64 rows, and as many as make the fullest CU's work least: its blocks (an XCD deals its
+// share out to 32 CUs) times a block's steps and what starting it costs, in microseconds, and the traffic of the partial results.  One block a
+// CU takes 1.6 times what its products need.  Backward, whole and in pieces: 1,000 x 2 x 64 172 and 65 us; pieces for two blocks a CU of 128
+// rows and more instead: 6,000 x 4 x 128, 8 groups forward 175 instead of 156 and backward 463 instead of 389, 256 x 2 x 128 28 and 61 instead of
+// 22 and 44.
+int diff_pieces(int64_t N, int64_t other, int H, int G, int rows, int D, int dtype) {
+  if (dtype != MOGA_F32) {
+    const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(max_tiles(N, G, rows), N)) * H;
+    return (int)std::max<int64_t>(1, std::min({(int64_t)16, 2 * kCus / blocks, other / G / 256}));
+  }
+  const int64_t tiles = (std::min(N, G * (((N + G - 1) / G + rows - 1) / rows)) * H + 7) / 8, most = std::min<int64_t>(16, other / G / 64);
+  const double step = D * 0.02, start = 2 * step, traffic = (double)N * H * D * 16 / 6e6;
+  int best = 1;
+  double least = INFINITY;
+  for (int p = 1; p <= most && tiles * p <= kCus; ++p) {
+    const int64_t fullest = (tiles * p + 31) / 32;
+    const double cost = (fullest == 1 ? 1.6 : (double)fullest) * (other / G / 32. / p * step + start) + (p > 1 ? p * traffic : 0.);
+    if (cost < least) least = cost, best = p;
+  }
+  return best;
 }
 
 size_t diff_piece_bytes(int64_t Nq, int H, int D) { return (size_t)Nq * H * 2 * (D + 2) * sizeof(float); }
@@ -821,7 +838,7 @@ DiffSplit diff_split(int64_t Nq, int64_t Nk, int H, int D, int G, int dtype) {
     const int64_t chunk = round_up((size_t)std::min(Nk, std::max({(int64_t)256, even, (Nk + most - 1) / most})), 128);
     return {(int)((Nk + chunk - 1) / chunk), (int)chunk};
   }
-  return {diff_pieces(Nq, Nk, H, G, rows_of(dtype), dtype), 0};
+  return {diff_pieces(Nq, Nk, H, G, rows_of(dtype), D, dtype), 0};
 }
 
 struct DiffBwdSplit {
@@ -830,7 +847,7 @@ struct DiffBwdSplit {
   size_t bytes() const { return q_bytes + share_bytes + k_bytes; }
 };
 DiffBwdSplit diff_bwd_split(int64_t Nq, int64_t Nk, int H, int D, int G, int dtype) {
-  DiffBwdSplit s = {diff_pieces(Nq, Nk, H, G, rows_of(dtype), dtype), diff_pieces(Nk, Nq, H, G, key_rows_of(dtype), dtype), 0, 0, 0};
+  DiffBwdSplit s = {diff_pieces(Nq, Nk, H, G, rows_of(dtype), D, dtype), diff_pieces(Nk, Nq, H, G, key_rows_of(dtype), D, dtype), 0, 0, 0};
   if (s.q > 1) s.q_bytes = (size_t)s.q * H * Nq * D * sizeof(float), s.share_bytes = round_up((size_t)s.q * H * Nq * sizeof(float), 256);
   if (s.k > 1) s.k_bytes = (size_t)s.k * 2 * H * Nk * D * sizeof(float);
   return s;
