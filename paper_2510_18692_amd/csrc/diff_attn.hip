@@ -486,15 +486,18 @@ __device__ __forceinline__ void diff_dq_block(DiffBwd a, int block, int piece, t
           for (int q = 0; q < NC; ++q) dp[q] = mma(f, df[q][kb], kb == 0 ? floatx4_t{0.f, 0.f, 0.f, 0.f} : dp[q]);
         }
 #pragma unroll
-        for (int q = 0; q < NC; ++q)
+        for (int q = 0; q < NC; ++q) {
+          float sum = 0.f;   // four by themselves: fewer roundings at the size of the whole sum
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             float p1 = fast_exp2(fmaf(s[0][q][i], c, -rc[q][0])), p2 = fast_exp2(fmaf(s[1][q][i], c, -rc[q][1]));
             if (kMask && 8 * g + 4 * t + i >= left) p1 = p2 = 0.f;
-            if constexpr (sizeof(T) == 2) share[q] = fmaf(p2, dp[q][i], share[q]);
+            if constexpr (sizeof(T) == 2) sum = fmaf(p2, dp[q][i], sum);
             d1[q][4 * t + i] = p1 * (dp[q][i] - rc[q][2]);
             d2[q][4 * t + i] = p2 * (dp[q][i] - rc[q][3]);
           }
+          share[q] += sum;
+        }
       }
       Frag<T> f1[NC], f2[NC];
 #pragma unroll
