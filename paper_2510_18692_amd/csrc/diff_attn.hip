@@ -394,9 +394,10 @@ struct DiffBwd {
   int q_pieces, k_pieces;
 };
 
-// The row constants: 16 lanes per row, bound by HBM (62,400 x 12 heads, bf16: 0.17 ms, 5.8 TB/s).  delta is made of the unrounded O_m: from rounded ones the gradients of groups of some hundred keys and
-// fewer are a tenth further off.  share (fp32): the rows' parts of -dlambda, which are delta_2; of bf16 calls, whose O_2 comes from
-// rounded weights, the dQ kernel makes them from the unrounded ones.
+// The row constants: 16 lanes per row, bound by HBM (62,400 x 12 heads, bf16: 0.17 ms, 5.8 TB/s).  delta is made of the unrounded O_m: from
+// rounded ones the gradients of groups of some hundred keys are a tenth further off (shorter groups: diff_delta_kernel).  share (fp32): the
+// rows' parts of -dlambda, which are delta_2; of bf16 calls, whose O_2 comes from rounded weights, the dQ kernel makes them from the
+// unrounded ones.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void diff_rows_kernel(const T* __restrict__ d_o, const float* __restrict__ parts, const float* __restrict__ lse,
                                                         int64_t rows, floatx4_t* __restrict__ out, float* __restrict__ share) {
@@ -425,6 +426,96 @@ __global__ __launch_bounds__(256) void diff_rows_kernel(const T* __restrict__ d_
   if (t == 0) {
     out[row] = floatx4_t{lse[row] * kLog2e, lse[rows + row] * kLog2e, -a, b - a};
     if constexpr (sizeof(T) == 4) share[row] = b;
+  }
+}
+
+// Scores of both maps and dP of 16 rows of a tile: its first tensor's times x, its second's times y.
+template <typename T, int D, int NC, typename Tiles>
+__device__ __forceinline__ void diff_products(const Tiles& tiles, int t, const Frag<T> (&x)[NC][D / 32], const Frag<T> (&y)[NC][D / 32],
+                                              floatx4_t (&s)[2][NC], floatx4_t (&dp)[NC]) {
+  constexpr int KB = D / 64;
+#pragma unroll
+  for (int kb = 0; kb < 2 * KB; ++kb) {
+    const Frag<T> f = tiles.nat(0, t, kb);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) s[kb / KB][c] = mma(f, x[c][kb], kb % KB == 0 ? floatx4_t{0.f, 0.f, 0.f, 0.f} : s[kb / KB][c]);
+  }
+#pragma unroll
+  for (int kb = 0; kb < 2 * KB; ++kb) {
+    const Frag<T> f = tiles.nat(1, t, kb);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) dp[c] = mma(f, y[c][kb], kb == 0 ? floatx4_t{0.f, 0.f, 0.f, 0.f} : dp[c]);
+  }
+}
+
+// The row constants of bf16 calls of short groups, with delta_m = sum P_m dP from unrounded weights by a sweep of their own.  The forward's sums
+// of V have weights rounded to operands, and where few keys carry a row delta's error is felt: dQ's is 1.43 of a plain rounding's instead of
+// 1.49 at 70 keys a group, dK's 1.41 instead of 1.46.  Up to 256 keys of a mean group the sweep takes what reading `parts` does (backward of
+// 10,007 x 12 heads, 40 groups 141 us against 138, 60,000 x 12, 1,000 groups 674 against 682, 1,560 x 4, 8 groups 34 against 29); at
+// 500 keys it takes longer (20 groups 220 against 192) for 1.445 instead of 1.47.
+constexpr int64_t kDeltaKeys = 256;
+__global__ __launch_bounds__(256, 3) void diff_delta_kernel(DiffBwd a, const float* __restrict__ lse, floatx4_t* __restrict__ out) {
+  constexpr int NC = kCols<unsigned short>, D = kHeadDim;
+  typedef unsigned short T;
+  typedef DiffTiles<T, D, false, 1, 2> Tiles;   // a ring of two: three blocks a CU
+  __shared__ Tiles::Lds lds;
+  WorkTile w;
+  if (!find_work<false>(a.cu_q, a.tile_start, a.G, a.H, kRows<T>, blockIdx.x, w)) return;
+  const int head = w.head, ge = w.ti.row_end;
+  const int gs = __builtin_amdgcn_readfirstlane(a.cu_k[w.ti.group]);
+  const int n = __builtin_amdgcn_readfirstlane(a.cu_k[w.ti.group + 1]) - gs;
+  if (n <= 0) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  const int row0 = w.ti.tile_row + 16 * NC * wave;
+  const int64_t head_q = (int64_t)head * a.Nq, head_k = (int64_t)head * a.Nk;
+  const bool active = row0 < ge;
+  const float c = a.scale * kLog2e;
+  bf16x8_t qf[NC][4], df[NC][4];
+  diff_columns<T, D, NC>(qf, (const T*)a.q, row0, ge, head_q);
+  diff_columns<T, D, NC>(df, (const T*)a.d_o, row0, ge, head_q);
+  float l[2][NC], delta[2][NC];
+#pragma unroll
+  for (int q = 0; q < NC; ++q)
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      l[m][q] = lse[(int64_t)m * a.H * a.Nq + head_q + min(row0 + 16 * q + r, ge - 1)] * kLog2e;
+      delta[m][q] = 0.f;
+    }
+  Tiles tiles;
+  tiles.start(lds, (const T*)a.k + (head_k + gs) * D, (const T*)a.v + (head_k + gs) * D, n);
+  for (int st = 0; st < (n + 31) >> 5; ++st) {
+    tiles.ready(st);
+    if (!active) continue;
+    const int left = n - 32 * st;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      floatx4_t s[2][NC], dp[NC];
+      diff_products<T, D>(tiles, t, qf, df, s, dp);
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int q = 0; q < NC; ++q) {
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float p = fast_exp2(fmaf(s[m][q][i], c, -l[m][q]));
+            sum = fmaf(8 * g + 4 * t + i >= left ? 0.f : p, dp[q][i], sum);
+          }
+          delta[m][q] += sum;
+        }
+    }
+  }
+  tiles.finish();
+  if (!active) return;
+#pragma unroll
+  for (int q = 0; q < NC; ++q) {
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      delta[m][q] += __shfl_xor(delta[m][q], 16, kWave);
+      delta[m][q] += __shfl_xor(delta[m][q], 32, kWave);
+    }
+    const int row = row0 + 16 * q + r;
+    if (row < ge && g == 0) out[head_q + row] = floatx4_t{l[0][q], l[1][q], -delta[0][q], delta[1][q] - delta[0][q]};
   }
 }
 
@@ -473,18 +564,7 @@ __device__ __forceinline__ void diff_dq_block(DiffBwd a, int block, int piece, t
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         floatx4_t s[2][NC], dp[NC];
-#pragma unroll
-        for (int kb = 0; kb < 2 * KB; ++kb) {
-          const Frag<T> f = tiles.nat(0, t, kb);
-#pragma unroll
-          for (int q = 0; q < NC; ++q) s[kb / KB][q] = mma(f, qf[q][kb], kb % KB == 0 ? floatx4_t{0.f, 0.f, 0.f, 0.f} : s[kb / KB][q]);
-        }
-#pragma unroll
-        for (int kb = 0; kb < 2 * KB; ++kb) {
-          const Frag<T> f = tiles.nat(1, t, kb);
-#pragma unroll
-          for (int q = 0; q < NC; ++q) dp[q] = mma(f, df[q][kb], kb == 0 ? floatx4_t{0.f, 0.f, 0.f, 0.f} : dp[q]);
-        }
+        diff_products<T, D>(tiles, t, qf, df, s, dp);
 #pragma unroll
         for (int q = 0; q < NC; ++q) {
           float sum = 0.f;   // four by themselves: fewer roundings at the size of the whole sum
@@ -583,18 +663,7 @@ __global__ __launch_bounds__(256, 1) void diff_dkdv_f32_kernel(DiffBwd a) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         floatx4_t s[2][NC], dp[NC];
-#pragma unroll
-        for (int kb = 0; kb < 2 * KB; ++kb) {
-          const Frag<T> f = tiles.nat(0, t, kb);
-#pragma unroll
-          for (int k = 0; k < NC; ++k) s[kb / KB][k] = mma(f, kf[k][kb], kb % KB == 0 ? floatx4_t{0.f, 0.f, 0.f, 0.f} : s[kb / KB][k]);
-        }
-#pragma unroll
-        for (int kb = 0; kb < 2 * KB; ++kb) {
-          const Frag<T> f = tiles.nat(1, t, kb);
-#pragma unroll
-          for (int k = 0; k < NC; ++k) dp[k] = mma(f, vf[k][kb], kb == 0 ? floatx4_t{0.f, 0.f, 0.f, 0.f} : dp[k]);
-        }
+        diff_products<T, D>(tiles, t, kf, vf, s, dp);
         floatx4_t rc[4];
 #pragma unroll
         for (int v = 0; v < 4; ++v) rc[v] = tiles.rows(v, 8 * g + 4 * t);
@@ -967,7 +1036,8 @@ extern "C" int moga_diff_attn_bwd(const void* d_oh, const void* qh, const void* 
   b.tile_start = tk;
 #define MOGA_DIFF_BWD(T, D)                                                                                                            \
   do {                                                                                                                                 \
-    diff_rows_kernel<T, D><<<(unsigned)((rows + 15) / 16), 256, 0, st>>>((const T*)d_oh, parts, lse, rows, rc, share);                  \
+    if (sizeof(T) == 2 && Nk <= kDeltaKeys * G) diff_delta_kernel<<<(unsigned)q_blocks, 256, 0, st>>>(a, lse, rc);                      \
+    else diff_rows_kernel<T, D><<<(unsigned)((rows + 15) / 16), 256, 0, st>>>((const T*)d_oh, parts, lse, rows, rc, share);             \
     if constexpr (sizeof(T) == 4) {                                                                                                    \
       diff_dq_f32_kernel<D><<<dim3((unsigned)q_blocks, split.q), 256, 0, st>>>(a);                                                     \
       if (Nk > 0) diff_dkdv_f32_kernel<D><<<dim3((unsigned)k_blocks, split.k), 256, 0, st>>>(b);                                        \

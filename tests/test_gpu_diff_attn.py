@@ -223,6 +223,21 @@ def test_rows_behind_the_last_group_stay(D, dtype):
     ref.within(dlam, *want["dlam"], "dlam")
 
 
+@pytest.mark.parametrize("n", [12, 70, 250])
+def test_gradients_of_short_groups(n):
+    """Two roundings to bf16 lie between the formulas and dQ or dK: dS as an operand and the result, sqrt(2) of the result's own.  The operand's is not
+    centred as dS is: keys drawn towards a query, (spread^2 scale)^2 64 of spread^2 64 = 3.5 % more, sqrt(2.035) = 1.427; 2 % for a finite sum."""
+    H, G = 12, max(3, 1500 // n)
+    cu = _cu([n] * G)
+    q, k, v, do, lam = _inputs(H, 128, torch.bfloat16, cu, cu, n)
+    got = _run(q, k, v, do, lam, cu, cu, 0.125)
+    want = ref.diff_all(q.double(), k.double(), v.double(), lam.double(), do.double(), cu, cu, 0.125, ref.HALF_STEP[q.dtype])
+    for name in ("dq", "dk"):
+        r = want[name][0]
+        own = (r.bfloat16().double() - r).norm()
+        assert (got[name].double() - r).norm() <= 1.455 * own, name
+
+
 def test_gradient_of_lambda_over_many_rows():
     """60,000 rows whose parts have either sign: errors of single rows average out, a common one adds up.  An eighth of u a row, common to all, is
     60,000 u / 8 of a sum of some 0.4 sqrt(60,000): 4.6e-6."""
