@@ -874,9 +874,9 @@ size_t tile_bytes(int G) { return G > MOGA_MAX_GROUPS ? round_up(((size_t)G + 1)
 // 8 groups 70 instead of 61.
 // fp32, whose steps take ten times as long: none under 64 rows, and as many as make the fullest CU's work least: its blocks (an XCD deals its
 // share out to 32 CUs) times a block's steps and what starting it costs, in microseconds, and the traffic of the partial results.  One block a
-// CU takes 1.6 times what its products need.  Backward, whole and in pieces: 1,000 x 2 x 64 172 and 65 us; pieces for two blocks a CU of 128
-// rows and more instead: 6,000 x 4 x 128, 8 groups forward 175 instead of 156 and backward 463 instead of 389, 256 x 2 x 128 28 and 61 instead of
-// 22 and 44.
+// CU takes 1.6 times what it would beside two others, two 1.1.  Groups of unequal length have some more tiles: half the cost is that of 5 % more.
+// Backward, whole and in pieces: 1,000 x 2 x 64 172 and 69 us; pieces for two blocks a CU of 128 rows and more instead: 6,000 x 4 x 128,
+// 8 groups forward 175 instead of 156 and backward 463 instead of 389, 256 x 2 x 128 28 and 61 instead of 22 and 44.
 int diff_pieces(int64_t N, int64_t other, int H, int G, int rows, int D, int dtype) {
   if (dtype != MOGA_F32) {
     const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(max_tiles(N, G, rows), N)) * H;
@@ -884,11 +884,15 @@ int diff_pieces(int64_t N, int64_t other, int H, int G, int rows, int D, int dty
   }
   const int64_t tiles = (std::min(N, G * (((N + G - 1) / G + rows - 1) / rows)) * H + 7) / 8, most = std::min<int64_t>(16, other / G / 64);
   const double step = D * 0.02, start = 2 * step, traffic = (double)N * H * D * 16 / 6e6;
+  auto fullest = [](double blocks) {   // of an XCD
+    const double k = std::ceil(blocks / 32);
+    return k <= 1 ? 1.6 : k == 2 ? 2.2 : k;
+  };
   int best = 1;
   double least = INFINITY;
   for (int p = 1; p <= most && tiles * p <= kCus; ++p) {
-    const int64_t fullest = (tiles * p + 31) / 32;
-    const double cost = (fullest == 1 ? 1.6 : (double)fullest) * (other / G / 32. / p * step + start) + (p > 1 ? p * traffic : 0.);
+    const double block = other / G / 32. / p * step + start;
+    const double cost = 0.5 * (fullest(tiles * p) + fullest(1.05 * tiles * p)) * block + (p > 1 ? p * traffic : 0.);
     if (cost < least) least = cost, best = p;
   }
   return best;
