@@ -839,13 +839,18 @@ __global__ __launch_bounds__(1024) void diff_dlambda_kernel(const float* __restr
   __shared__ float acc[16];
   const float* p = share + blockIdx.x * Nq;
   const int n = Nq > 0 ? cu_q[G] : 0;
-  float u[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};   // eight loads on their way
-  int i = threadIdx.x;
-  for (; i + 7 * 1024 < n; i += 8 * 1024)
+  constexpr int U = 16;   // loads on their way
+  float u[U];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) u[k] += p[i + 1024 * k];
-  for (; i < n; i += 1024) u[0] += p[i];
-  float s = wave_sum(((u[0] + u[1]) + (u[2] + u[3])) + ((u[4] + u[5]) + (u[6] + u[7])));
+  for (int k = 0; k < U; ++k) u[k] = 0.f;
+  for (int i = threadIdx.x; i < n; i += U * 1024)
+#pragma unroll
+    for (int k = 0; k < U; ++k) u[k] += i + 1024 * k < n ? p[i + 1024 * k] : 0.f;
+#pragma unroll
+  for (int h = U / 2; h > 0; h /= 2)
+#pragma unroll
+    for (int k = 0; k < h; ++k) u[k] += u[k + h];
+  float s = wave_sum(u[0]);
   if ((threadIdx.x & 63) == 0) acc[threadIdx.x >> 6] = s;
   __syncthreads();
   if (threadIdx.x < 64) {
