@@ -899,23 +899,31 @@ using torch::autograd::variable_list;
 
 Tensor or_empty(const OptTensor& t) { return t ? *t : Tensor(); }
 OptTensor or_none(const Tensor& t) { return t.defined() ? OptTensor(t) : std::nullopt; }
+// Contiguous and where a C call may read it: a part of a longer tensor (a concatenation's gradient, say) can begin at any element.
+Tensor aligned(const Tensor& t) {
+  const Tensor c = t.contiguous();
+  return (uintptr_t)c.data_ptr() % 16 ? c.clone() : c;
+}
 
 struct LayerNorm : public torch::autograd::Function<LayerNorm> {
   static Tensor forward(AutogradContext* ctx, const Tensor& x, const OptTensor& w, const OptTensor& b, double eps) {
-    require(x);
+    require(x, w, b);
     need(x.dim() >= 1, "x: at least one dimension");
     const int64_t C = x.size(-1);
     need(C >= 1, "x: an empty last dimension");
-    const Tensor rows = x.view({x.numel() / C, C});
-    auto [y, mean, rstd] = layer_norm_fwd(rows, w, b, eps, true, std::nullopt);
-    ctx->save_for_backward({rows, or_empty(w), *mean, *rstd});
+    const Tensor rows = aligned(x.view({x.numel() / C, C}));
+    OptTensor wa, ba;
+    if (w) wa = aligned(*w);
+    if (b) ba = aligned(*b);
+    auto [y, mean, rstd] = layer_norm_fwd(rows, wa, ba, eps, true, std::nullopt);
+    ctx->save_for_backward({rows, or_empty(wa), *mean, *rstd});
     ctx->saved_data["bias"] = b.has_value();
     return y.view(x.sizes());
   }
   static variable_list backward(AutogradContext* ctx, const variable_list& grads) {
     const auto s = ctx->get_saved_variables();
     const bool bias = ctx->saved_data["bias"].toBool();
-    const Tensor d_y = grads[0].contiguous();
+    const Tensor d_y = aligned(grads[0]);
     // inputs are counted without those that are absent
     const bool dw = (s[1].defined() && ctx->needs_input_grad(1)) || (bias && ctx->needs_input_grad(s[1].defined() ? 2 : 1));
     auto [d_x, d_w, d_b] = layer_norm_bwd(d_y.view(s[0].sizes()), s[0], or_none(s[1]), s[2], s[3], dw, std::nullopt);
@@ -937,8 +945,8 @@ struct Rotary : public torch::autograd::Function<Rotary> {
     const auto s = ctx->get_saved_variables();
     const auto how = ctx->saved_data["how"].toDoubleVector();
     OptTensor dq, dk;
-    if (grads[0].defined()) dq = grads[0].contiguous();
-    if (grads[1].defined()) dk = grads[1].contiguous();
+    if (grads[0].defined()) dq = aligned(grads[0]);
+    if (grads[1].defined()) dk = aligned(grads[1]);
     variable_list out(7);
     if (!dq && !dk) return out;
     auto [a, b] = rotary_turn(dq, dk, Rotation(s[0], s[1], ctx->saved_data["pairs"].toIntVector(), how[0] != 0., how[1]), true, std::nullopt);
@@ -996,7 +1004,7 @@ struct DiffAttention : public torch::autograd::Function<DiffAttention> {
     const std::vector<double> a = ctx->saved_data["args"].toDoubleVector();
     const c10::OptionalDeviceGuard guard(qh.device());
     const int64_t H = qh.size(0), N = qh.size(1), D = qh.size(2);
-    Tensor d_o = grads[0].defined() ? grads[0].contiguous() : at::zeros({N, H, D}, qh.options());
+    Tensor d_o = grads[0].defined() ? aligned(grads[0]) : at::zeros({N, H, D}, qh.options());
     auto [d_oh, d_gate] = unpermute_bwd(d_o, oh, perm, gate, std::nullopt);
     auto [d_qh, d_kh, d_vh, d_lam] = diff_attn_bwd(d_oh, qh, kh, vh, parts, lse, lam, cu, cu, a[0], std::nullopt);
     Tensor d_q, d_k, d_v;

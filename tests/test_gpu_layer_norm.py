@@ -146,6 +146,24 @@ def test_autograd():
     assert torch.equal(bs.grad, db)
 
 
+def test_autograd_of_parts_of_longer_tensors():
+    """Rows, weights and gradients that begin at an odd element."""
+    C, n = 35, 9
+    x, dy, w, b = _inputs(2 * n, C, torch.float32, 21)
+    both = torch.cat([w, b]).requires_grad_(True)   # b begins at element 35
+    xs = x.clone().requires_grad_(True)
+    y = torch.cat([layer_norm(xs[:n], both[:C], both[C:], 1e-5), layer_norm(xs[n:], both[C:], both[:C], 1e-5)])
+    y.backward(dy)
+    parts = []
+    for r, ww, bb in ((slice(0, n), w, b), (slice(n, 2 * n), b, w)):
+        xr = x[r].clone()
+        yr, mean, rstd = mg.moga_layer_norm_fwd(xr, ww, bb, 1e-5)
+        assert torch.equal(y[r], yr)
+        parts.append(mg.moga_layer_norm_bwd(dy[r].clone(), xr, ww, mean, rstd))
+    assert torch.equal(xs.grad, torch.cat([p[0] for p in parts]))
+    assert torch.equal(both.grad, torch.cat([parts[0][1] + parts[1][2], parts[0][2] + parts[1][1]]))
+
+
 def test_refuses_tensors_that_do_not_fit():
     x, dy, w, b = _inputs(8, 64, torch.bfloat16, 1)
     with pytest.raises(ValueError):
