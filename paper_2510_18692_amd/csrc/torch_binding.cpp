@@ -934,8 +934,9 @@ struct LayerNorm : public torch::autograd::Function<LayerNorm> {
 struct Rotary : public torch::autograd::Function<Rotary> {
   static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& pos, const Tensor& freq,
                                const std::vector<int64_t>& pairs, bool interleaved, double factor) {
-    auto [qo, ko] = rotary_turn(q, k, Rotation(pos, freq, pairs, interleaved, factor), false, std::nullopt);
-    ctx->save_for_backward({pos, freq});
+    const Rotation how(aligned(pos), aligned(freq), pairs, interleaved, factor);   // positions of a piece of a sequence
+    auto [qo, ko] = rotary_turn(q, k, how, false, std::nullopt);
+    ctx->save_for_backward({how.pos, how.freq});
     ctx->saved_data["pairs"] = pairs;
     ctx->saved_data["how"] = std::vector<double>{interleaved ? 1. : 0., factor};
     ctx->set_materialize_grads(false);
@@ -974,7 +975,7 @@ struct DiffAttention : public torch::autograd::Function<DiffAttention> {
     need_like(lam, q, {q.size(1)}, at::kFloat, "lambda");
     need(pos.has_value() == freq.has_value(), "positions and inv_freq");
     std::optional<Rotation> how;
-    if (pos) how.emplace(*pos, *freq, pairs, interleaved, factor);
+    if (pos) how.emplace(aligned(*pos), aligned(*freq), pairs, interleaved, factor);
     auto [group, gate, probs, logits] = route(x, w, std::nullopt, true, false, std::nullopt);
     Tensor qh, kh, vh;
     Permuted p;
@@ -989,7 +990,8 @@ struct DiffAttention : public torch::autograd::Function<DiffAttention> {
     Tensor o = unpermute(oh, p.perm, gate, std::nullopt, std::nullopt);
     Tensor loss = alpha ? at::empty({}, x.options().dtype(at::kFloat)) : at::zeros({}, x.options().dtype(at::kFloat)), frac;
     if (alpha) frac = std::get<0>(balance_into(loss, group, gate, M, *alpha, std::nullopt));
-    ctx->save_for_backward({x, w, group, gate, *probs, p.perm, p.cu_seqlens, qh, kh, vh, lam, oh, *parts, lse, frac, or_empty(pos), or_empty(freq)});
+    ctx->save_for_backward({x, w, group, gate, *probs, p.perm, p.cu_seqlens, qh, kh, vh, lam, oh, *parts, lse, frac, how ? how->pos : Tensor(),
+                            how ? how->freq : Tensor()});
     ctx->saved_data["args"] = std::vector<double>{scale, alpha.value_or(0.), alpha ? 1. : 0., grad_x ? 1. : 0., interleaved ? 1. : 0., factor};
     ctx->saved_data["pairs"] = pairs;
     ctx->mark_non_differentiable({group});

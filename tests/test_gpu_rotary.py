@@ -130,6 +130,18 @@ def test_autograd():
     assert torch.equal(torch.autograd.grad(yk, b, dk)[0], ek)
 
 
+def test_autograd_at_positions_of_a_piece():
+    """Positions that are a slice of a longer list begin at any element."""
+    q, k, d = _rnd(1, 21, 2, 64), _rnd(2, 21, 1, 64), _rnd(3, 21, 2, 64)
+    pos = torch.arange(100, dtype=torch.int32).cuda()
+    freq, _ = mg.moga_rotary_freqs(64)
+    a = q.clone().requires_grad_(True)
+    yq, yk = rotary(a, k, pos[37:58], freq)
+    eq, ek = mg.moga_rotary_fwd(q, k, pos[37:58].clone(), freq)
+    assert torch.equal(yq, eq) and torch.equal(yk, ek)
+    assert torch.equal(torch.autograd.grad(yq, a, d)[0], mg.moga_rotary_bwd(d, None, pos[37:58].clone(), freq)[0])
+
+
 def test_nothing_to_do_and_refusals():
     freq, _ = mg.moga_rotary_freqs(128)
     e = torch.empty((0, 3, 128), device="cuda")
