@@ -50,15 +50,24 @@ __device__ __forceinline__ float to_f32(unsigned short v) { return bf16_bits_to_
 __device__ __forceinline__ void from_f32(float& d, float v) { d = v; }
 __device__ __forceinline__ void from_f32(unsigned short& d, float v) { d = f32_to_bf16_bits(v); }
 
-// Columns col .. col + V - 1 of a row of C, as they lie there; zeros past its end.
+// Columns col .. col + V - 1 of a row of C, as they lie there, with the next row's first ones past its end (clear_past); zeros past the last row's.
+// Element by element, in every row's last piece, the loads would be waited for where they are issued: 4,099 x 1535 backward bf16 44 us
+// instead of 32, fp32 31 instead of 27.
 template <typename T>
-__device__ __forceinline__ Bytes16<T> load_part(const T* __restrict__ row, int col, int C) {
+__device__ __forceinline__ Bytes16<T> load_part(const T* __restrict__ row, int col, int C, bool last_row) {
   constexpr int V = kPer16<T>;
-  if (col + V <= C) return *(const Bytes16<T>*)(row + col);
+  if (col + V <= C || (col < C && C >= V && !last_row)) return *(const Bytes16<T>*)(row + col);
   float f[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) f[i] = col + i < C ? to_f32(row[col + i]) : 0.f;
   return pack(f);   // exact: values of T
+}
+template <int V>
+__device__ __forceinline__ void clear_past(float (&f)[V], int col, int C) {
+  if (col + V > C)
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (col + i >= C) f[i] = 0.f;
 }
 template <typename T, int V>
 __device__ __forceinline__ void store_part(T* __restrict__ row, int col, int C, const float (&f)[V]) {
@@ -138,7 +147,7 @@ __global__ __launch_bounds__(LANES ? 256 : 64 * kMaxWaves) void layer_norm_fwd_k
 #pragma unroll
   for (int p = 0; p < PARTS; ++p) {
     col[p] = (p * d.lanes + d.lane) * V;
-    if (d.row < N) next[p] = load_part(x + d.row * C, col[p], C);
+    if (d.row < N) next[p] = load_part(x + d.row * C, col[p], C, d.row + 1 == N);
   }
 #pragma unroll
   for (int p = 0; p < PARTS; ++p) {
@@ -150,10 +159,13 @@ __global__ __launch_bounds__(LANES ? 256 : 64 * kMaxWaves) void layer_norm_fwd_k
     float f[PARTS][V];
     float s[1] = {0.f};
 #pragma unroll
-    for (int p = 0; p < PARTS; ++p) unpack(next[p], f[p]);
+    for (int p = 0; p < PARTS; ++p) {
+      unpack(next[p], f[p]);
+      clear_past(f[p], col[p], C);
+    }
     if (d.row + d.step < N)
 #pragma unroll
-      for (int p = 0; p < PARTS; ++p) next[p] = load_part(x + (d.row + d.step) * C, col[p], C);
+      for (int p = 0; p < PARTS; ++p) next[p] = load_part(x + (d.row + d.step) * C, col[p], C, d.row + d.step + 1 == N);
 #pragma unroll
     for (int p = 0; p < PARTS; ++p)
 #pragma unroll
@@ -201,8 +213,8 @@ __global__ __launch_bounds__(LANES ? 256 : 64 * kMaxWaves) void layer_norm_bwd_k
   auto fetch = [&](int64_t row) {
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) {
-      next_x[p] = load_part(x + row * C, col[p], C);
-      next_g[p] = load_part(dy + row * C, col[p], C);
+      next_x[p] = load_part(x + row * C, col[p], C, row + 1 == N);
+      next_g[p] = load_part(dy + row * C, col[p], C, row + 1 == N);
     }
     next_mu = mean[row];
     next_r = rstd[row];
@@ -224,6 +236,8 @@ __global__ __launch_bounds__(LANES ? 256 : 64 * kMaxWaves) void layer_norm_bwd_k
     for (int p = 0; p < PARTS; ++p) {
       unpack(next_x[p], f[p]);
       unpack(next_g[p], g[p]);
+      clear_past(f[p], col[p], C);
+      clear_past(g[p], col[p], C);
     }
     const float mu = next_mu, r = next_r;
     if (d.row + d.step < N) fetch(d.row + d.step);
