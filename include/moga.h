@@ -571,6 +571,7 @@ int moga_layer_norm_bwd(const void* d_y, const void* x, int dtype, const float* 
  * positions [axes, N] int32 (any value), axes in [1, 4]: axis a turns the next axis_pairs[a] pairs (axis_pairs: a HOST array whose sum is
  * R / 2, NULL for one axis), e.g. (frame, row, column) of a latent grid.  inv_freq [R / 2] double on the device (moga_rotary_build_freqs per
  * axis, one after the other).  Angles are reduced in 64 bits, so that far positions keep their accuracy.
+ * For differential attention the maps of a head are turned by themselves: call it with 2 Hq and 2 Hk heads of D / 2 channels (the same tensors).
  * q, qo [N, Hq, D], k, ko [N, Hk, D] token order; Hq or Hk may be 0 (then its pointers are ignored).  D a multiple of 8, at most 256;
  * dtype F32 or BF16; N < 2^28.  Outputs must not alias inputs.
  */
@@ -597,6 +598,21 @@ int moga_rotary_permute_bwd(const void* d_qh, const void* d_kh, const void* d_vh
                             const double* inv_freq, int R, int interleaved, float factor, void* d_q, void* d_k, void* d_v, void* stream);
 
 /*
+ * moga_rotary_permute_fwd/_bwd for differential attention (moga_diff_attn_fwd): its two maps are attentions of their own, from the two halves of
+ * a head's channels of q and k, so each half is turned within itself, as a head of D / 2 channels would be (a rotation of the whole head
+ * would mix the maps, or give one the fast pairs and the other the slow ones).  R channels of each map are turned, R <= D / 2; D a
+ * multiple of 16.  each_map 0: inv_freq [R / 2] turns both maps alike (axis_pairs: sum R / 2); else inv_freq [R] has the first map's R / 2 pairs, then the
+ * second's (axis_pairs: sum R).
+ */
+int moga_rotary_permute_maps_fwd(const void* q, const void* k, const void* v, int dtype, int64_t N, int H, int D, const int32_t* perm,
+                                 const int32_t* positions, int axes, const int* axis_pairs_or_null, const double* inv_freq, int R,
+                                 int each_map, int interleaved, float factor, void* qh, void* kh, void* vh, void* stream);
+int moga_rotary_permute_maps_bwd(const void* d_qh, const void* d_kh, const void* d_vh, int dtype, int64_t N, int H, int D,
+                                 const int32_t* perm, const int32_t* positions, int axes, const int* axis_pairs_or_null,
+                                 const double* inv_freq, int R, int each_map, int interleaved, float factor, void* d_q, void* d_k, void* d_v,
+                                 void* stream);
+
+/*
  * Angles per position of R / 2 pairs, on the HOST, in 64 bits: inv_freq[i] = base^(-2 i / R) (inv_freq: HOST array of R / 2), for contexts
  * scale_factor (>= 1) times as long as the original one
  *   PLAIN:  as they are (the other arguments are not read)
@@ -611,7 +627,8 @@ int moga_rotary_build_freqs(int R, double base, int scaling, double scale_factor
 
 /*
  * Differential attention inside groups: the difference of two attention maps, one from the first and one from the second half of a head's
- * channels of Q and K, over the same values (Q = [Q1 | Q2], K = [K1 | K2] of D / 2 channels each):
+ * channels of Q and K, over the same values (Q = [Q1 | Q2], K = [K1 | K2] of D / 2 channels each; rotary positions turn each by itself,
+ * moga_rotary_permute_maps_fwd):
  *   A_m = softmax(softmax_scale * Q_m K_m^T) inside a group,   oh = A_1 vh - lambda[h] * A_2 vh
  *   parts[m] = A_m vh  [2, H, Nq, D] fp32 (NULL to skip; the backward needs it)
  *   lse[m][h][j] = log sum_k exp(softmax_scale * Q_m . K_m)  [2, H, Nq] fp32

@@ -25,16 +25,17 @@ def layer_norm(x, weight=None, bias=None, eps=1e-6):
     return mg._nat.layer_norm(x, weight, bias, eps)
 
 
-def rotary(q, k, positions, inv_freq, axis_pairs=None, interleaved=False, factor=1.0):
-    """Rotary positions of q [N, Hq, D] and k [N, Hk, D] (binding.moga_rotary_fwd) -> (qo, ko)."""
-    return mg._nat.rotary_apply(q, k, positions, inv_freq, axis_pairs or [], interleaved, factor)
+def rotary(q, k, positions, inv_freq, axis_pairs=None, interleaved=False, factor=1.0, maps=1):
+    """Rotary positions of q [N, Hq, D] and k [N, Hk, D] (binding.moga_rotary_fwd; maps=2 before moga_diff_attention) -> (qo, ko)."""
+    return mg._nat.rotary_apply(q, k, positions, inv_freq, axis_pairs or [], interleaved, factor, maps)
 
 
 def moga_diff_attention(x, w, q, k, v, lam, softmax_scale, balance_alpha=None, grad_x=False, positions=None, inv_freq=None, axis_pairs=None,
                         interleaved=False, factor=1.0):
     """moga_attention with differential attention in the groups: the two halves of a head's channels are two maps, lam f32 [H] the weight of
-    the second (moga_diff_attn_fwd); gradients flow to lam as well.  With positions and inv_freq (binding.moga_rotary_freqs) q and k are
-    rotated on their way into the groups.  -> (o [N, H, D], balancing loss or None, group [N]).
+    the second (moga_diff_attn_fwd); gradients flow to lam as well.  With positions and inv_freq q and k are rotated on their way into the groups, each map
+    within its own D / 2 channels: inv_freq of at most D / 4 pairs (binding.moga_rotary_freqs(D // 2)) turns both maps alike, one of D / 2 pairs has the
+    first map's and then the second's (binding.moga_rotary_permute_fwd, maps=2).  -> (o [N, H, D], balancing loss or None, group [N]).
     A step whose backward is captured into a graph: let go of the eager results of the same leaves before the capture (torch keeps the stream
     on which a leaf was first used, and a capture may not join work of another)."""
     o, loss, group = mg._nat.diff_attention(x, w, q, k, v, lam, softmax_scale, balance_alpha, grad_x, positions, inv_freq, axis_pairs or [],

@@ -102,6 +102,10 @@ _SIGNATURES = {
                                        _vp]),
     "moga_rotary_permute_bwd": (_i32, [_vp, _vp, _vp, _i32, _i64, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _i32, _i32, _f32, _vp, _vp, _vp,
                                        _vp]),
+    "moga_rotary_permute_maps_fwd": (_i32, [_vp, _vp, _vp, _i32, _i64, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _i32, _i32, _i32, _f32, _vp, _vp,
+                                            _vp, _vp]),
+    "moga_rotary_permute_maps_bwd": (_i32, [_vp, _vp, _vp, _i32, _i64, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _i32, _i32, _i32, _f32, _vp, _vp,
+                                            _vp, _vp]),
     "moga_rotary_build_freqs": (_i32, [_i32, _f64, _i32, _f64, _f64, _f64, _f64, _vp, _vp]),
     "moga_diff_attn_fwd": (_i32, [_vp, _vp, _vp, _i32, _i64, _i64, _i32, _i32, _vp, _vp, _vp, _i32, _f32, _vp, _vp, _vp, _vp, _sz, _vp]),
     "moga_diff_attn_bwd": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i64, _i64, _i32, _i32, _vp, _vp, _vp, _i32, _f32, _vp, _vp, _vp,
@@ -456,24 +460,27 @@ def moga_rotary_freqs(rot_dims, base=10000.0, scaling=None, scale_factor=1.0, or
     return torch.from_numpy(np.concatenate(parts)).to(device), factor.value
 
 
-def moga_rotary_fwd(q, k, positions, inv_freq, axis_pairs=None, interleaved=False, factor=1.0, stream=None):
-    """q [N, Hq, D], k [N, Hk, D] (or None), positions i32 [N] or [axes, N], inv_freq f64 [R / 2] -> (qo, ko)"""
-    return _nat.rotary(q, k, positions, inv_freq, axis_pairs or [], interleaved, factor, False, _st(stream))
+def moga_rotary_fwd(q, k, positions, inv_freq, axis_pairs=None, interleaved=False, factor=1.0, stream=None, maps=1):
+    """q [N, Hq, D], k [N, Hk, D] (or None), positions i32 [N] or [axes, N], inv_freq f64 [R / 2] -> (qo, ko)
+    maps=2 (differential attention): each half of a head's channels is turned by itself, with inv_freq of at most D / 4 pairs for both."""
+    return _nat.rotary(q, k, positions, inv_freq, axis_pairs or [], interleaved, factor, maps, False, _st(stream))
 
 
-def moga_rotary_bwd(d_qo, d_ko, positions, inv_freq, axis_pairs=None, interleaved=False, factor=1.0, stream=None):
+def moga_rotary_bwd(d_qo, d_ko, positions, inv_freq, axis_pairs=None, interleaved=False, factor=1.0, stream=None, maps=1):
     """-> (d_q, d_k)"""
-    return _nat.rotary(d_qo, d_ko, positions, inv_freq, axis_pairs or [], interleaved, factor, True, _st(stream))
+    return _nat.rotary(d_qo, d_ko, positions, inv_freq, axis_pairs or [], interleaved, factor, maps, True, _st(stream))
 
 
-def moga_rotary_permute_fwd(q, k, v, perm, positions, inv_freq, axis_pairs=None, interleaved=False, factor=1.0, stream=None):
-    """moga_rotary_fwd of q and k and the gather of moga_permute in one launch: q, k, v [N, H, D] -> (qh, kh, vh [H, N, D])"""
-    return _nat.rotary_permute(q, k, v, perm, positions, inv_freq, axis_pairs or [], interleaved, factor, False, _st(stream))
+def moga_rotary_permute_fwd(q, k, v, perm, positions, inv_freq, axis_pairs=None, interleaved=False, factor=1.0, stream=None, maps=1):
+    """moga_rotary_fwd of q and k and the gather of moga_permute in one launch: q, k, v [N, H, D] -> (qh, kh, vh [H, N, D])
+    maps=2 (differential attention): each half of a head's channels is turned by itself (moga_rotary_permute_maps_fwd), with inv_freq of at most
+    D / 4 pairs for both, or of D / 2 pairs, the first half's and then the second's."""
+    return _nat.rotary_permute(q, k, v, perm, positions, inv_freq, axis_pairs or [], interleaved, factor, maps, False, _st(stream))
 
 
-def moga_rotary_permute_bwd(d_qh, d_kh, d_vh, perm, positions, inv_freq, axis_pairs=None, interleaved=False, factor=1.0, stream=None):
+def moga_rotary_permute_bwd(d_qh, d_kh, d_vh, perm, positions, inv_freq, axis_pairs=None, interleaved=False, factor=1.0, stream=None, maps=1):
     """-> (d_q, d_k, d_v) each [N, H, D]"""
-    return _nat.rotary_permute(d_qh, d_kh, d_vh, perm, positions, inv_freq, axis_pairs or [], interleaved, factor, True, _st(stream))
+    return _nat.rotary_permute(d_qh, d_kh, d_vh, perm, positions, inv_freq, axis_pairs or [], interleaved, factor, maps, True, _st(stream))
 
 
 def moga_diff_attn_fwd(qh, kh, vh, lam, cu_seqlens_q, cu_seqlens_k, softmax_scale, want_parts=True, stream=None):

@@ -4,6 +4,7 @@
 // turned by the angle p * inv_freq[i] and scaled:
 //   y1 = f (x1 cos - x2 sin), y2 = f (x2 cos + x1 sin); the backward turns by minus the angle.
 // With several axes a token has a position on each, and every axis a run of pairs.
+// In maps (differential attention) each half of a head is turned by itself, as a head of D / 2 channels would be.
 //
 // Angles: the product and its reduction to a part of a turn in 64 bits (at position 500,000 a product in 32 bits is 0.03 radians off), then
 // sine and cosine in 32 bits, once per token and pair, in LDS, for all heads of q and k.
@@ -55,25 +56,28 @@ struct RotaryArgs {
   void* dst[3];
   int heads[3], first[4];   // heads of each; first[i]: those before it, first[3] of all
   const int32_t* pos;       // [axes][N]
-  const double* inv_freq;   // [R / 2]
+  const double* inv_freq;   // [pairs]
   const int32_t* perm;      // sorted order: slot -> token
   int64_t N;
-  int D, R, axes, bound[kMaxAxes];   // bound[a]: pairs of the axes up to a
+  int D, R, axes, bound[kMaxAxes];   // R: turned channels of a head, or of each map; bound[a]: pairs of the axes up to a
+  int pairs, second;                 // pairs that have an angle; in maps: which of them is the second map's first
   float factor, sign;
   int tokens, heads_each;   // of a block
 };
 
 // LAYOUT 0: token order to token order; 1: token order to sorted [H, N, D]; 2: sorted to token order.
 // A block takes `tokens` rows of `heads_each` heads.  WHOLE: pairs lie within a chunk of 16 bytes, or are the same places of two chunks.
-template <typename T, bool INTERLEAVED, bool WHOLE, int LAYOUT>
+// MAPS: a head is two maps of whole chunks.
+template <typename T, bool INTERLEAVED, bool WHOLE, int LAYOUT, bool MAPS>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
   constexpr int V = Chunk<T>::V;
-  extern __shared__ floatx2_t turn[];   // [tokens][R / 2]: cosine, sine, times the factor
+  extern __shared__ floatx2_t turn[];   // [tokens][pairs]: cosine, sine, times the factor
   const int half = a.R / 2, chunks = a.D / V;
   const int64_t row0 = (int64_t)blockIdx.x * a.tokens;
   const int rows = (int)min((int64_t)a.tokens, a.N - row0);
-  for (int i = threadIdx.x; i < rows * half; i += 256) {
-    const int r = i / half, p = i - r * half;
+  const int angles = MAPS ? a.pairs : half;
+  for (int i = threadIdx.x; i < rows * angles; i += 256) {
+    const int r = i / angles, p = i - r * angles;
     const int64_t tok = LAYOUT == 0 ? row0 + r : a.perm[row0 + r];
     int axis = 0;
 #pragma unroll
@@ -94,6 +98,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
   for (int i = threadIdx.x; i < rows * nh * chunks; i += 256) {
     const int r = LAYOUT == 1 ? in : out, hh = h0 + (LAYOUT == 1 ? out : in);
     const int at = chunk;
+    const bool second = MAPS && at >= chunks / 2;
+    const int own = second ? at - chunks / 2 : at;   // of its head or map
     chunk += chunk_step;
     in += in_step;
     out += out_step;
@@ -105,9 +111,9 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
     const int64_t in_tokens = (tok * H + head) * a.D, in_sorted = ((int64_t)head * a.N + slot) * a.D;
     const T* __restrict__ src = (const T*)a.src[which] + (LAYOUT == 2 ? in_sorted : in_tokens);
     T* __restrict__ dst = (T*)a.dst[which] + (LAYOUT == 1 ? in_sorted : in_tokens);
-    const floatx2_t* t = turn + r * half;
+    const floatx2_t* t = turn + r * angles + (second ? a.second : 0);
     const uintx4_t w = *(const uintx4_t*)(src + at * V);
-    if (which == 2 || at * V >= a.R) {
+    if (which == 2 || own * V >= a.R) {
       *(uintx4_t*)(dst + at * V) = w;
       continue;
     }
@@ -116,7 +122,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
     if constexpr (INTERLEAVED) {
 #pragma unroll
       for (int e = 0; e < V; e += 2) {
-        const int p = (at * V + e) / 2;
+        const int p = (own * V + e) / 2;
         if (p < half) {
           const floatx2_t cs = t[p];
           y[e] = f[e] * cs[0] - f[e + 1] * cs[1];
@@ -127,10 +133,10 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
         }
       }
     } else if constexpr (WHOLE) {
-      const bool low = at < pairs;
-      const int c = low ? at : at - pairs;
+      const bool low = own < pairs;
+      const int c = low ? own : own - pairs;
       float o[V];   // the partners, which their own lane loads too: the second read is from L1
-      Chunk<T>::get(*(const uintx4_t*)(src + (low ? at + pairs : c) * V), o);
+      Chunk<T>::get(*(const uintx4_t*)(src + (low ? at + pairs : at - pairs) * V), o);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const floatx2_t cs = t[c * V + e];
@@ -139,11 +145,11 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
     } else {   // partners anywhere: read one by one
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const int d = at * V + e;
+        const int d = own * V + e;
         if (d < a.R) {
           const bool low = d < half;
           const floatx2_t cs = t[low ? d : d - half];
-          const float other = value(src[low ? d + half : d - half]);
+          const float other = value(src[at * V + e + (low ? half : -half)]);
           y[e] = low ? f[e] * cs[0] - other * cs[1] : f[e] * cs[0] + other * cs[1];
         } else {
           y[e] = f[e];
@@ -159,23 +165,25 @@ struct RotaryShape {
   int D, axes, R, interleaved, dtype;
   const int* axis_pairs;
   float factor;
+  int maps = 1, each = 0;   // maps of a head; each: with pairs of its own
+  int pairs() const { return R / 2 * (each ? maps : 1); }
 };
 
 int check_rotary(const RotaryShape& s) {
-  if (s.N < 0 || s.D < 1 || s.axes < 1 || s.R < 2 || s.R % 2 || s.R > s.D) return MOGA_ERR_INVALID_ARG;
+  if (s.N < 0 || s.D < 1 || s.axes < 1 || s.R < 2 || s.R % 2 || s.R > s.D / s.maps) return MOGA_ERR_INVALID_ARG;
   if (!(std::fabs(s.factor) < INFINITY)) return MOGA_ERR_INVALID_ARG;
   if (s.dtype != MOGA_F32 && s.dtype != MOGA_BF16) return MOGA_ERR_UNSUPPORTED;
-  if (s.D % 8 || s.D > kMaxHeadDim || s.axes > kMaxAxes || s.N >= ((int64_t)1 << 28)) return MOGA_ERR_UNSUPPORTED;
+  if (s.D % (8 * s.maps) || s.D > kMaxHeadDim || s.axes > kMaxAxes || s.N >= ((int64_t)1 << 28)) return MOGA_ERR_UNSUPPORTED;
   if (!s.axis_pairs) return s.axes == 1 ? MOGA_OK : MOGA_ERR_INVALID_ARG;
   int64_t sum = 0;
   for (int a = 0; a < s.axes; ++a) {
     if (s.axis_pairs[a] < 0) return MOGA_ERR_INVALID_ARG;
     sum += s.axis_pairs[a];
   }
-  return sum == s.R / 2 ? MOGA_OK : MOGA_ERR_INVALID_ARG;
+  return sum == s.pairs() ? MOGA_OK : MOGA_ERR_INVALID_ARG;
 }
 
-template <typename T, int LAYOUT>
+template <typename T, int LAYOUT, bool MAPS>
 int launch_rotary(RotaryArgs& a, const RotaryShape& s, hipStream_t st) {
   constexpr int V = Chunk<T>::V;
   const int heads = a.first[3], chunks = s.D / V;
@@ -188,10 +196,10 @@ int launch_rotary(RotaryArgs& a, const RotaryShape& s, hipStream_t st) {
   a.heads_each = (heads + parts - 1) / parts;
   const dim3 grid((unsigned)row_blocks, (unsigned)((heads + a.heads_each - 1) / a.heads_each));
   if (!grid_fits(row_blocks * grid.y, 256)) return MOGA_ERR_UNSUPPORTED;
-  const size_t lds = (size_t)a.tokens * (s.R / 2) * sizeof(floatx2_t);
-  if (s.interleaved) rotary_kernel<T, true, true, LAYOUT><<<grid, 256, lds, st>>>(a);
-  else if (s.R / 2 % V == 0) rotary_kernel<T, false, true, LAYOUT><<<grid, 256, lds, st>>>(a);
-  else rotary_kernel<T, false, false, LAYOUT><<<grid, 256, lds, st>>>(a);
+  const size_t lds = (size_t)a.tokens * a.pairs * sizeof(floatx2_t);
+  if (s.interleaved) rotary_kernel<T, true, true, LAYOUT, MAPS><<<grid, 256, lds, st>>>(a);
+  else if (s.R / 2 % V == 0) rotary_kernel<T, false, true, LAYOUT, MAPS><<<grid, 256, lds, st>>>(a);
+  else rotary_kernel<T, false, false, LAYOUT, MAPS><<<grid, 256, lds, st>>>(a);
   return launch_status();
 }
 
@@ -223,11 +231,15 @@ int rotary(const void* const (&src)[3], void* const (&dst)[3], const int (&heads
   a.D = s.D;
   a.R = s.R;
   a.axes = s.axes;
-  for (int x = 0, n = 0; x < kMaxAxes; ++x) a.bound[x] = n += !s.axis_pairs ? (x == 0 ? s.R / 2 : 0) : x < s.axes ? s.axis_pairs[x] : 0;
+  a.pairs = s.pairs();
+  a.second = s.each ? s.R / 2 : 0;
+  for (int x = 0, n = 0; x < kMaxAxes; ++x) a.bound[x] = n += !s.axis_pairs ? (x == 0 ? a.pairs : 0) : x < s.axes ? s.axis_pairs[x] : 0;
   a.factor = s.factor;
   a.sign = sign;
-#define MOGA_ROTARY(T) \
-  (layout == 0 ? launch_rotary<T, 0>(a, s, st) : layout == 1 ? launch_rotary<T, 1>(a, s, st) : launch_rotary<T, 2>(a, s, st))
+#define MOGA_ROTARY(T)                                                                                                              \
+  (s.maps == 2   ? layout == 1 ? launch_rotary<T, 1, true>(a, s, st) : launch_rotary<T, 2, true>(a, s, st)                          \
+   : layout == 0 ? launch_rotary<T, 0, false>(a, s, st)                                                                             \
+   : layout == 1 ? launch_rotary<T, 1, false>(a, s, st) : launch_rotary<T, 2, false>(a, s, st))
   return s.dtype == MOGA_F32 ? MOGA_ROTARY(float) : MOGA_ROTARY(unsigned short);
 #undef MOGA_ROTARY
 }
@@ -265,6 +277,22 @@ extern "C" int moga_rotary_permute_bwd(const void* d_qh, const void* d_kh, const
   if (H < 1) return MOGA_ERR_INVALID_ARG;
   return rotary({d_qh, d_kh, d_vh}, {d_q, d_k, d_v}, {H, H, H}, perm, 2, positions, inv_freq,
                 {N, D, axes, R, interleaved, dtype, axis_pairs, factor}, -1.f, (hipStream_t)stream);
+}
+
+extern "C" int moga_rotary_permute_maps_fwd(const void* q, const void* k, const void* v, int dtype, int64_t N, int H, int D, const int32_t* perm,
+                                            const int32_t* positions, int axes, const int* axis_pairs, const double* inv_freq, int R, int each_map,
+                                            int interleaved, float factor, void* qh, void* kh, void* vh, void* stream) {
+  if (H < 1) return MOGA_ERR_INVALID_ARG;
+  return rotary({q, k, v}, {qh, kh, vh}, {H, H, H}, perm, 1, positions, inv_freq,
+                {N, D, axes, R, interleaved, dtype, axis_pairs, factor, 2, each_map}, 1.f, (hipStream_t)stream);
+}
+
+extern "C" int moga_rotary_permute_maps_bwd(const void* d_qh, const void* d_kh, const void* d_vh, int dtype, int64_t N, int H, int D,
+                                            const int32_t* perm, const int32_t* positions, int axes, const int* axis_pairs, const double* inv_freq,
+                                            int R, int each_map, int interleaved, float factor, void* d_q, void* d_k, void* d_v, void* stream) {
+  if (H < 1) return MOGA_ERR_INVALID_ARG;
+  return rotary({d_qh, d_kh, d_vh}, {d_q, d_k, d_v}, {H, H, H}, perm, 2, positions, inv_freq,
+                {N, D, axes, R, interleaved, dtype, axis_pairs, factor, 2, each_map}, -1.f, (hipStream_t)stream);
 }
 
 // Host only.  All in 64 bits.

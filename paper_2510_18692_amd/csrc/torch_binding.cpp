@@ -655,18 +655,20 @@ std::tuple<Tensor, OptTensor, OptTensor> layer_norm_bwd(const Tensor& d_y, const
   return {d_x, d_w, d_b};
 }
 
-// What turns the pairs of a head: positions [axes, N] (or [N]), radians per position [R / 2], pairs of each axis.
+// What turns the pairs of a head, or (maps 2) of each half of one: positions [axes, N] (or [N]), radians per position of the pairs, pairs of each axis.
 struct Rotation {
   Tensor pos, freq;
   std::vector<int64_t> pairs;
   bool interleaved;
   double factor;
+  int64_t maps;
   std::vector<int> axis_pairs;
   int axes = 1;
 
-  Rotation(const Tensor& pos, const Tensor& freq, const std::vector<int64_t>& pairs, bool interleaved, double factor)
-      : pos(pos), freq(freq), pairs(pairs), interleaved(interleaved), factor(factor) {
+  Rotation(const Tensor& pos, const Tensor& freq, const std::vector<int64_t>& pairs, bool interleaved, double factor, int64_t maps)
+      : pos(pos), freq(freq), pairs(pairs), interleaved(interleaved), factor(factor), maps(maps) {
     require(pos, freq);
+    need(maps == 1 || maps == 2, "maps: 1 or 2");
     need_dims(freq, 1);
     need(pos.dim() == 1 || pos.dim() == 2, "positions: one or two dimensions");
     axes = pos.dim() == 1 ? 1 : to_int(pos.size(0));
@@ -680,6 +682,12 @@ struct Rotation {
   }
   const int* host_pairs() const { return axis_pairs.empty() ? nullptr : axis_pairs.data(); }
   int R() const { return 2 * to_int(freq.size(0)); }
+  // In maps of D / 2 channels: whether each has pairs of its own.
+  bool each_map(int64_t D) const {
+    const int64_t n = freq.size(0);
+    need(4 * n <= D || 2 * n == D, "inv_freq: at most D / 4 pairs for both maps, or D / 2, the first map's and then the second's");
+    return 4 * n > D;
+  }
 };
 
 std::tuple<OptTensor, OptTensor> rotary_turn(const OptTensor& q, const OptTensor& k, const Rotation& how, bool back, const OptStream& stream) {
@@ -689,18 +697,20 @@ std::tuple<OptTensor, OptTensor> rotary_turn(const OptTensor& q, const OptTensor
   const c10::OptionalDeviceGuard guard(first.device());
   const Call call(stream);
   need_dims(first, 3);
-  const int64_t N = first.size(0), D = first.size(2);
+  const int64_t N = first.size(0), D = first.size(2), maps = how.maps;
   how.fits(first, N);
   if (q && k) {
     need_dims(*k, 3);
     need_like(*k, first, {N, k->size(1), D}, first.scalar_type(), "k");
   }
+  need(maps == 1 || (D % 2 == 0 && 4 * how.freq.size(0) <= D), "inv_freq: at most D / 4 pairs for both maps");   // heads of D / 2 channels
   OptTensor qo, ko;
   if (q) qo = call.make(q->sizes(), *q);
   if (k) ko = call.make(k->sizes(), *k);
   if ((!q || q->size(1) == 0) && (!k || k->size(1) == 0)) return {qo, ko};
   check(back ? "moga_rotary_bwd" : "moga_rotary_fwd",
-        (back ? moga_rotary_bwd : moga_rotary_fwd)(ptr(q), ptr(k), dt(first), N, q ? to_int(q->size(1)) : 0, k ? to_int(k->size(1)) : 0, to_int(D),
+        (back ? moga_rotary_bwd : moga_rotary_fwd)(ptr(q), ptr(k), dt(first), N, q ? to_int(maps * q->size(1)) : 0, k ? to_int(maps * k->size(1)) : 0,
+                                                   to_int(D / maps),
                                                    as<int32_t>(how.pos), how.axes, how.host_pairs(), as<double>(how.freq), how.R(),
                                                    how.interleaved, (float)how.factor, ptr(qo), ptr(ko), call.stream()));
   return {qo, ko};
@@ -719,6 +729,15 @@ std::tuple<Tensor, Tensor, Tensor> rotary_permute(const Tensor& q, const Tensor&
   how.fits(q, N);
   const std::vector<int64_t> size = back ? std::vector<int64_t>{N, H, D} : std::vector<int64_t>{H, N, D};
   Tensor qo = call.make(size, q), ko = call.make(size, k), vo = call.make(size, v);
+  if (how.maps == 2) {
+    const bool each = how.each_map(D);
+    check(back ? "moga_rotary_permute_maps_bwd" : "moga_rotary_permute_maps_fwd",
+          (back ? moga_rotary_permute_maps_bwd : moga_rotary_permute_maps_fwd)(
+              ptr(q), ptr(k), ptr(v), dt(q), N, to_int(H), to_int(D), as<int32_t>(perm), as<int32_t>(how.pos), how.axes, how.host_pairs(),
+              as<double>(how.freq), each ? how.R() / 2 : how.R(), each, how.interleaved, (float)how.factor, ptr(qo), ptr(ko), ptr(vo),
+              call.stream()));
+    return {qo, ko, vo};
+  }
   check(back ? "moga_rotary_permute_bwd" : "moga_rotary_permute_fwd",
         (back ? moga_rotary_permute_bwd : moga_rotary_permute_fwd)(ptr(q), ptr(k), ptr(v), dt(q), N, to_int(H), to_int(D), as<int32_t>(perm),
                                                                    as<int32_t>(how.pos), how.axes, how.host_pairs(), as<double>(how.freq), how.R(),
@@ -933,12 +952,12 @@ struct LayerNorm : public torch::autograd::Function<LayerNorm> {
 
 struct Rotary : public torch::autograd::Function<Rotary> {
   static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& pos, const Tensor& freq,
-                               const std::vector<int64_t>& pairs, bool interleaved, double factor) {
-    const Rotation how(aligned(pos), aligned(freq), pairs, interleaved, factor);   // positions of a piece of a sequence
+                               const std::vector<int64_t>& pairs, bool interleaved, double factor, int64_t maps) {
+    const Rotation how(aligned(pos), aligned(freq), pairs, interleaved, factor, maps);   // positions of a piece of a sequence
     auto [qo, ko] = rotary_turn(q, k, how, false, std::nullopt);
     ctx->save_for_backward({how.pos, how.freq});
     ctx->saved_data["pairs"] = pairs;
-    ctx->saved_data["how"] = std::vector<double>{interleaved ? 1. : 0., factor};
+    ctx->saved_data["how"] = std::vector<double>{interleaved ? 1. : 0., factor, (double)maps};
     ctx->set_materialize_grads(false);
     return {*qo, *ko};
   }
@@ -948,9 +967,10 @@ struct Rotary : public torch::autograd::Function<Rotary> {
     OptTensor dq, dk;
     if (grads[0].defined()) dq = aligned(grads[0]);
     if (grads[1].defined()) dk = aligned(grads[1]);
-    variable_list out(7);
+    variable_list out(8);
     if (!dq && !dk) return out;
-    auto [a, b] = rotary_turn(dq, dk, Rotation(s[0], s[1], ctx->saved_data["pairs"].toIntVector(), how[0] != 0., how[1]), true, std::nullopt);
+    auto [a, b] = rotary_turn(dq, dk, Rotation(s[0], s[1], ctx->saved_data["pairs"].toIntVector(), how[0] != 0., how[1], (int64_t)how[2]), true,
+                              std::nullopt);
     out[0] = or_empty(a);
     out[1] = or_empty(b);
     return out;
@@ -975,7 +995,8 @@ struct DiffAttention : public torch::autograd::Function<DiffAttention> {
     need_like(lam, q, {q.size(1)}, at::kFloat, "lambda");
     need(pos.has_value() == freq.has_value(), "positions and inv_freq");
     std::optional<Rotation> how;
-    if (pos) how.emplace(aligned(*pos), aligned(*freq), pairs, interleaved, factor);
+    if (pos) how.emplace(aligned(*pos), aligned(*freq), pairs, interleaved, factor, 2);
+    if (how) how->each_map(q.size(2));
     auto [group, gate, probs, logits] = route(x, w, std::nullopt, true, false, std::nullopt);
     Tensor qh, kh, vh;
     Permuted p;
@@ -1011,7 +1032,7 @@ struct DiffAttention : public torch::autograd::Function<DiffAttention> {
     auto [d_qh, d_kh, d_vh, d_lam] = diff_attn_bwd(d_oh, qh, kh, vh, parts, lse, lam, cu, cu, a[0], std::nullopt);
     Tensor d_q, d_k, d_v;
     if (s[15].defined())
-      std::tie(d_q, d_k, d_v) = rotary_permute(d_qh, d_kh, d_vh, perm, Rotation(s[15], s[16], ctx->saved_data["pairs"].toIntVector(), a[4] != 0., a[5]),
+      std::tie(d_q, d_k, d_v) = rotary_permute(d_qh, d_kh, d_vh, perm, Rotation(s[15], s[16], ctx->saved_data["pairs"].toIntVector(), a[4] != 0., a[5], 2),
                                                true, std::nullopt);
     else
       std::tie(d_q, d_k, d_v) = permute_bwd(d_qh, d_kh, d_vh, perm, std::nullopt);
@@ -1086,13 +1107,15 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
   m.def(
       "rotary",
       [](const OptTensor& q, const OptTensor& k, const Tensor& pos, const Tensor& freq, const std::vector<int64_t>& pairs, bool interleaved,
-         double factor, bool back, const OptStream& stream) { return rotary_turn(q, k, Rotation(pos, freq, pairs, interleaved, factor), back, stream); },
+         double factor, int64_t maps, bool back, const OptStream& stream) {
+        return rotary_turn(q, k, Rotation(pos, freq, pairs, interleaved, factor, maps), back, stream);
+      },
       nogil);
   m.def(
       "rotary_permute",
       [](const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& perm, const Tensor& pos, const Tensor& freq,
-         const std::vector<int64_t>& pairs, bool interleaved, double factor, bool back, const OptStream& stream) {
-        return rotary_permute(q, k, v, perm, Rotation(pos, freq, pairs, interleaved, factor), back, stream);
+         const std::vector<int64_t>& pairs, bool interleaved, double factor, int64_t maps, bool back, const OptStream& stream) {
+        return rotary_permute(q, k, v, perm, Rotation(pos, freq, pairs, interleaved, factor, maps), back, stream);
       },
       nogil);
   m.def("diff_attn_fwd", &diff_attn_fwd, nogil);
@@ -1101,8 +1124,9 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
       "layer_norm", [](const Tensor& x, const OptTensor& w, const OptTensor& b, double eps) { return LayerNorm::apply(x, w, b, eps); }, nogil);
   m.def(
       "rotary_apply",
-      [](const Tensor& q, const Tensor& k, const Tensor& pos, const Tensor& freq, const std::vector<int64_t>& pairs, bool interleaved, double factor) {
-        auto r = Rotary::apply(q, k, pos, freq, pairs, interleaved, factor);
+      [](const Tensor& q, const Tensor& k, const Tensor& pos, const Tensor& freq, const std::vector<int64_t>& pairs, bool interleaved, double factor,
+         int64_t maps) {
+        auto r = Rotary::apply(q, k, pos, freq, pairs, interleaved, factor, maps);
         return std::make_tuple(r[0], r[1]);
       },
       nogil);
