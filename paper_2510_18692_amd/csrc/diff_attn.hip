@@ -213,7 +213,10 @@ __global__ __launch_bounds__(256, 2) void diff_fwd_kernel(DiffFwd a) {
 #pragma unroll
       for (int dt = 0; dt < D / 16; ++dt) {
         const floatx4_t o1 = st.o[0][dt][q] * inv1, o2 = st.o[1][dt][q] * inv2;
-        store4((T*)a.o + (head_q + row) * D, dt, o1 - o2 * lam);
+        floatx4_t o;   // one rounding of the maps' own sums, written out: else the compiler chooses, and not alike with and without parts
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = fmaf(-lam, o2[i], o1[i]);
+        store4((T*)a.o + (head_q + row) * D, dt, o);
         if (a.parts) {
           store4(a.parts + (head_q + row) * D, dt, o1);
           store4(a.parts + ((int64_t)a.H * a.Nq + head_q + row) * D, dt, o2);
@@ -367,7 +370,7 @@ __global__ __launch_bounds__(256) void diff_merge_kernel(DiffFwd a, int pieces, 
   T* out = (T*)a.o + row * D + lane * V;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const float v = o[0][i] - lam * o[1][i];
+    const float v = fmaf(-lam, o[1][i], o[0][i]);
     if constexpr (sizeof(T) == 4) out[i] = v;
     else out[i] = f32_to_bf16_bits(v);
     if (a.parts) {
