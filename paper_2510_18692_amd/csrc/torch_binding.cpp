@@ -980,7 +980,7 @@ struct Rotary : public torch::autograd::Function<Rotary> {
 struct DiffAttention : public torch::autograd::Function<DiffAttention> {
   static variable_list forward(AutogradContext* ctx, const Tensor& x, const Tensor& w, const Tensor& q, const Tensor& k, const Tensor& v,
                                const Tensor& lam, double scale, std::optional<double> alpha, bool grad_x, const OptTensor& pos,
-                               const OptTensor& freq, const std::vector<int64_t>& pairs, bool interleaved, double factor) {
+                               const OptTensor& freq, const std::vector<int64_t>& pairs, bool interleaved, double factor, bool train) {
     require(x, w, q, k, v, lam, pos, freq);
     need_dims(x, 2);
     need_dims(w, 2);
@@ -1007,11 +1007,11 @@ struct DiffAttention : public torch::autograd::Function<DiffAttention> {
       p = permute(group, M, q, k, v, std::nullopt);
       qh = *p.qh, kh = *p.kh, vh = *p.vh;
     }
-    auto [oh, parts, lse] = diff_attn_fwd(qh, kh, vh, lam, p.cu_seqlens, p.cu_seqlens, scale, true, std::nullopt);
+    auto [oh, parts, lse] = diff_attn_fwd(qh, kh, vh, lam, p.cu_seqlens, p.cu_seqlens, scale, train, std::nullopt);
     Tensor o = unpermute(oh, p.perm, gate, std::nullopt, std::nullopt);
     Tensor loss = alpha ? at::empty({}, x.options().dtype(at::kFloat)) : at::zeros({}, x.options().dtype(at::kFloat)), frac;
     if (alpha) frac = std::get<0>(balance_into(loss, group, gate, M, *alpha, std::nullopt));
-    ctx->save_for_backward({x, w, group, gate, *probs, p.perm, p.cu_seqlens, qh, kh, vh, lam, oh, *parts, lse, frac, how ? how->pos : Tensor(),
+    ctx->save_for_backward({x, w, group, gate, *probs, p.perm, p.cu_seqlens, qh, kh, vh, lam, oh, or_empty(parts), lse, frac, how ? how->pos : Tensor(),
                             how ? how->freq : Tensor()});
     ctx->saved_data["args"] = std::vector<double>{scale, alpha.value_or(0.), alpha ? 1. : 0., grad_x ? 1. : 0., interleaved ? 1. : 0., factor};
     ctx->saved_data["pairs"] = pairs;
@@ -1041,7 +1041,7 @@ struct DiffAttention : public torch::autograd::Function<DiffAttention> {
     if (a[3] != 0.) dx = x.scalar_type();
     auto [d_w, d_x] = route_bwd_with(x, w, probs, group, gate, d_gate, balanced ? OptTensor(frac) : std::nullopt, a[1],
                                      balanced ? OptTensor(grads[1]) : std::nullopt, dx, std::nullopt);
-    variable_list out(14);
+    variable_list out(15);
     out[0] = or_empty(d_x);
     out[1] = d_w, out[2] = d_q, out[3] = d_k, out[4] = d_v, out[5] = d_lam;
     return out;
@@ -1052,7 +1052,11 @@ std::tuple<Tensor, Tensor, Tensor> diff_attention(const Tensor& x, const Tensor&
                                                   const Tensor& lam, double scale, std::optional<double> alpha, bool grad_x,
                                                   const OptTensor& pos, const OptTensor& freq, const std::vector<int64_t>& pairs,
                                                   bool interleaved, double factor) {
-  auto r = DiffAttention::apply(x, w, q, k, v, lam, scale, alpha, grad_x, pos, freq, pairs, interleaved, factor);
+  // the two maps' sums of V are the backward's: 8 bytes a channel and row
+  bool train = false;
+  if (at::GradMode::is_enabled())
+    for (const Tensor* t : {&x, &w, &q, &k, &v, &lam}) train = train || t->requires_grad();
+  auto r = DiffAttention::apply(x, w, q, k, v, lam, scale, alpha, grad_x, pos, freq, pairs, interleaved, factor, train);
   return {r[0], r[1], r[2]};
 }
 
