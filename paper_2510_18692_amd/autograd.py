@@ -8,6 +8,8 @@ balancing loss when it is used); the assignment itself is a constant of differen
 gradient is returned for the router input x unless `grad_x=True` (the optional dX of the router
 backward).  Everything runs in the HIP library; the autograd function itself is native
 (csrc/torch_binding.cpp), so that the backward pass does not enter the interpreter.
+`layer_norm`, `rotary` and `moga_diff_attention` have first derivatives only: gradients taken with
+create_graph=True raise an error where they are differentiated again.
 """
 from __future__ import annotations
 

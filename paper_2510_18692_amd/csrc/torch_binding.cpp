@@ -924,6 +924,28 @@ Tensor aligned(const Tensor& t) {
   return (uintptr_t)c.data_ptr() % 16 ? c.clone() : c;
 }
 
+// The calls give first derivatives.  With create_graph=True their gradients get a node that refuses, on the way to what they depend on; without one the
+// graph would end there, and a second derivative would come out without their part.
+struct NoDerivative : public torch::autograd::Node {
+  variable_list apply(variable_list&&) override {
+    TORCH_CHECK(false, "layer_norm, rotary and moga_diff_attention have no second derivative");
+  }
+};
+// Of a backward that runs now: its gradients, what it was given, and whether the former depend on the forward's inputs too.
+variable_list first_only(variable_list out, const variable_list& given, bool on_inputs = true) {
+  if (!at::GradMode::is_enabled()) return out;
+  torch::autograd::edge_list to;
+  if (on_inputs) to = torch::autograd::get_current_node()->next_edges();
+  for (const Tensor& g : given)
+    if (g.defined() && g.requires_grad()) to.push_back(torch::autograd::impl::gradient_edge(g));
+  if (to.empty()) return out;
+  const std::shared_ptr<NoDerivative> node(new NoDerivative(), torch::autograd::deleteNode);
+  node->set_next_edges(std::move(to));
+  for (Tensor& g : out)
+    if (g.defined()) torch::autograd::create_gradient_edge(g, node);
+  return out;
+}
+
 struct LayerNorm : public torch::autograd::Function<LayerNorm> {
   static Tensor forward(AutogradContext* ctx, const Tensor& x, const OptTensor& w, const OptTensor& b, double eps) {
     require(x, w, b);
@@ -946,7 +968,7 @@ struct LayerNorm : public torch::autograd::Function<LayerNorm> {
     // inputs are counted without those that are absent
     const bool dw = (s[1].defined() && ctx->needs_input_grad(1)) || (bias && ctx->needs_input_grad(s[1].defined() ? 2 : 1));
     auto [d_x, d_w, d_b] = layer_norm_bwd(d_y.view(s[0].sizes()), s[0], or_none(s[1]), s[2], s[3], dw, std::nullopt);
-    return {d_x.view(d_y.sizes()), s[1].defined() ? or_empty(d_w) : Tensor(), bias ? or_empty(d_b) : Tensor(), Tensor()};
+    return first_only({d_x.view(d_y.sizes()), s[1].defined() ? or_empty(d_w) : Tensor(), bias ? or_empty(d_b) : Tensor(), Tensor()}, grads);
   }
 };
 
@@ -973,7 +995,7 @@ struct Rotary : public torch::autograd::Function<Rotary> {
                               std::nullopt);
     out[0] = or_empty(a);
     out[1] = or_empty(b);
-    return out;
+    return first_only(out, grads, false);   // linear
   }
 };
 
@@ -1044,7 +1066,7 @@ struct DiffAttention : public torch::autograd::Function<DiffAttention> {
     variable_list out(15);
     out[0] = or_empty(d_x);
     out[1] = d_w, out[2] = d_q, out[3] = d_k, out[4] = d_v, out[5] = d_lam;
-    return out;
+    return first_only(out, grads);
   }
 };
 
