@@ -946,6 +946,8 @@ variable_list first_only(variable_list out, const variable_list& given, bool on_
   return out;
 }
 
+OptTensor aligned(const OptTensor& t) { return t ? OptTensor(aligned(*t)) : std::nullopt; }
+
 struct LayerNorm : public torch::autograd::Function<LayerNorm> {
   static Tensor forward(AutogradContext* ctx, const Tensor& x, const OptTensor& w, const OptTensor& b, double eps) {
     require(x, w, b);
@@ -953,10 +955,8 @@ struct LayerNorm : public torch::autograd::Function<LayerNorm> {
     const int64_t C = x.size(-1);
     need(C >= 1, "x: an empty last dimension");
     const Tensor rows = aligned(x.view({x.numel() / C, C}));
-    OptTensor wa, ba;
-    if (w) wa = aligned(*w);
-    if (b) ba = aligned(*b);
-    auto [y, mean, rstd] = layer_norm_fwd(rows, wa, ba, eps, true, std::nullopt);
+    const OptTensor wa = aligned(w);
+    auto [y, mean, rstd] = layer_norm_fwd(rows, wa, aligned(b), eps, true, std::nullopt);
     ctx->save_for_backward({rows, or_empty(wa), *mean, *rstd});
     ctx->saved_data["bias"] = b.has_value();
     return y.view(x.sizes());
@@ -975,8 +975,9 @@ struct LayerNorm : public torch::autograd::Function<LayerNorm> {
 struct Rotary : public torch::autograd::Function<Rotary> {
   static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& pos, const Tensor& freq,
                                const std::vector<int64_t>& pairs, bool interleaved, double factor, int64_t maps) {
+    require(q, k, pos, freq);
     const Rotation how(aligned(pos), aligned(freq), pairs, interleaved, factor, maps);   // positions of a piece of a sequence
-    auto [qo, ko] = rotary_turn(q, k, how, false, std::nullopt);
+    auto [qo, ko] = rotary_turn(aligned(q), aligned(k), how, false, std::nullopt);
     ctx->save_for_backward({how.pos, how.freq});
     ctx->saved_data["pairs"] = pairs;
     ctx->saved_data["how"] = std::vector<double>{interleaved ? 1. : 0., factor, (double)maps};
@@ -986,9 +987,7 @@ struct Rotary : public torch::autograd::Function<Rotary> {
   static variable_list backward(AutogradContext* ctx, const variable_list& grads) {
     const auto s = ctx->get_saved_variables();
     const auto how = ctx->saved_data["how"].toDoubleVector();
-    OptTensor dq, dk;
-    if (grads[0].defined()) dq = aligned(grads[0]);
-    if (grads[1].defined()) dk = aligned(grads[1]);
+    const OptTensor dq = aligned(or_none(grads[0])), dk = aligned(or_none(grads[1]));
     variable_list out(8);
     if (!dq && !dk) return out;
     auto [a, b] = rotary_turn(dq, dk, Rotation(s[0], s[1], ctx->saved_data["pairs"].toIntVector(), how[0] != 0., how[1], (int64_t)how[2]), true,
@@ -1000,10 +999,11 @@ struct Rotary : public torch::autograd::Function<Rotary> {
 };
 
 struct DiffAttention : public torch::autograd::Function<DiffAttention> {
-  static variable_list forward(AutogradContext* ctx, const Tensor& x, const Tensor& w, const Tensor& q, const Tensor& k, const Tensor& v,
-                               const Tensor& lam, double scale, std::optional<double> alpha, bool grad_x, const OptTensor& pos,
+  static variable_list forward(AutogradContext* ctx, const Tensor& x_in, const Tensor& w_in, const Tensor& q_in, const Tensor& k_in,
+                               const Tensor& v_in, const Tensor& lam, double scale, std::optional<double> alpha, bool grad_x, const OptTensor& pos,
                                const OptTensor& freq, const std::vector<int64_t>& pairs, bool interleaved, double factor, bool train) {
-    require(x, w, q, k, v, lam, pos, freq);
+    require(x_in, w_in, q_in, k_in, v_in, lam, pos, freq);
+    const Tensor x = aligned(x_in), w = aligned(w_in), q = aligned(q_in), k = aligned(k_in), v = aligned(v_in);
     need_dims(x, 2);
     need_dims(w, 2);
     need_dims(q, 3);
