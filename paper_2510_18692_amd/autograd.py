@@ -28,7 +28,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-6):
 
 
 def rotary(q, k, positions, inv_freq, axis_pairs=None, interleaved=False, factor=1.0, maps=1):
-    """Rotary positions of q [N, Hq, D] and k [N, Hk, D] (binding.moga_rotary_fwd; maps=2 before moga_diff_attention) -> (qo, ko)."""
+    """Rotary positions of q [N, Hq, D] and k [N, Hk, D], either may be None (binding.moga_rotary_fwd; maps=2 before moga_diff_attention) -> (qo, ko)."""
     return mg._nat.rotary_apply(q, k, positions, inv_freq, axis_pairs or [], interleaved, factor, maps)
 
 

@@ -973,21 +973,26 @@ struct LayerNorm : public torch::autograd::Function<LayerNorm> {
 };
 
 struct Rotary : public torch::autograd::Function<Rotary> {
-  static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& pos, const Tensor& freq,
+  // Outputs: of q and k those that are there.
+  static variable_list forward(AutogradContext* ctx, const OptTensor& q, const OptTensor& k, const Tensor& pos, const Tensor& freq,
                                const std::vector<int64_t>& pairs, bool interleaved, double factor, int64_t maps) {
     require(q, k, pos, freq);
     const Rotation how(aligned(pos), aligned(freq), pairs, interleaved, factor, maps);   // positions of a piece of a sequence
     auto [qo, ko] = rotary_turn(aligned(q), aligned(k), how, false, std::nullopt);
     ctx->save_for_backward({how.pos, how.freq});
     ctx->saved_data["pairs"] = pairs;
-    ctx->saved_data["how"] = std::vector<double>{interleaved ? 1. : 0., factor, (double)maps};
+    ctx->saved_data["how"] = std::vector<double>{interleaved ? 1. : 0., factor, (double)maps, q ? 1. : 0., k ? 1. : 0.};
     ctx->set_materialize_grads(false);
-    return {*qo, *ko};
+    variable_list out;
+    if (qo) out.push_back(*qo);
+    if (ko) out.push_back(*ko);
+    return out;
   }
   static variable_list backward(AutogradContext* ctx, const variable_list& grads) {
     const auto s = ctx->get_saved_variables();
     const auto how = ctx->saved_data["how"].toDoubleVector();
-    const OptTensor dq = aligned(or_none(grads[0])), dk = aligned(or_none(grads[1]));
+    const OptTensor dq = how[3] != 0. ? aligned(or_none(grads[0])) : std::nullopt;
+    const OptTensor dk = how[4] != 0. ? aligned(or_none(grads.back())) : std::nullopt;
     variable_list out(8);
     if (!dq && !dk) return out;
     auto [a, b] = rotary_turn(dq, dk, Rotation(s[0], s[1], ctx->saved_data["pairs"].toIntVector(), how[0] != 0., how[1], (int64_t)how[2]), true,
@@ -1150,10 +1155,11 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
       "layer_norm", [](const Tensor& x, const OptTensor& w, const OptTensor& b, double eps) { return LayerNorm::apply(x, w, b, eps); }, nogil);
   m.def(
       "rotary_apply",
-      [](const Tensor& q, const Tensor& k, const Tensor& pos, const Tensor& freq, const std::vector<int64_t>& pairs, bool interleaved, double factor,
-         int64_t maps) {
-        auto r = Rotary::apply(q, k, pos, freq, pairs, interleaved, factor, maps);
-        return std::make_tuple(r[0], r[1]);
+      [](const OptTensor& q, const OptTensor& k, const Tensor& pos, const Tensor& freq, const std::vector<int64_t>& pairs, bool interleaved,
+         double factor, int64_t maps) {
+        need(q || k, "q or k");
+        const auto r = Rotary::apply(q, k, pos, freq, pairs, interleaved, factor, maps);
+        return std::make_tuple(q ? OptTensor(r[0]) : std::nullopt, k ? OptTensor(r.back()) : std::nullopt);
       },
       nogil);
   m.def("diff_attention", &diff_attention, nogil);

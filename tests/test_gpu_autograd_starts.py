@@ -1,4 +1,4 @@
-"""autograd's rotary and moga_diff_attention on tensors that begin at any element, as pieces of longer ones do."""
+"""autograd's rotary and moga_diff_attention on tensors that begin at any element, as pieces of longer ones do, and rotary of queries or keys alone."""
 import pytest
 import torch
 
@@ -32,6 +32,24 @@ def test_rotary(dtype, maps):
     assert all(torch.equal(s, t) for s, t in zip(y, mg.moga_rotary_fwd(q, k, pos, freq, maps=maps)))
     got = torch.autograd.grad(y, [a, b], [_later(dq), _later(dk)])
     assert all(torch.equal(s, t) for s, t in zip(got, mg.moga_rotary_bwd(dq, dk, pos, freq, maps=maps)))
+
+
+def test_rotary_of_one_side():
+    N, D = 33, 64
+    x, d = _rnd(1, N, 3, D), _rnd(2, N, 3, D)
+    pos = torch.arange(N, dtype=torch.int32, device="cuda")
+    freq, _ = mg.moga_rotary_freqs(D)
+    want, back = mg.moga_rotary_fwd(x, None, pos, freq)[0], mg.moga_rotary_bwd(d, None, pos, freq)[0]
+    for side in range(2):
+        a = x.clone().requires_grad_()
+        y = rotary(*((a, None) if side == 0 else (None, a)), pos, freq)
+        assert y[1 - side] is None and torch.equal(y[side], want)
+        assert torch.equal(torch.autograd.grad(y[side], a, d)[0], back)
+    with pytest.raises(ValueError):
+        rotary(None, None, pos, freq)
+    q, k = x.clone().requires_grad_(), d   # only one of two needs a gradient
+    yq, yk = rotary(q, k, pos, freq)
+    assert torch.equal(torch.autograd.grad(yq.sum() + yk.sum(), q)[0], mg.moga_rotary_bwd(torch.ones_like(x), None, pos, freq)[0])
 
 
 @pytest.mark.parametrize("positions", [False, True])
