@@ -230,7 +230,7 @@ __global__ __launch_bounds__(256, 2) void diff_fwd_kernel(DiffFwd a) {
   }
 }
 
-// bf16 calls of few queries a group: the blocks go by the keys, `chunk` of a group each, and take all queries of the group, 16 at a time.  The
+// bf16 calls of few queries: the blocks go by the keys, `chunk` of a group each, and take all queries of the group, 16 at a time.  The
 // four waves share the keys out, every fourth tile each from a ring of its own without a barrier, and add up what they have.  Bound by HBM:
 // 4 x 32 KB are on their way to a CU.  4 queries, 65,536 keys, 12 heads: 77 us, 5.2 TB/s (a call 84 us; by tiles of 128 queries with split keys 247).
 // Sums and maxima go to part and stat, for piece (first key / chunk) of the group.
@@ -911,12 +911,18 @@ size_t diff_piece_bytes(int64_t Nq, int H, int D) { return (size_t)Nq * H * 2 * 
 // How a forward call shares out its keys.  chunk > 0: diff_few_kernel, pieces of `chunk` keys, at most `pieces` of a group; else pieces of every
 // tile of queries (1: whole).
 struct DiffSplit { int pieces, chunk; };
+// The sizes of the groups are on the device, and all queries of a call may be one group's, which diff_few_kernel takes 16 at a time, with the keys
+// read again each time: four times at most.  By the mean alone a call of one group of 6,001 queries beside 399 of one, 4,000 keys each, one head, took 13.3 ms
+// against 0.18 by tiles, and one of 3,800 (with as many keys) beside 256 of one with 1,000, 12 heads, 8.3 against 0.45; with 64 queries at most 61
+// beside three of one take 45 us against 23.  Where every group has as many, beyond 64 tiles take 0.46 to 1.06 of the time (12 heads, 24 groups of 16 queries and
+// 300 keys 20 us against 44, 64 of 16 and 4,000 284 against 298, 32 of 4 and 4,000 171 against 167), 1.27 at worst (one head, 43 of 4 and 16,384).
+constexpr int64_t kFewQueries = 64;
 DiffSplit diff_split(int64_t Nq, int64_t Nk, int H, int D, int G, int dtype) {
-  // Up to 16 queries a group the matrix products of a tile of 128 are idle work, and three of its waves too: pieces of keys for two rounds of
+  // Up to 16 queries a mean group the matrix products of a tile of 128 are idle work, and three of its waves too: pieces of keys for two rounds of
   // blocks, one a CU (or one round more than what the groups' last pieces make), none under 256 keys, and as many as 256 MB hold (one group
   // might have all the keys).  A group's last piece is half a piece on average.
   const int64_t most = (256 << 20) / (int64_t)diff_piece_bytes(Nq, H, D);
-  if (dtype == MOGA_BF16 && Nq <= 16 * (int64_t)G && Nk / G >= 128 && most >= 1) {
+  if (dtype == MOGA_BF16 && Nq <= std::min(kFewQueries, 16 * (int64_t)G) && Nk / G >= 128 && most >= 1) {
     const int64_t ends = (int64_t)G * H / 2, rounds = std::max<int64_t>(2, (ends + 2 * kCus - 1) / kCus);
     const int64_t even = Nk * H / std::max<int64_t>(1, rounds * kCus * 49 / 50 - ends);
     const int64_t chunk = round_up((size_t)std::min(Nk, std::max({(int64_t)256, even, (Nk + most - 1) / most})), 128);

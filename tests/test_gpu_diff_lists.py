@@ -18,31 +18,53 @@ def _room(cu_q, cu_k, H):
     return need, mg.load().moga_workspace_preferred_bytes(mg.OP_DIFF_ATTN_FWD, cu_q[-1], cu_k[-1], H, 128, G, 0, BF16)
 
 
-def _lists(groups, longest, most):
+def _lists(groups, longest, queries):
+    """Some groups with a query or more, most with none; 0 to `longest` keys, and one group with all of them."""
     g = torch.Generator().manual_seed(groups)
-    cu_q = _cu([int(x) for x in torch.randint(0, most + 1, (groups - 1,), generator=g)] + [40])
-    return cu_q, _cu([longest] + [int(x) for x in torch.randint(0, longest + 1, (groups - 1,), generator=g)])
+    sq = torch.bincount(torch.randint(0, groups, (queries,), generator=g), minlength=groups)
+    return _cu(sq.tolist()), _cu([longest] + [int(x) for x in torch.randint(0, longest + 1, (groups - 1,), generator=g)])
 
 
-# groups, longest list, most queries of a group but the last
-MANY = [(257, 600, 1), (300, 600, 16), (1100, 300, 3)]
+MANY = [(257, 600, 3), (300, 600, 64), (1100, 300, 41)]
 
 
-@pytest.mark.parametrize("groups,longest,most", MANY)
-def test_the_lists_are_split_by_their_keys(groups, longest, most):
-    """Tiles of 128 queries (their groups alone fill the chip) would not be split: any room beyond the lookup's is that of pieces of keys."""
-    cu_q, cu_k = _lists(groups, longest, most)
-    need, room = _room(cu_q, cu_k, 2)
-    assert need >= 4 * (groups + 1) and room > need
-    tiles = -(-cu_q[-1] // 128) + groups   # as the host counts them
-    assert tiles * 2 > 256
+@pytest.mark.parametrize("groups,longest,queries", MANY)
+def test_the_lists_are_split_by_their_keys(groups, longest, queries):
+    """Tiles of 128 queries are split from 512 keys of a mean group on: any room beyond the lookup's is that of pieces of keys."""
+    cu_q, cu_k = _lists(groups, longest, queries)
+    need, room = _room(cu_q, cu_k, 12)
+    assert cu_k[-1] < 512 * groups and need >= 4 * (groups + 1) and room > need
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("groups,longest,most", MANY)
-def test_more_groups_than_the_lookup_scans(groups, longest, most):
-    cu_q, cu_k = _lists(groups, longest, most)
-    t = _inputs(2, 128, torch.bfloat16, cu_q, cu_k, 33)
+@pytest.mark.parametrize("groups,longest,queries", MANY)
+def test_more_groups_than_the_lookup_scans(groups, longest, queries):
+    cu_q, cu_k = _lists(groups, longest, queries)
+    t = _inputs(12, 128, torch.bfloat16, cu_q, cu_k, 33)
+    _check(_run(*t, cu_q, cu_k, 0.125), *t, cu_q, cu_k, 0.125, near=False)
+
+
+# one group has most of the queries
+SKEWED = [(12, [1] * 256 + [3800], [1000] * 256 + [3800]), (1, [1] * 399 + [6001], [4000] * 400), (3, [1] * 40 + [300], [400] * 41)]
+
+
+@pytest.mark.parametrize("H,sq,sk", SKEWED)
+def test_many_queries_are_no_few(H, sq, sk):
+    """diff_few_kernel reads a group's keys for every 16 queries, and the host does not know the groups: it is taken where all queries in one group would
+    be four times that.  By tiles these calls are whole (room for the lookup alone) or in 16 pieces at most."""
+    need, room = _room(_cu(sq), _cu(sk), H)
+    assert room <= need + 16 * sum(sq) * H * 2 * 130 * 4 and (sum(sq) < 1000 or room == need)
+
+
+@pytest.mark.gpu
+def test_one_long_group_among_single_queries():
+    H, sq, sk = SKEWED[2]
+    cu_q, cu_k = _cu(sq), _cu(sk)
+    t = _inputs(H, 128, torch.bfloat16, cu_q, cu_k, 35)
+    _check(_run(*t, cu_q, cu_k, 0.125), *t, cu_q, cu_k, 0.125, near=False)
+    cu_q = _cu([1, 1, 61, 1])   # few in all: four times 16 in one group
+    cu_k = _cu([700, 300, 900, 1200])
+    t = _inputs(H, 128, torch.bfloat16, cu_q, cu_k, 36)
     _check(_run(*t, cu_q, cu_k, 0.125), *t, cu_q, cu_k, 0.125, near=False)
 
 
