@@ -6,8 +6,10 @@
 //   dV = (P_1 - lambda P_2)^T dO, dlambda = -sum P_2 * dP
 // so that a backward has the matrix products of plain attention, and a forward one and a half times them (two weighted sums of V).
 //
-// bf16 calls are bound by the matrix cores (diff_steps.h, diff_keys.h, dQ below), those of few queries by HBM, fp32 calls by products of 1 / 8
-// of bf16's rate and, at the sizes of gradient checks, by launches and by the length of a group's sweep.
+// bf16 calls of long groups are bound by the matrix and vector work of a SIMD (diff_steps.h, diff_keys.h), those of groups of some hundred rows by rounds of
+// unequal blocks (matrix cores busy 0.33 to 0.37 of the cycles at 10,007 x 12, 20 groups), those of few queries by HBM, fp32 calls by products of 1 / 8
+// of bf16's rate (8,192 x 12 heads of 128, one group: 120 TFLOP/s forward and dQ, 102 dK and dV, of 154) and, at the sizes of gradient
+// checks, by launches and by the length of a group's sweep.
 #include <algorithm>
 #include <cmath>
 
@@ -126,7 +128,7 @@ __device__ __forceinline__ void diff_fwd_step(const Tiles& tiles, const Frag<T> 
   }
 }
 
-// fp32: step by step.  4,096 x 2 heads of 64, 8 groups: 34 us in pieces of the keys and 7 to join them.
+// fp32: step by step.  4,096 x 2 heads of 64, 8 groups: 33 us in pieces of the keys and 7 to join them.
 template <typename T, int D>
 struct DiffPlainSweep : DiffState<D, 1> {
   typedef DiffTiles<T, D> Tiles;
@@ -155,8 +157,8 @@ __device__ __forceinline__ void piece_range(int piece, int pieces, int& first, i
   n = end - 32 * t0;
 }
 
-// A tile of kRows queries, or (SPLIT) blockIdx.y's share of its keys.  32,760 x 12 heads, bf16, 8 groups 1.27 ms; 10,007 x 12, 20 groups of unequal
-// length 105 us.
+// A tile of kRows queries, or (SPLIT) blockIdx.y's share of its keys.  32,760 x 12 heads, bf16, 8 groups 1.31 ms by itself; 10,007 x 12, 20 groups
+// of unequal length 117 us.
 template <typename T, int D, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void diff_fwd_kernel(DiffFwd a) {
   constexpr int NC = kCols<T>;
@@ -232,7 +234,8 @@ __global__ __launch_bounds__(256, 2) void diff_fwd_kernel(DiffFwd a) {
 
 // bf16 calls of few queries: the blocks go by the keys, `chunk` of a group each, and take all queries of the group, 16 at a time.  The
 // four waves share the keys out, every fourth tile each from a ring of its own without a barrier, and add up what they have.  Bound by HBM:
-// 4 x 32 KB are on their way to a CU.  4 queries, 65,536 keys, 12 heads: 77 us, 5.2 TB/s (a call 84 us; by tiles of 128 queries with split keys 247).
+// 4 x 32 KB are on their way to a CU.  4 queries, 65,536 keys, 12 heads: 78 us, 5.2 TB/s; a call, with the join, of four lists of equal length 92 us,
+// by tiles of 128 queries with split keys 109.
 // Sums and maxima go to part and stat, for piece (first key / chunk) of the group.
 __global__ __launch_bounds__(256, 1) void diff_few_kernel(DiffFwd a, int chunk) {
   constexpr int D = kHeadDim;
@@ -455,7 +458,8 @@ __device__ __forceinline__ void diff_products(const Tiles& tiles, int t, const F
 // of V have weights rounded to operands, and where few keys carry a row delta's error is felt: dQ's is 1.43 of a plain rounding's instead of
 // 1.49 at 70 keys a group, dK's 1.41 instead of 1.46.  Up to 256 keys of a mean group the sweep takes what reading `parts` does (backward of
 // 10,007 x 12 heads, 40 groups 141 us against 138, 60,000 x 12, 1,000 groups 674 against 682, 1,560 x 4, 8 groups 34 against 29); at
-// 500 keys it takes longer (20 groups 220 against 192) for 1.445 instead of 1.47.
+// 500 keys it takes longer (20 groups 220 against 192) for 1.445 instead of 1.47.  The host knows the mean group only: a long group among short ones pays for
+// three products more beside the backward's seven.
 constexpr int64_t kDeltaKeys = 256;
 __global__ __launch_bounds__(256, 3) void diff_delta_kernel(DiffBwd a, const float* __restrict__ lse, floatx4_t* __restrict__ out) {
   constexpr int NC = kCols<unsigned short>, D = kHeadDim;
@@ -792,7 +796,7 @@ __global__ __launch_bounds__(256, 2) void diff_dq_f32_kernel(DiffBwd a) {
 }
 
 // bf16, both: blocks of keys (first of their pieces, then the next), then blocks of queries, which fill the others' last rounds: 10,007 x 12
-// heads, 20 unequal groups 206 us, 62,400 x 12, 8 groups 10.5 ms.
+// heads, 20 unequal groups 227 us, 62,400 x 12, 8 groups 10.6 ms.
 __global__ __launch_bounds__(256, 2) void diff_bwd_kernel(DiffBwd a, const int32_t* __restrict__ q_tiles, int q_blocks, int k_blocks) {
   __shared__ union {
     DiffTiles<unsigned short, kHeadDim>::Lds q;
@@ -878,13 +882,15 @@ int64_t diff_blocks(int64_t N, int H, int G, int rows) { return (max_tiles(N, G,
 size_t tile_bytes(int G) { return G > MOGA_MAX_GROUPS ? round_up(((size_t)G + 1) * sizeof(int32_t), 256) : 0; }
 
 // Pieces of the rows that a tile sweeps, where tiles of `rows` rows leave CUs idle.  bf16: as many as fill two blocks a CU, none under 256 rows of a
-// mean group.  Backward, whole and in pieces: 1,000 x 3 heads 86 and 40 us, 4,096 x 3 286 and 151; with pieces of 128 rows 4,096 x 3,
-// 8 groups 70 instead of 61.
+// mean group.  Whole and in pieces, forward: 1,000 x 3 heads 34 and 29 us, 4,096 x 3 101 and 72, 16,384 x 1 370 and 243, 16,384 x 1, 4 groups 100 and 89;
+// backward 55 and 41, 161 and 135, 771 and 490, 212 and 157.  It loses where tiles of several groups leave few CUs idle: 4,096 x 3, 8 groups
+// 24 and 31, backward 40 and 49 (in pieces of 128 rows a seventh more), 8,192 x 3, 4 groups 59 and 74, 124 and 133, 1,000 x 12 35 and 45, 58 and 70.
 // fp32, whose steps take ten times as long: none under 64 rows, and as many as make the fullest CU's work least: its blocks (an XCD deals its
 // share out to 32 CUs) times a block's steps and what starting it costs, in microseconds, and the traffic of the partial results.  One block a
 // CU takes 1.6 times what it would beside two others, two 1.1.  Groups of unequal length have some more tiles: half the cost is that of 5 % more.
-// Backward, whole and in pieces: 1,000 x 2 x 64 172 and 69 us; pieces for two blocks a CU of 128 rows and more instead: 6,000 x 4 x 128,
-// 8 groups forward 175 instead of 156 and backward 463 instead of 389, 256 x 2 x 128 28 and 61 instead of 22 and 44.
+// Backward, whole and in pieces: 1,000 x 2 x 64 175 and 68 us, 256 x 2 x 128 94 and 45, 6,000 x 4 x 128, 8 groups 449 and 378, 4,096 x 2 x 128, 8 groups 169
+// and 138; forward 73 and 34, 39 and 22, 174 and 154, 70 and 65, but 4,096 x 2 x 64, 8 groups 40.6 and 42.4.  Of sizes taken together: without the second
+// half of the cost a step of 4,096 x 2 x 64 in unequal groups took 128 us and not 120, the backward of 4,096 x 2 x 128 in equal ones 121 and not 138.
 int diff_pieces(int64_t N, int64_t other, int H, int G, int rows, int D, int dtype) {
   if (dtype != MOGA_F32) {
     const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(max_tiles(N, G, rows), N)) * H;

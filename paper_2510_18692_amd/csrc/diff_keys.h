@@ -4,12 +4,14 @@
 //   dV += (P_1 - lambda P_2) dO,  dK_1 += (P_1 dP') Q_1,  dK_2 += (P_2 (delta_2 - delta_1 - dP')) Q_2
 // with scale and lambda left to the end.  dP' has delta_1 as its starting value, and its sum is rounded once in 32 bits.
 //
-// Bound by the matrix cores and by the power they draw (1.85 GHz of 2.4).  Two waves a SIMD leave a lane 256 registers: 128 hold dK and dV, 32
+// Bound by the two kinds of work of a SIMD, which hardly overlap: with dQ's blocks in the launch, matrix products keep it busy for 0.54 of the cycles and
+// vector instructions for 0.50 (0.57 exponents a product, plain attention has 0.25 and 0.33; half of a step's vector work has no product beside it), at 1.87 GHz and
+// 1,275 W of the card's 1,400.  The plain attention's kernels, at the same clock: 0.73 and 0.31, 0.78 and 0.37.  Two waves a SIMD leave a lane 256 registers: 128 hold dK and dV, 32
 // K; with V's 32 as well the rest spills (11 ms), so V waits in LDS, where reading it takes less time than the products that use it.  One
 // wave a SIMD with everything in registers is slower though it reads LDS less (48 keys a wave: 6.6 ms against 5.9), because a wave by itself
 // overlaps little of its exponents and roundings with its products; a block of eight waves sharing a tile waits at its barriers (6.2).
-// 62,400 x 12 heads, 8 groups: dK, dV and dQ in one launch 10.5 ms, 1.0 PFLOP/s of 7 products of 256 operations a pair of rows (a library's
-// square bf16 product reaches 1.17 on this card).
+// 62,400 x 12 heads, 8 groups: dK, dV and dQ in one launch 10.6 ms, 1.05 PFLOP/s of 7 products of 256 operations a pair of rows (plain attention's
+// backward executes 1.3 on the same card).
 #pragma once
 
 #include "diff_attn.h"

@@ -2,8 +2,9 @@
 //
 // With a step's vector work all between its products, two waves overlap little: a step took the sum of its products' and its vector
 // work's cycles.  Here the vector work of one group of products lies among the next ones; fragments are read two ahead, and only
-// vector instructions may cross a group.  62,400 x 12 heads, 8 groups 4.5 -> 4.25 ms (1.06 PFLOP/s of 768 operations a pair; a library's square
-// product reaches 1.17), 32,760 x 12, 8 groups 1.46 -> 1.27.  Bound by the matrix cores and the power they draw.  32 queries a wave: an
+// vector instructions may cross a group.  62,400 x 12 heads, 8 groups 4.5 -> 4.25 ms, 32,760 x 12, 8 groups 1.46 -> 1.27 (4.3 and 1.31 on another
+// card; 1.11 PFLOP/s of 768 operations a pair, where plain attention's forward executes 1.3).  Bound by both kinds of work of a SIMD: matrix products 0.59 of the cycles,
+// vector instructions 0.54 (two exponents for every three products, one for two in plain attention), at 1.82 GHz and 1,312 W of 1,400.  32 queries a wave: an
 // accumulator of 16 more would not fit beside two maps' sums of V, and 16 would read every fragment for half the products.  A block of
 // eight waves was slower (4.5 ms).
 #pragma once

@@ -51,8 +51,8 @@ __device__ __forceinline__ void from_f32(float& d, float v) { d = v; }
 __device__ __forceinline__ void from_f32(unsigned short& d, float v) { d = f32_to_bf16_bits(v); }
 
 // Columns col .. col + V - 1 of a row of C, as they lie there, with the next row's first ones past its end (clear_past); zeros past the last row's.
-// Element by element, in every row's last piece, the loads would be waited for where they are issued: 4,099 x 1535 backward bf16 44 us
-// instead of 32, fp32 31 instead of 27.
+// Element by element, in every row's last piece, the loads would be waited for where they are issued: 4,099 x 1535 backward (a call of two
+// launches) bf16 44 us instead of 32, fp32 31 instead of 28.
 template <typename T>
 __device__ __forceinline__ Bytes16<T> load_part(const T* __restrict__ row, int col, int C, bool last_row) {
   constexpr int V = kPer16<T>;

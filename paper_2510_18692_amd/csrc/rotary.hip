@@ -11,9 +11,10 @@
 //
 // Bound by HBM: every chunk of 16 bytes is read and written once, by a lane of its own, so that loads and stores are whole rows.  A lane of the
 // half layout reads its partner's chunk too, from L1; one lane for both partners halves those loads but splits every row's traffic in two:
-// 32,760 x 12 heads of 128, 96 channels turned, bf16, into sorted order 139 us against 128, back 149 against 139 (4.7 and 4.3 TB/s; gathering
-// rows without turning them takes 111).  Three chunks of a lane in flight together were slower everywhere (149, 156; fewer waves fit).
-// 99,840 x 40 heads of q and k in token order, neighbours, three axes, bf16: 0.72 ms (5.7 TB/s).
+// 32,760 x 12 heads of 128, 96 channels turned, bf16, into sorted order 139 us against 128, back 149 against 139.  Three chunks of a lane in
+// flight together were slower everywhere (149, 156; fewer waves fit).  By itself each launch takes 132 and 140 us (4.6 and 4.3 TB/s), in maps of 64
+// channels 132 and 141, in fp32 265 and 273; the call that moves the same rows back without turning them 122, this one 144.  In token order,
+// neighbours, three axes, 99,840 x 40 heads of q and k, bf16 0.73 ms (5.6 TB/s), 49,920 x 40, fp32 0.76 (5.4).
 #include <algorithm>
 #include <cmath>
 
