@@ -1080,9 +1080,9 @@ std::tuple<Tensor, Tensor, Tensor> diff_attention(const Tensor& x, const Tensor&
                                                   const OptTensor& pos, const OptTensor& freq, const std::vector<int64_t>& pairs,
                                                   bool interleaved, double factor) {
   // the two maps' sums of V are the backward's: 8 bytes a channel and row
-  bool train = false;
-  if (at::GradMode::is_enabled())
-    for (const Tensor* t : {&x, &w, &q, &k, &v, &lam}) train = train || t->requires_grad();
+  bool train = freq && freq->requires_grad();   // which gets no gradient, but a backward runs
+  for (const Tensor* t : {&x, &w, &q, &k, &v, &lam}) train = train || t->requires_grad();
+  train = train && at::GradMode::is_enabled();
   auto r = DiffAttention::apply(x, w, q, k, v, lam, scale, alpha, grad_x, pos, freq, pairs, interleaved, factor, train);
   return {r[0], r[1], r[2]};
 }

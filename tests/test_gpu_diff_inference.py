@@ -51,3 +51,15 @@ def test_one_leaf_is_enough_for_a_backward(leaf):
     o, _, _ = moga_diff_attention(*t, 0.125)
     o.float().square().sum().backward()
     assert torch.equal(t[leaf].grad, all_of_them[leaf].grad)
+
+
+def test_frequencies_that_ask_for_a_gradient():
+    """They get none, but autograd runs the backward for them."""
+    from paper_2510_18692_amd import binding as mg
+    N, H = 200, 2
+    t = _inputs(N, H)
+    freq = mg.moga_rotary_freqs(64)[0].requires_grad_()
+    pos = torch.arange(N, dtype=torch.int32, device="cuda")
+    o, _, _ = moga_diff_attention(*t, 0.125, positions=pos, inv_freq=freq)
+    o.float().sum().backward()
+    assert freq.grad is None
