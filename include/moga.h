@@ -50,6 +50,9 @@ typedef enum {
 
 typedef enum { MOGA_F32 = 0, MOGA_BF16 = 1 } moga_dtype;
 
+typedef enum { MOGA_NORM_NONE = 0, MOGA_NORM_RMS = 1, MOGA_NORM_LAYER = 2 } moga_norm;        /* moga_residual_norm_* */
+typedef enum { MOGA_ACT_SILU = 0, MOGA_ACT_GELU = 1, MOGA_ACT_GELU_TANH = 2 } moga_activation; /* moga_gated_ffn_* */
+
 typedef enum {
   MOGA_OP_ROUTE = 0,
   MOGA_OP_PERMUTE = 1,
@@ -64,7 +67,10 @@ typedef enum {
   MOGA_OP_FUSED_ATTN_BWD = 10, /* moga_fused_attn_bwd (the bytes of MOGA_OP_ATTN_BWD) */
   MOGA_OP_DIFF_ATTN_FWD = 11,  /* N = Nq, M = G */
   MOGA_OP_DIFF_ATTN_BWD = 12,  /* N = Nq, M = G */
-  MOGA_OP_LAYER_NORM_BWD = 13  /* M = 1, d_model = C */
+  MOGA_OP_LAYER_NORM_BWD = 13, /* M = 1, d_model = C */
+  MOGA_OP_RESIDUAL_NORM_BWD = 14, /* M = rows of gate, scale and shift (1 without them), d_model = C */
+  MOGA_OP_GATED_FFN_FWD = 15,  /* M = 1, d_model = C, D = F */
+  MOGA_OP_GATED_FFN_BWD = 16   /* M = 1, d_model = C, D = F */
 } moga_op;
 
 /* Human-readable name of a status code (static storage, never NULL). */
@@ -563,6 +569,56 @@ int moga_layer_norm_fwd(const void* x, int dtype, const float* weight_or_null, c
 int moga_layer_norm_bwd(const void* d_y, const void* x, int dtype, const float* weight_or_null, const float* mean, const float* rstd,
                         int64_t N, int C, void* d_x, float* d_weight_or_null, float* d_bias_or_null, void* ws, size_t ws_bytes,
                         void* stream);
+
+/*
+ * The residual sum of a block, with its gate, and the norms before and after it (any C in [1, 16384]):
+ *   z = post(y) * post_weight;  r = x + residual_scale * gate * z;  h = (pre(r) * weight + bias) * (1 + scale) + shift
+ * post and pre: MOGA_NORM_RMS v / sqrt(mean_c v^2 + eps), MOGA_NORM_LAYER (v - mean_c v) / sqrt(mean_c (v - mean_c v)^2 + eps), or MOGA_NORM_NONE:
+ * z = y, or no h at all.  The sum that a block's output goes into and the norm that the next block reads are one pass over the tokens.
+ * Without y (NULL) r is x itself: h = pre(x) ... alone, r is not written, and post is NONE.
+ *   x, r [N, C] of x_dtype; y, h [N, C] of y_dtype: both F32, both BF16, or x F32 and y BF16 (a residual stream kept in 32 bits).
+ *   post_weight, weight, bias [C] fp32; gate, scale, shift [rows, C] fp32, each NULL for none: token n goes by row n / tokens_per_row (>= 1), rows =
+ *   the next whole number above N / tokens_per_row (one conditioning for all tokens: tokens_per_row >= N).  eps finite and >= 0, residual_scale finite.
+ * stats [4, N] fp32 (NULL where no backward follows): mean and 1 / deviation of y's rows, then of r's.
+ * fp32 statistics and sums; h comes from the unrounded r, r and h are rounded once.  N < 2^31.
+ */
+typedef struct {
+  const void *x, *y;
+  const float *gate, *post_weight, *weight, *bias, *scale, *shift;
+  int64_t N, tokens_per_row;
+  int C, x_dtype, y_dtype, post, pre;
+  float residual_scale, eps;
+} moga_residual_norm;   /* in host memory; its pointers are device pointers */
+int moga_residual_norm_fwd(const moga_residual_norm* args, void* r, void* h, float* stats_or_null, void* stream);
+
+/*
+ * Backward of moga_residual_norm_fwd, of the same args and its stats (x and y are read again; r is not needed).  d_h [N, C] of y_dtype: with a norm
+ * pre, and only then; d_r [N, C] of x_dtype, the gradient of r by its other uses, or NULL for zeros (without y: what is added to d_x).
+ *   d_x [N, C] of x_dtype, d_y [N, C] of y_dtype (with y);  d_gate, d_scale, d_shift [rows, C], d_post_weight, d_weight, d_bias [C] fp32, each NULL to
+ *   skip (and NULL for a parameter that is NULL); of N == 0 tokens zeros (one row).  Sums in a fixed order: results repeat bit by bit.
+ * Workspace: MOGA_OP_RESIDUAL_NORM_BWD (not needed without the parameters' gradients).
+ */
+int moga_residual_norm_bwd(const moga_residual_norm* args, const float* stats, const void* d_r_or_null, const void* d_h, void* d_x, void* d_y,
+                           float* d_gate_or_null, float* d_post_weight_or_null, float* d_weight_or_null, float* d_bias_or_null,
+                           float* d_scale_or_null, float* d_shift_or_null, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Gated feed-forward:  [a, u] = x W_in^T,  h = act(a) * u,  y = h W_out^T
+ * x, y [N, C], w_in [2 F, C] (the F rows of a, then the F rows of u), w_out [C, F], h [N, F]; all of dtype F32 or BF16, C <= 65536 and F <= 262144
+ * multiples of 8 (F32: of 4), N < 2^31.  act: silu a / (1 + e^-a), gelu a (1 + erf(a / sqrt 2)) / 2, or gelu's tanh form.
+ * h is written in any case (the second product reads it); au [N, 2 F] = [a, u] for a backward, else NULL.  fp32 sums; h is taken from the unrounded a
+ * and u, and a, u, h and y are rounded once.  Results repeat bit by bit.  Workspace: MOGA_OP_GATED_FFN_FWD.
+ */
+int moga_gated_ffn_fwd(const void* x, const void* w_in, const void* w_out, int dtype, int64_t N, int C, int F, int activation, void* h,
+                       void* au_or_null, void* y, void* ws, size_t ws_bytes, void* stream);
+/*
+ * Backward of moga_gated_ffn_fwd, from its au and h:  dh = d_y W_out,  da = dh * u * act'(a),  du = dh * act(a) (rounded once),
+ *   d_x = [da, du] W_in;  d_w_in = [da, du]^T x;  d_w_out = d_y^T h        each like what it is the gradient of, each NULL to skip
+ * of N == 0 tokens the weights' gradients are zeros.  Workspace: MOGA_OP_GATED_FFN_BWD (it holds [da, du]).
+ */
+int moga_gated_ffn_bwd(const void* d_y, const void* x, const void* w_in, const void* w_out, const void* au, const void* h, int dtype, int64_t N,
+                       int C, int F, int activation, void* d_x_or_null, void* d_w_in_or_null, void* d_w_out_or_null, void* ws, size_t ws_bytes,
+                       void* stream);
 
 /*
  * Rotary positions.  The first R channels of a head (R even, R <= D; the others are copied) are R / 2 pairs: channels (2 i, 2 i + 1) if

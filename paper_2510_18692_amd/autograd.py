@@ -8,7 +8,7 @@ balancing loss when it is used); the assignment itself is a constant of differen
 gradient is returned for the router input x unless `grad_x=True` (the optional dX of the router
 backward).  Everything runs in the HIP library; the autograd function itself is native
 (csrc/torch_binding.cpp), so that the backward pass does not enter the interpreter.
-`layer_norm`, `rotary` and `moga_diff_attention` have first derivatives only: gradients taken with
+`layer_norm`, `residual_norm`, `gated_ffn`, `rotary` and `moga_diff_attention` have first derivatives only: gradients taken with
 create_graph=True raise an error where they are differentiated again.
 """
 from __future__ import annotations
@@ -25,6 +25,19 @@ def moga_attention(x, w, q, k, v, softmax_scale, balance_alpha=None, grad_x=Fals
 def layer_norm(x, weight=None, bias=None, eps=1e-6):
     """Layer norm over the last axis of x [..., C] (contiguous), weight and bias f32 [C] or None -> y like x."""
     return mg._nat.layer_norm(x, weight, bias, eps)
+
+
+def residual_norm(x, y=None, gate=None, post_weight=None, weight=None, bias=None, scale=None, shift=None, post="none", pre="layer", residual_scale=1.0,
+                  tokens_per_row=None, eps=1e-6, dtype=None):
+    """r = x + residual_scale * gate * post(y) * post_weight, and h = (pre(r) * weight + bias) * (1 + scale) + shift, in one pass
+    (binding.moga_residual_norm_fwd): x, y [..., C] (contiguous) -> (r, which is x without y; h, None without pre)."""
+    return mg._nat.residual_norm(x, y, gate, post_weight, weight, bias, scale, shift, mg._one_of(mg.NORMS, post, "post"),
+                                 mg._one_of(mg.NORMS, pre, "pre"), residual_scale, tokens_per_row, eps, dtype)
+
+
+def gated_ffn(x, w_in, w_out, activation="silu"):
+    """(act(a) * u) w_out^T with [a, u] = x w_in^T: x [..., C] (contiguous), w_in [2 F, C], w_out [C, F] (binding.moga_gated_ffn_fwd) -> y like x."""
+    return mg._nat.gated_ffn(x, w_in, w_out, mg._one_of(mg.ACTIVATIONS, activation, "activation"))
 
 
 def rotary(q, k, positions, inv_freq, axis_pairs=None, interleaved=False, factor=1.0, maps=1):

@@ -14,6 +14,7 @@ import importlib.machinery
 import importlib.util
 import os
 import threading
+import typing
 
 import torch
 
@@ -21,10 +22,12 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmoga.so")
 
 MOGA_F32, MOGA_BF16 = 0, 1
+NORMS = {"none": 0, "rms": 1, "layer": 2}
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
 ROTARY_SCALINGS = {None: 0, "linear": 1, "base": 2, "parts": 3}
 (OP_ROUTE, OP_PERMUTE, OP_ATTN_FWD, OP_ATTN_BWD, OP_ROUTE_BWD, OP_BALANCE_LOSS, OP_VARLEN_ATTN_FWD,
  OP_VARLEN_ATTN_BWD, OP_ATTN_BWD_JOINT, OP_ATTN_FWD_CALL, OP_FUSED_ATTN_BWD, OP_DIFF_ATTN_FWD, OP_DIFF_ATTN_BWD,
- OP_LAYER_NORM_BWD) = range(14)
+ OP_LAYER_NORM_BWD, OP_RESIDUAL_NORM_BWD, OP_GATED_FFN_FWD, OP_GATED_FFN_BWD) = range(17)
 
 _c = ctypes
 _vp, _i64, _i32, _f32, _sz = _c.c_void_p, _c.c_int64, _c.c_int, _c.c_float, _c.c_size_t
@@ -110,6 +113,10 @@ _SIGNATURES = {
     "moga_diff_attn_fwd": (_i32, [_vp, _vp, _vp, _i32, _i64, _i64, _i32, _i32, _vp, _vp, _vp, _i32, _f32, _vp, _vp, _vp, _vp, _sz, _vp]),
     "moga_diff_attn_bwd": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i64, _i64, _i32, _i32, _vp, _vp, _vp, _i32, _f32, _vp, _vp, _vp,
                                   _vp, _vp, _sz, _vp]),
+    "moga_residual_norm_fwd": (_i32, [_vp, _vp, _vp, _vp, _vp]),
+    "moga_residual_norm_bwd": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "moga_gated_ffn_fwd": (_i32, [_vp, _vp, _vp, _i32, _i64, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "moga_gated_ffn_bwd": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i64, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp]),
 }
 EXPORTS = tuple(_SIGNATURES)
 
@@ -441,6 +448,53 @@ def moga_layer_norm_fwd(x, weight=None, bias=None, eps=1e-6, want_stats=True, st
 def moga_layer_norm_bwd(d_y, x, weight, mean, rstd, want_dw=True, stream=None):
     """-> (d_x [N, C], d_weight f32 [C] | None, d_bias f32 [C] | None)"""
     return _nat.layer_norm_bwd(d_y, x, weight, mean, rstd, want_dw, _st(stream))
+
+
+def _one_of(table, key, name):
+    if key not in table:
+        raise ValueError(f"{name} {key!r}: one of {list(table)}")
+    return table[key]
+
+
+class ResidualNormGrads(typing.NamedTuple):
+    d_x: torch.Tensor
+    d_y: typing.Optional[torch.Tensor]
+    d_gate: typing.Optional[torch.Tensor]
+    d_post_weight: typing.Optional[torch.Tensor]
+    d_weight: typing.Optional[torch.Tensor]
+    d_bias: typing.Optional[torch.Tensor]
+    d_scale: typing.Optional[torch.Tensor]
+    d_shift: typing.Optional[torch.Tensor]
+
+
+def moga_residual_norm_fwd(x, y=None, gate=None, post_weight=None, weight=None, bias=None, scale=None, shift=None, post="none", pre="layer",
+                           residual_scale=1.0, tokens_per_row=None, eps=1e-6, dtype=None, want_stats=True, stream=None):
+    """r = x + residual_scale * gate * post(y) * post_weight; h = (pre(r) * weight + bias) * (1 + scale) + shift.  x [N, C], y [N, C] or None (then
+    r is x); post and pre "none", "rms" or "layer"; post_weight, weight, bias f32 [C]; gate, scale, shift f32 [rows, C], where token n goes by row
+    n // tokens_per_row (None: one row for all); dtype of h where there is no y (default x's)
+    -> (r like x | None without y, h like y | None without pre, stats f32 [4, N] | None)"""
+    return _nat.residual_norm_fwd(x, y, gate, post_weight, weight, bias, scale, shift, _one_of(NORMS, post, "post"), _one_of(NORMS, pre, "pre"),
+                                  residual_scale, tokens_per_row, eps, dtype, want_stats, _st(stream))
+
+
+def moga_residual_norm_bwd(d_r, d_h, x, stats, y=None, gate=None, post_weight=None, weight=None, bias=None, scale=None, shift=None, post="none",
+                           pre="layer", residual_scale=1.0, tokens_per_row=None, eps=1e-6, want_params=True, stream=None):
+    """d_r [N, C] (None: zeros; without y: what is added to d_x), d_h [N, C] (None without pre) -> ResidualNormGrads, whose parts are None where the
+    argument was None; want_params=False skips those of the parameters."""
+    return ResidualNormGrads(*_nat.residual_norm_bwd(d_r, d_h, x, stats, y, gate, post_weight, weight, bias, scale, shift, _one_of(NORMS, post, "post"),
+                                                     _one_of(NORMS, pre, "pre"), residual_scale, tokens_per_row, eps, want_params, _st(stream)))
+
+
+def moga_gated_ffn_fwd(x, w_in, w_out, activation="silu", want_saved=True, stream=None):
+    """[a, u] = x w_in^T, h = act(a) * u, y = h w_out^T.  x [N, C], w_in [2 F, C], w_out [C, F]; activation "silu", "gelu" or "gelu_tanh"
+    -> (y [N, C], [a, u] [N, 2 F] | None, h [N, F] | None)"""
+    return _nat.gated_ffn_fwd(x, w_in, w_out, _one_of(ACTIVATIONS, activation, "activation"), want_saved, _st(stream))
+
+
+def moga_gated_ffn_bwd(d_y, x, w_in, w_out, au, h, activation="silu", want_dx=True, want_dw_in=True, want_dw_out=True, stream=None):
+    """-> (d_x [N, C] | None, d_w_in [2 F, C] | None, d_w_out [C, F] | None), each like what it is the gradient of"""
+    return _nat.gated_ffn_bwd(d_y, x, w_in, w_out, au, h, _one_of(ACTIVATIONS, activation, "activation"), want_dx, want_dw_in, want_dw_out,
+                              _st(stream))
 
 
 def moga_rotary_freqs(rot_dims, base=10000.0, scaling=None, scale_factor=1.0, original_len=0.0, beta_fast=32.0, beta_slow=1.0, device="cuda"):

@@ -15,7 +15,7 @@ LIB = os.path.join(HERE, "libmoga.so")
 BENCH_LIB = os.path.join(HERE, "libmoga_bench.so")   # peak microbenchmarks for bench.py only
 EXAMPLE = os.path.join(HERE, "c_abi_example")
 SOURCES = ["api.hip", "route.hip", "permute.hip", "attn_fwd.hip", "attn_bwd.hip", "balance.hip", "static_index.hip",
-           "layer_norm.hip", "rotary.hip", "diff_attn.hip"]
+           "layer_norm.hip", "rotary.hip", "diff_attn.hip", "residual_norm.hip", "gated_ffn.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=default",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",   # no packed-fp32 VALU ops

@@ -12,6 +12,9 @@ extern "C" size_t moga_varlen_attn_bwd_ws_bytes(int64_t Nq, int H, int G);
 extern "C" size_t moga_diff_attn_fwd_ws_bytes(int G);
 extern "C" size_t moga_diff_attn_bwd_ws_bytes(int64_t Nq, int H, int G);
 extern "C" size_t moga_layer_norm_bwd_ws_bytes(int64_t N, int C, int dtype);
+extern "C" size_t moga_residual_norm_bwd_ws_bytes(int64_t N, int M, int C);
+extern "C" size_t moga_gated_ffn_fwd_ws_bytes(int64_t N, int C, int F, int dtype);
+extern "C" size_t moga_gated_ffn_bwd_ws_bytes(int64_t N, int C, int F, int dtype);
 
 extern "C" const char* moga_status_string(int status) {
   switch (status) {
@@ -24,7 +27,7 @@ extern "C" const char* moga_status_string(int status) {
   }
 }
 
-extern "C" int moga_version(void) { return 106; }
+extern "C" int moga_version(void) { return 107; }
 
 // Test hook: overrides the mean group size below which the bf16 attention calls pick their
 // small-group kernels (negative: each call's own default).
@@ -53,6 +56,9 @@ extern "C" size_t moga_workspace_bytes(int op, int64_t N, int H, int D, int M, i
     case MOGA_OP_DIFF_ATTN_FWD: return moga_diff_attn_fwd_ws_bytes(M);
     case MOGA_OP_DIFF_ATTN_BWD: return moga_diff_attn_bwd_ws_bytes(N, H, M);
     case MOGA_OP_LAYER_NORM_BWD: return moga_layer_norm_bwd_ws_bytes(N, d_model, dtype);
+    case MOGA_OP_RESIDUAL_NORM_BWD: return moga_residual_norm_bwd_ws_bytes(N, M, d_model);
+    case MOGA_OP_GATED_FFN_FWD: return moga_gated_ffn_fwd_ws_bytes(N, d_model, D, dtype);
+    case MOGA_OP_GATED_FFN_BWD: return moga_gated_ffn_bwd_ws_bytes(N, d_model, D, dtype);
     default: return 0;
   }
 }

@@ -1,0 +1,527 @@
+// Gated feed-forward, forward and backward.
+//
+//   [a, u] = x W_in^T,  h = act(a) u,  y = h W_out^T
+//   dh = d_y W_out,  da = dh u act'(a),  du = dh act(a),  d_x = [da, du] W_in,  d_W_in = [da, du]^T x,  d_W_out = d_y^T h
+#include <algorithm>
+#include <cmath>
+
+#include "matmul_tiles.h"
+
+namespace moga {
+namespace {
+
+constexpr int kFfnMaxC = 65536, kFfnMaxF = 262144;
+
+// ---- the activation ----
+template <typename T> __device__ __forceinline__ float exp_neg(float v);   // e^-v
+template <> __device__ __forceinline__ float exp_neg<unsigned short>(float v) { return fast_exp2(v * -1.4426950408889634f); }
+template <> __device__ __forceinline__ float exp_neg<float>(float v) { return expf(-v); }
+template <typename T> __device__ __forceinline__ float inverse(float v);
+template <> __device__ __forceinline__ float inverse<unsigned short>(float v) { return __builtin_amdgcn_rcpf(v); }
+template <> __device__ __forceinline__ float inverse<float>(float v) { return 1.f / v; }
+
+// act(a) and act'(a).  tanh's form is a sigmoid: (1 + tanh v) / 2 = 1 / (1 + e^-2v).
+template <typename T>
+__device__ __forceinline__ void activate(int act, float a, float& f, float& slope) {
+  if (act == MOGA_ACT_SILU) {
+    const float p = inverse<T>(1.f + exp_neg<T>(a));
+    f = a * p;
+    slope = fmaf(f, 1.f - p, p);
+  } else if (act == MOGA_ACT_GELU) {
+    const float p = 0.5f + 0.5f * erff(a * 0.70710678118654752f);
+    f = a * p;
+    slope = fmaf(a * 0.39894228040143268f, exp_neg<T>(0.5f * a * a), p);
+  } else {
+    constexpr float k = 1.5957691216057308f, c = 0.044715f;   // 2 sqrt(2 / pi)
+    const float a2 = a * a, p = inverse<T>(1.f + exp_neg<T>(k * a * fmaf(c, a2, 1.f)));
+    f = a * p;
+    slope = fmaf(f * (1.f - p), k * fmaf(3.f * c, a2, 1.f), p);
+  }
+}
+
+// ---- tiles ----
+enum Kind { kPlain, kGated, kGatedBwd };
+
+template <typename T>
+struct Product {
+  const T *a, *b;        // A(m, k), B(n, k)
+  int64_t lda, ldb;
+  int64_t M;
+  int N, act;            // kGated: N = F, b [2 F][ldb]
+  int64_t K;
+  T* c;                  // [M][N]; kGated: h; kGatedBwd: [da, du], [M][2 N]
+  T* c2;                 // kGated: [a, u], [M][2 N], or NULL
+  const T* saved;        // kGatedBwd: [a, u]
+  float* part;           // of split products: [split][M][N], or NULL
+  int64_t k_each;        // k of a split
+  unsigned tiles_m, tiles_n;
+};
+
+template <typename T> __device__ __forceinline__ void store4(T* p, floatx4_t v);
+template <> __device__ __forceinline__ void store4<float>(float* p, floatx4_t v) { *(floatx4_t*)p = v; }
+
+__device__ __forceinline__ uintx2_t pack4(floatx4_t v) { return uintx2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}; }
+// Lane group g holds columns 4 g .. 4 g + 3 of two neighbouring tiles, and gets eight neighbouring columns from column() on.
+__device__ __forceinline__ int pair_column(int g) { return (g & 1) * 16 + (g >> 1) * 8; }
+__device__ __forceinline__ uintx4_t pair_up(uintx2_t p, uintx2_t q) {
+  const auto x = __builtin_amdgcn_permlane16_swap(p[0], q[0], false, false), y = __builtin_amdgcn_permlane16_swap(p[1], q[1], false, false);
+  return uintx4_t{x[0], y[0], x[1], y[1]};
+}
+__device__ __forceinline__ void pair_up(floatx4_t p, floatx4_t q, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(p[i]), __float_as_uint(q[i]), false, false);
+    v[i] = __uint_as_float(x[0]);
+    v[4 + i] = __uint_as_float(x[1]);
+  }
+}
+
+// Two neighbouring tiles of a row of C, rounded once: 16 bytes a lane at p + column.
+__device__ __forceinline__ void put_pair(unsigned short* row, int col, int g, int64_t N, floatx4_t p, floatx4_t q) {
+  const uintx4_t v = pair_up(pack4(p), pack4(q));
+  col += pair_column(g);
+  if (col < N) *(uintx4_t*)(row + col) = v;
+}
+__device__ __forceinline__ void put_pair(float* row, int col, int g, int64_t N, floatx4_t p, floatx4_t q) {
+  col += 4 * g;
+  if (col < N) *(floatx4_t*)(row + col) = p;
+  if (col + 16 < N) *(floatx4_t*)(row + col + 16) = q;
+}
+
+__device__ __forceinline__ void grad_pair(const unsigned short* saved, unsigned short* out, int64_t F, int col, int g, int act, floatx4_t p, floatx4_t q) {
+  float dh[8];
+  pair_up(p, q, dh);
+  col += pair_column(g);
+  if (col >= F) return;
+  const uintx4_t a4 = *(const uintx4_t*)(saved + col), u4 = *(const uintx4_t*)(saved + F + col);
+  uintx4_t da4, du4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float f0, s0, f1, s1;
+    activate<unsigned short>(act, bf16_lo_to_f32(a4[i]), f0, s0);
+    activate<unsigned short>(act, bf16_hi_to_f32(a4[i]), f1, s1);
+    da4[i] = pack_bf16x2(dh[2 * i] * bf16_lo_to_f32(u4[i]) * s0, dh[2 * i + 1] * bf16_hi_to_f32(u4[i]) * s1);
+    du4[i] = pack_bf16x2(dh[2 * i] * f0, dh[2 * i + 1] * f1);
+  }
+  *(uintx4_t*)(out + col) = da4;
+  *(uintx4_t*)(out + F + col) = du4;
+}
+__device__ __forceinline__ void grad_pair(const float* saved, float* out, int64_t F, int col, int g, int act, floatx4_t p, floatx4_t q) {
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int at = col + 16 * t + 4 * g;
+    if (at >= F) return;
+    const floatx4_t dh = t ? q : p, a = *(const floatx4_t*)(saved + at), u = *(const floatx4_t*)(saved + F + at);
+    floatx4_t da, du;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float f, s;
+      activate<float>(act, a[i], f, s);
+      da[i] = dh[i] * u[i] * s;
+      du[i] = dh[i] * f;
+    }
+    *(floatx4_t*)(out + at) = da;
+    *(floatx4_t*)(out + F + at) = du;
+  }
+}
+
+// WM x WN waves, TM x TN tiles of 16 each
+template <typename T, Kind KIND, bool A_KFIRST, bool B_KFIRST, int WM, int WN, int TM, int TN>
+__global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void product_kernel(const Product<T> p) {
+  constexpr int THREADS = 64 * WM * WN, BM = 16 * WM * TM, BN = 16 * WN * TN;
+  using OpA = Operand<T, A_KFIRST, BM, THREADS, TM>;
+  using OpB = Operand<T, B_KFIRST, BN, THREADS, TN>;
+  constexpr int BK = OpA::BK;
+  constexpr unsigned kStage = OpA::kBytes + OpB::kBytes;
+  __shared__ __attribute__((aligned(1024))) unsigned char s_mem[2 * kStage];
+  const unsigned lds = lds_addr_uniform(s_mem);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
+
+  // tiles in panels of 8 rows of tiles, down a panel's columns
+  const unsigned tiles = p.tiles_m * p.tiles_n, split = blockIdx.x / tiles;
+  unsigned b = xcd_order(blockIdx.x % tiles, tiles);
+  const unsigned panel = b / (8 * p.tiles_n), in = b - panel * 8 * p.tiles_n, high = min(8u, p.tiles_m - panel * 8);
+  const unsigned bm = panel * 8 + in % high, bn = in / high;
+
+  const int64_t m0 = (int64_t)bm * BM, k0 = split * p.k_each;
+  const int n0 = bn * (KIND == kGated ? BN / 2 : BN), k_count = (int)min(p.k_each, p.K - k0);
+  constexpr bool PAIRED = KIND == kGated;
+  OpA oa;
+  OpB ob;
+  oa.init(p.a, p.lda, m0, p.M, k0, k_count, wm * TM);
+  if constexpr (PAIRED) ob.init_paired(p.b, p.ldb, n0, p.N, k_count, wn * TN);
+  else ob.init(p.b, p.ldb, n0, p.N, k0, k_count, wn * TN);
+
+  auto stage = [&](unsigned at) {
+#pragma unroll
+    for (int i = 0; i < OpA::L; ++i) oa.stage(at, i);
+#pragma unroll
+    for (int i = 0; i < OpB::L; ++i) ob.template stage<PAIRED>(at + OpA::kBytes, i);
+    oa.advance();
+    ob.template advance<PAIRED>();
+  };
+
+  floatx4_t acc[TM][TN];
+#pragma unroll
+  for (int m = 0; m < TM; ++m)
+#pragma unroll
+    for (int n = 0; n < TN; ++n) acc[m][n] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+
+  const int steps = (k_count + BK - 1) / BK;
+  stage(lds);
+  unsigned at = lds, other = lds + kStage;
+  for (int s = 0; s < steps; ++s) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (s + 1 < steps) stage(other);
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      Frag<T> fa[TM], fb[TN];
+#pragma unroll
+      for (int n = 0; n < TN; ++n) fb[n] = ob.get(at + OpA::kBytes, n, kk);
+#pragma unroll
+      for (int m = 0; m < TM; ++m) fa[m] = oa.get(at, m, kk);
+#pragma unroll
+      for (int m = 0; m < TM; ++m)
+#pragma unroll
+        for (int n = 0; n < TN; ++n) acc[m][n] = mfma_frag(fb[n], fa[m], acc[m][n]);
+    }
+    const unsigned t = at;
+    at = other;
+    other = t;
+  }
+
+  // lane: row r of a tile, columns 4 g .. 4 g + 3
+  const int r = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+  const int64_t N = p.N;
+#pragma unroll
+  for (int m = 0; m < TM; ++m) {
+    const int64_t row = m0 + (wm * TM + m) * 16 + r;
+    const bool ok = row < p.M;
+    if constexpr (KIND == kPlain) {
+      const int col = n0 + wn * TN * 16;
+      if (p.part) {
+        float* out = p.part + ((int64_t)split * p.M + row) * N;
+#pragma unroll
+        for (int n = 0; n < TN; ++n)
+          if (ok && col + 16 * n + 4 * g < N) *(floatx4_t*)(out + col + 16 * n + 4 * g) = acc[m][n];
+      } else {
+#pragma unroll
+        for (int n = 0; n < TN; n += 2) put_pair(p.c + row * N, col + 16 * n, g, ok ? N : 0, acc[m][n], acc[m][n + 1]);
+      }
+    } else if constexpr (KIND == kGated) {
+      const int col = n0 + wn * TN * 8;
+      static_assert(TN == 4);
+      floatx4_t h[2];
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float f, slope;
+          activate<T>(p.act, acc[m][n][i], f, slope);
+          h[n][i] = f * acc[m][n + 2][i];
+        }
+      put_pair(p.c + row * N, col, g, ok ? N : 0, h[0], h[1]);
+      if (p.c2) {
+        put_pair(p.c2 + row * 2 * N, col, g, ok ? N : 0, acc[m][0], acc[m][1]);
+        put_pair(p.c2 + row * 2 * N + N, col, g, ok ? N : 0, acc[m][2], acc[m][3]);
+      }
+    } else {
+      const int col = n0 + wn * TN * 16;
+#pragma unroll
+      for (int n = 0; n < TN; n += 2)
+        grad_pair(p.saved + (ok ? row : 0) * 2 * N, p.c + (ok ? row : 0) * 2 * N, ok ? N : 0, col + 16 * n, g, p.act, acc[m][n], acc[m][n + 1]);
+    }
+  }
+}
+
+
+// Sums of the splits, in their order, rounded once.
+template <typename T>
+__global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ part, int splits, int64_t n, T* __restrict__ c) {
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * 1024) {
+    floatx4_t s = *(const floatx4_t*)(part + i);
+#pragma unroll 4
+    for (int k = 1; k < splits; ++k) s += *(const floatx4_t*)(part + k * n + i);
+    if constexpr (sizeof(T) == 4) *(floatx4_t*)(c + i) = s;
+    else *(uintx2_t*)(c + i) = pack4(s);
+  }
+}
+
+// ---- few tokens ----
+// A block owns 16 columns of C (GATED: 16 of a and the same 16 of u) for up to 16 TT tokens.  Its waves take turns of 128 bytes of k, so that a weight
+// is read once, a line at a time, and their sums meet in LDS.  Loads past k, F or the last token give zeros (buffer bounds).
+template <typename T, bool GATED, int TT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void few_kernel(const Product<T> p) {
+  constexpr int ES = sizeof(T), V = 16 / ES, SETS = GATED ? 2 : 1, U = TT == 1 ? 4 : 2;
+  __shared__ floatx4_t s_sum[WAVES][SETS * TT][64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, r = l & 15, g = l >> 4;
+  const int n0 = blockIdx.x * 16, N = p.N;
+  const int row_bytes = (int)(p.K * ES);
+  auto rsrc = [](const T* base) { return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)kBufferBytes, 0x00020000); };
+  const auto ra = rsrc(p.a);
+  const auto rb = rsrc(p.b + (int64_t)n0 * p.ldb), rb2 = rsrc(p.b + ((int64_t)N + n0) * p.ldb);
+  const unsigned vb = n0 + r < N ? r * row_bytes + g * 16 : kPastBuffer;
+  unsigned va[TT];
+#pragma unroll
+  for (int t = 0; t < TT; ++t) va[t] = 16 * t + r < p.M ? (16 * t + r) * row_bytes + g * 16 : kPastBuffer;
+  floatx4_t acc[SETS][TT];
+#pragma unroll
+  for (int s = 0; s < SETS; ++s)
+#pragma unroll
+    for (int t = 0; t < TT; ++t) acc[s][t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+  for (int k = wave * 128; k < row_bytes; k += WAVES * 128 * U) {
+    Frag<T> fb[U][2][SETS], fa[U][2][TT];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int at = k + u * WAVES * 128 + h * 64;
+        const bool in = at + g * 16 < row_bytes;
+        const unsigned b = in ? vb : kPastBuffer;
+        fb[u][h][0].v = __builtin_bit_cast(decltype(fb[u][h][0].v), __builtin_amdgcn_raw_buffer_load_b128(rb, b, at, 0));
+        if constexpr (GATED) fb[u][h][1].v = __builtin_bit_cast(decltype(fb[u][h][1].v), __builtin_amdgcn_raw_buffer_load_b128(rb2, b, at, 0));
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+          fa[u][h][t].v = __builtin_bit_cast(decltype(fa[u][h][t].v), __builtin_amdgcn_raw_buffer_load_b128(ra, in ? va[t] : kPastBuffer, at, 0));
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+#pragma unroll
+          for (int s = 0; s < SETS; ++s) acc[s][t] = mfma_frag(fb[u][h][s], fa[u][h][t], acc[s][t]);
+  }
+#pragma unroll
+  for (int s = 0; s < SETS; ++s)
+#pragma unroll
+    for (int t = 0; t < TT; ++t) s_sum[wave][s * TT + t][l] = acc[s][t];
+  __syncthreads();
+  for (int t = wave; t < TT; t += WAVES) {
+    const int64_t row = 16 * t + r;
+    const int col = n0 + 4 * g;
+    floatx4_t v[SETS];
+#pragma unroll
+    for (int s = 0; s < SETS; ++s) {
+      v[s] = s_sum[0][s * TT + t][l];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) v[s] += s_sum[w][s * TT + t][l];
+    }
+    if (row >= p.M || col >= N) continue;
+    auto put = [&](T* at, floatx4_t x) {
+      if constexpr (ES == 4) *(floatx4_t*)at = x;
+      else *(uintx2_t*)at = pack4(x);
+    };
+    if constexpr (GATED) {
+      floatx4_t h;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float f, slope;
+        activate<T>(p.act, v[0][i], f, slope);
+        h[i] = f * v[1][i];
+      }
+      put(p.c + row * N + col, h);
+      if (p.c2) {
+        put(p.c2 + row * 2 * N + col, v[0]);
+        put(p.c2 + row * 2 * N + N + col, v[1]);
+      }
+    } else {
+      put(p.c + row * N + col, v[0]);
+    }
+  }
+}
+
+// ---- host ----
+constexpr int kFewTokens = 64;
+
+// How a product is cut: blocks of 256 x 256 or 128 x 128, K in `splits` runs of k_each.
+struct Cut {
+  bool big;
+  int splits;
+  int64_t k_each;
+  unsigned tiles_m, tiles_n;
+};
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+Cut cut_of(int64_t M, int64_t N, int64_t K, int dtype, Kind kind) {
+  const int bk = dtype == MOGA_F32 ? 32 : 64;
+  const int64_t steps = ceil_div(K, bk);
+  Cut best{};
+  double least = 0;
+  for (int big = 0; big < (dtype == MOGA_F32 ? 1 : 2); ++big) {
+    const int bm = big ? 256 : 128, bn = (big ? 256 : 128) / (kind == kGated ? 2 : 1);
+    const int64_t tiles = ceil_div(M, bm) * ceil_div(N, bn);
+    // microseconds: a step of a full chip's blocks, a block's start and end, and the sums of the splits written and read
+    const double step = big ? 1.7 : 1.0, ends = big ? 8 : 4, resident = big ? 256 : 512;
+    for (int s = 1; s <= (kind == kPlain ? 32 : 1); ++s) {
+      const int64_t each = ceil_div(steps, s);
+      if (s > 1 && (each < 8 || ceil_div(steps, each) != s)) continue;
+      const double cost = std::ceil(tiles * s / resident) * (each * step + ends) + (s > 1 ? 6 + M * N * 4. * (2 * s) / 4e6 : 0);
+      if (least == 0 || cost < least) {
+        least = cost;
+        best = {big != 0, s, s > 1 ? each * bk : K, (unsigned)ceil_div(M, bm), (unsigned)ceil_div(N, bn)};
+      }
+    }
+  }
+  return best;
+}
+
+size_t part_bytes(int64_t M, int64_t N, int64_t K, int dtype) {
+  const Cut c = cut_of(M, N, K, dtype, kPlain);
+  return c.splits > 1 ? round_up((size_t)c.splits * M * N * sizeof(float), 256) : 0;
+}
+
+template <typename T, Kind KIND, bool AK, bool BK>
+void launch_product(Product<T> p, int dtype, float* part, hipStream_t st) {
+  const Cut c = cut_of(p.M, p.N, p.K, dtype, KIND);
+  p.tiles_m = c.tiles_m;
+  p.tiles_n = c.tiles_n;
+  p.k_each = c.k_each;
+  p.part = c.splits > 1 ? part : nullptr;
+  const unsigned blocks = c.tiles_m * c.tiles_n * c.splits;
+  if constexpr (sizeof(T) == 2) {
+    if (c.big) product_kernel<T, KIND, AK, BK, 2, 4, 8, 4><<<blocks, 512, 0, st>>>(p);
+    else product_kernel<T, KIND, AK, BK, 2, 2, 4, 4><<<blocks, 256, 0, st>>>(p);
+  } else {
+    product_kernel<T, KIND, AK, BK, 2, 2, 4, 4><<<blocks, 256, 0, st>>>(p);
+  }
+  if (c.splits > 1) {
+    const int64_t n = p.M * p.N;
+    join_kernel<T><<<(unsigned)std::min<int64_t>(4096, ceil_div(n, 1024)), 256, 0, st>>>(part, c.splits, n, p.c);
+  }
+}
+
+template <typename T, bool GATED>
+void launch_few(const Product<T>& p, hipStream_t st) {
+  const unsigned blocks = (unsigned)ceil_div(p.N, 16);
+  if (p.M <= 16) {
+    if (blocks >= 512) few_kernel<T, GATED, 1, 4><<<blocks, 256, 0, st>>>(p);
+    else if (blocks >= 192) few_kernel<T, GATED, 1, 8><<<blocks, 512, 0, st>>>(p);
+    else few_kernel<T, GATED, 1, 16><<<blocks, 1024, 0, st>>>(p);
+  } else if (p.M <= 32) {
+    if (blocks >= 512) few_kernel<T, GATED, 2, 4><<<blocks, 256, 0, st>>>(p);
+    else few_kernel<T, GATED, 2, 8><<<blocks, 512, 0, st>>>(p);
+  } else {
+    if (blocks >= 512) few_kernel<T, GATED, 4, 4><<<blocks, 256, 0, st>>>(p);
+    else few_kernel<T, GATED, 4, 8><<<blocks, 512, 0, st>>>(p);
+  }
+}
+
+template <typename T>
+Product<T> product(const void* a, int64_t lda, const void* b, int64_t ldb, int64_t M, int N, int64_t K, void* c) {
+  Product<T> p{};
+  p.a = (const T*)a;
+  p.b = (const T*)b;
+  p.lda = lda;
+  p.ldb = ldb;
+  p.M = M;
+  p.N = N;
+  p.K = K;
+  p.c = (T*)c;
+  return p;
+}
+
+template <typename T>
+void ffn_fwd(const void* x, const void* w_in, const void* w_out, int dtype, int64_t N, int C, int F, int act, void* h, void* au, void* y, void* ws,
+             hipStream_t st) {
+  Product<T> in = product<T>(x, C, w_in, C, N, F, C, h);
+  in.c2 = (T*)au;
+  in.act = act;
+  const Product<T> out = product<T>(h, F, w_out, F, N, C, F, y);
+  if (N <= kFewTokens) {
+    launch_few<T, true>(in, st);
+    launch_few<T, false>(out, st);
+  } else {
+    launch_product<T, kGated, false, false>(in, dtype, nullptr, st);
+    launch_product<T, kPlain, false, false>(out, dtype, (float*)ws, st);
+  }
+}
+
+// Workspace of the backward: [da, du], and the splits of one product after the other.
+struct FfnBwdWs {
+  size_t part, bytes;   // offset of the splits; all
+  FfnBwdWs(int64_t N, int C, int F, int dtype) {
+    part = round_up((size_t)N * 2 * F * elem_size(dtype), 256);
+    bytes = part + std::max({part_bytes(N, C, 2 * (int64_t)F, dtype), part_bytes(2 * (int64_t)F, C, N, dtype), part_bytes(C, F, N, dtype)});
+  }
+};
+
+template <typename T>
+void ffn_bwd(const void* d_y, const void* x, const void* w_in, const void* w_out, const void* au, const void* h, int dtype, int64_t N, int C, int F,
+             int act, void* d_x, void* d_w_in, void* d_w_out, void* ws, hipStream_t st) {
+  float* part = (float*)((char*)ws + FfnBwdWs(N, C, F, dtype).part);
+  if (d_x || d_w_in) {
+    Product<T> dh = product<T>(d_y, C, w_out, F, N, F, C, ws);
+    dh.saved = (const T*)au;
+    dh.act = act;
+    launch_product<T, kGatedBwd, false, true>(dh, dtype, nullptr, st);
+  }
+  if (d_x) launch_product<T, kPlain, false, true>(product<T>(ws, 2 * (int64_t)F, w_in, C, N, C, 2 * (int64_t)F, d_x), dtype, part, st);
+  if (d_w_in) launch_product<T, kPlain, true, true>(product<T>(ws, 2 * (int64_t)F, x, C, 2 * (int64_t)F, C, N, d_w_in), dtype, part, st);
+  if (d_w_out) launch_product<T, kPlain, true, true>(product<T>(d_y, C, h, F, C, F, N, d_w_out), dtype, part, st);
+}
+
+int check_ffn(int64_t N, int C, int F, int dtype, int act) {
+  if (N < 0 || C < 1 || F < 1) return MOGA_ERR_INVALID_ARG;
+  if (dtype != MOGA_F32 && dtype != MOGA_BF16) return MOGA_ERR_UNSUPPORTED;
+  if (act != MOGA_ACT_SILU && act != MOGA_ACT_GELU && act != MOGA_ACT_GELU_TANH) return MOGA_ERR_UNSUPPORTED;
+  const int v = dtype == MOGA_F32 ? 4 : 8;
+  if (C % v || F % v || C > kFfnMaxC || F > kFfnMaxF || N >= ((int64_t)1 << 31)) return MOGA_ERR_UNSUPPORTED;
+  // blocks of the largest grids, and bytes of 256 rows within 31 bits
+  const int64_t most = std::max({ceil_div(N, 128) * ceil_div(F, 64), ceil_div(N, 128) * ceil_div(C, 128), ceil_div(2 * (int64_t)F, 128) * ceil_div(C, 128)});
+  return grid_fits(32 * most, 512) ? MOGA_OK : MOGA_ERR_UNSUPPORTED;
+}
+
+}  // namespace
+}  // namespace moga
+
+using namespace moga;
+
+extern "C" size_t moga_gated_ffn_fwd_ws_bytes(int64_t N, int C, int F, int dtype) {
+  if (check_ffn(N, C, F, dtype, MOGA_ACT_SILU) != MOGA_OK || N <= kFewTokens) return 0;
+  return part_bytes(N, C, F, dtype);
+}
+extern "C" size_t moga_gated_ffn_bwd_ws_bytes(int64_t N, int C, int F, int dtype) {
+  if (check_ffn(N, C, F, dtype, MOGA_ACT_SILU) != MOGA_OK || N == 0) return 0;
+  return FfnBwdWs(N, C, F, dtype).bytes;
+}
+
+extern "C" int moga_gated_ffn_fwd(const void* x, const void* w_in, const void* w_out, int dtype, int64_t N, int C, int F, int activation, void* h,
+                                  void* au, void* y, void* ws, size_t ws_bytes, void* stream) {
+  const int bad = check_ffn(N, C, F, dtype, activation);
+  if (bad) return bad;
+  if (N == 0) return MOGA_OK;
+  if (!x || !w_in || !w_out || !h || !y) return MOGA_ERR_INVALID_ARG;
+  if (!(aligned16(x) && aligned16(w_in) && aligned16(w_out) && aligned16(h) && aligned16(au) && aligned16(y) && aligned16(ws)))
+    return MOGA_ERR_INVALID_ARG;
+  const size_t need = moga_gated_ffn_fwd_ws_bytes(N, C, F, dtype);
+  if (need && (!ws || ws_bytes < need)) return MOGA_ERR_WORKSPACE;
+  const hipStream_t st = (hipStream_t)stream;
+  if (dtype == MOGA_F32) ffn_fwd<float>(x, w_in, w_out, dtype, N, C, F, activation, h, au, y, ws, st);
+  else ffn_fwd<unsigned short>(x, w_in, w_out, dtype, N, C, F, activation, h, au, y, ws, st);
+  return launch_status();
+}
+
+extern "C" int moga_gated_ffn_bwd(const void* d_y, const void* x, const void* w_in, const void* w_out, const void* au, const void* h, int dtype,
+                                  int64_t N, int C, int F, int activation, void* d_x, void* d_w_in, void* d_w_out, void* ws, size_t ws_bytes,
+                                  void* stream) {
+  const int bad = check_ffn(N, C, F, dtype, activation);
+  if (bad) return bad;
+  if (!(aligned16(d_y) && aligned16(x) && aligned16(w_in) && aligned16(w_out) && aligned16(au) && aligned16(h) && aligned16(d_x) &&
+        aligned16(d_w_in) && aligned16(d_w_out) && aligned16(ws)))
+    return MOGA_ERR_INVALID_ARG;
+  const hipStream_t st = (hipStream_t)stream;
+  if (N == 0) {   // of no tokens: zeros
+    const int64_t floats = (int64_t)C * F * elem_size(dtype) / 4;   // C and F are multiples of 4
+    if (d_w_in) launch_fill_zero((float*)d_w_in, 2 * floats, st);
+    if (d_w_out) launch_fill_zero((float*)d_w_out, floats, st);
+    return d_w_in || d_w_out ? launch_status() : MOGA_OK;
+  }
+  if (!d_x && !d_w_in && !d_w_out) return MOGA_OK;
+  if (!d_y || ((d_x || d_w_in) && (!w_out || !au)) || (d_x && !w_in) || (d_w_in && !x) || (d_w_out && !h)) return MOGA_ERR_INVALID_ARG;
+  if (!ws || ws_bytes < moga_gated_ffn_bwd_ws_bytes(N, C, F, dtype)) return MOGA_ERR_WORKSPACE;
+  if (dtype == MOGA_F32) ffn_bwd<float>(d_y, x, w_in, w_out, au, h, dtype, N, C, F, activation, d_x, d_w_in, d_w_out, ws, st);
+  else ffn_bwd<unsigned short>(d_y, x, w_in, w_out, au, h, dtype, N, C, F, activation, d_x, d_w_in, d_w_out, ws, st);
+  return launch_status();
+}

@@ -655,6 +655,145 @@ std::tuple<Tensor, OptTensor, OptTensor> layer_norm_bwd(const Tensor& d_y, const
   return {d_x, d_w, d_b};
 }
 
+// ---- residual sum with gate, and the norms before and after it ----
+// The parameters of a call; its tensors are looked at here and outlive it in the caller.
+struct ResidualNorm {
+  Tensor x;
+  OptTensor y, gate, post_weight, weight, bias, scale, shift;
+  int64_t post, pre;
+  double residual_scale;
+  std::optional<int64_t> tokens_per_row;
+  double eps;
+  at::ScalarType type;   // of y and h
+  int64_t N = 0, C = 0, rows = 1;
+
+  // dtype: of h where there is no y, else y's
+  ResidualNorm(const Tensor& x, const OptTensor& y, const OptTensor& gate, const OptTensor& post_weight, const OptTensor& weight, const OptTensor& bias,
+               const OptTensor& scale, const OptTensor& shift, int64_t post, int64_t pre, double residual_scale, std::optional<int64_t> tokens_per_row,
+               double eps, std::optional<at::ScalarType> dtype)
+      : x(x), y(y), gate(gate), post_weight(post_weight), weight(weight), bias(bias), scale(scale), shift(shift), post(post), pre(pre),
+        residual_scale(residual_scale), tokens_per_row(tokens_per_row), eps(eps) {
+    require(x, y, gate, post_weight, weight, bias, scale, shift);
+    need_dims(x, 2);
+    N = x.size(0), C = x.size(1);
+    type = y ? y->scalar_type() : dtype.value_or(x.scalar_type());
+    need(!y || !dtype || *dtype == y->scalar_type(), "dtype: not y's");
+    if (type != at::kFloat && type != at::kBFloat16) raise(PyExc_TypeError, std::string("unsupported dtype ") + c10::toString(type));
+    need_like(y, x, x.sizes(), type, "y");
+    need(!tokens_per_row || *tokens_per_row >= 1, "tokens_per_row: at least 1");
+    if (tokens_per_row && N > 0) rows = (N + *tokens_per_row - 1) / *tokens_per_row;
+    need_like(post_weight, x, {C}, at::kFloat, "post_weight");
+    need_like(weight, x, {C}, at::kFloat, "weight");
+    need_like(bias, x, {C}, at::kFloat, "bias");
+    need_like(gate, x, {rows, C}, at::kFloat, "gate");
+    need_like(scale, x, {rows, C}, at::kFloat, "scale");
+    need_like(shift, x, {rows, C}, at::kFloat, "shift");
+  }
+  moga_residual_norm args() const {
+    moga_residual_norm a{};
+    a.x = ptr(x), a.y = ptr(y);
+    a.gate = as<float>(gate), a.post_weight = as<float>(post_weight), a.weight = as<float>(weight), a.bias = as<float>(bias);
+    a.scale = as<float>(scale), a.shift = as<float>(shift);
+    a.N = N, a.C = to_int(C);
+    a.tokens_per_row = tokens_per_row.value_or(std::max<int64_t>(N, 1));
+    a.x_dtype = dt(x), a.y_dtype = type == at::kFloat ? MOGA_F32 : MOGA_BF16;
+    a.post = to_int(post), a.pre = to_int(pre);
+    a.residual_scale = (float)residual_scale, a.eps = (float)eps;
+    return a;
+  }
+};
+
+std::tuple<OptTensor, OptTensor, OptTensor> residual_norm_fwd(const ResidualNorm& p, bool want_stats, const OptStream& stream) {
+  const c10::OptionalDeviceGuard guard(p.x.device());
+  const Call call(stream);
+  OptTensor r, h, stats;
+  if (p.y) r = call.make(p.x.sizes(), p.x);
+  if (p.pre != MOGA_NORM_NONE) h = call.make(p.x.sizes(), p.x, p.type);
+  if (want_stats) stats = call.make({4, p.N}, p.x, at::kFloat);
+  const moga_residual_norm a = p.args();
+  check("moga_residual_norm_fwd", moga_residual_norm_fwd(&a, ptr(r), ptr(h), as<float>(stats), call.stream()));
+  return {r, h, stats};
+}
+
+// d_x, d_y, d_gate, d_post_weight, d_weight, d_bias, d_scale, d_shift
+using ResidualNormGrads = std::tuple<Tensor, OptTensor, OptTensor, OptTensor, OptTensor, OptTensor, OptTensor, OptTensor>;
+ResidualNormGrads residual_norm_bwd(const ResidualNorm& p, const OptTensor& d_r, const OptTensor& d_h, const Tensor& stats, bool want_params,
+                                    const OptStream& stream) {
+  require(d_r, d_h, stats);
+  const c10::OptionalDeviceGuard guard(p.x.device());
+  const Call call(stream);
+  need_like(d_r, p.x, p.x.sizes(), p.x.scalar_type(), "d_r");
+  need_like(d_h, p.x, p.x.sizes(), p.type, "d_h");
+  need_like(stats, p.x, {4, p.N}, at::kFloat, "stats");
+  Tensor d_x = call.make(p.x.sizes(), p.x);
+  OptTensor d_y, ws;
+  if (p.y) d_y = call.make(p.x.sizes(), p.x, p.type);
+  auto like = [&](const OptTensor& t) { return want_params && t ? OptTensor(call.make(t->sizes(), *t)) : std::nullopt; };
+  const OptTensor d_gate = like(p.gate), d_post = like(p.post_weight), d_w = like(p.weight), d_b = like(p.bias), d_scale = like(p.scale),
+                  d_shift = like(p.shift);
+  if (d_gate || d_post || d_w || d_b || d_scale || d_shift) {
+    const int64_t rows = p.gate || p.scale || p.shift ? p.rows : 1;
+    ws = call.workspace(moga_workspace_bytes(MOGA_OP_RESIDUAL_NORM_BWD, p.N, 0, 0, to_int(rows), to_int(p.C), dt(p.x)), p.x);
+  }
+  const moga_residual_norm a = p.args();
+  check("moga_residual_norm_bwd",
+        moga_residual_norm_bwd(&a, as<float>(stats), ptr(d_r), ptr(d_h), ptr(d_x), ptr(d_y), as<float>(d_gate), as<float>(d_post), as<float>(d_w),
+                               as<float>(d_b), as<float>(d_scale), as<float>(d_shift), ptr(ws), bytes_of(ws), call.stream()));
+  return {d_x, d_y, d_gate, d_post, d_w, d_b, d_scale, d_shift};
+}
+
+// ---- gated feed-forward ----
+struct FfnSizes {
+  int64_t N, C, F;
+  FfnSizes(const Tensor& x, const Tensor& w_in, const Tensor& w_out) {
+    need_dims(x, 2);
+    need_dims(w_in, 2);
+    need_dims(w_out, 2);
+    N = x.size(0), C = x.size(1), F = w_out.size(1);
+    need_like(w_in, x, {2 * F, C}, x.scalar_type(), "w_in");
+    need_like(w_out, x, {C, F}, x.scalar_type(), "w_out");
+  }
+};
+
+// y, [a, u], h; the latter two are returned for a backward only
+std::tuple<Tensor, OptTensor, OptTensor> gated_ffn_fwd(const Tensor& x, const Tensor& w_in, const Tensor& w_out, int64_t act, bool want_saved,
+                                                       const OptStream& stream) {
+  require(x, w_in, w_out);
+  const c10::OptionalDeviceGuard guard(x.device());
+  const Call call(stream);
+  const FfnSizes s(x, w_in, w_out);
+  Tensor y = call.make(x.sizes(), x), h = call.make({s.N, s.F}, x);
+  OptTensor au, ws;
+  if (want_saved) au = call.make({s.N, 2 * s.F}, x);
+  const size_t bytes = moga_workspace_bytes(MOGA_OP_GATED_FFN_FWD, s.N, 0, to_int(s.F), 1, to_int(s.C), dt(x));
+  if (bytes) ws = call.workspace(bytes, x);
+  check("moga_gated_ffn_fwd", moga_gated_ffn_fwd(ptr(x), ptr(w_in), ptr(w_out), dt(x), s.N, to_int(s.C), to_int(s.F), to_int(act), ptr(h), ptr(au),
+                                                 ptr(y), ptr(ws), bytes_of(ws), call.stream()));
+  return {y, au, want_saved ? OptTensor(h) : std::nullopt};
+}
+
+std::tuple<OptTensor, OptTensor, OptTensor> gated_ffn_bwd(const Tensor& d_y, const Tensor& x, const Tensor& w_in, const Tensor& w_out, const Tensor& au,
+                                                          const Tensor& h, int64_t act, bool want_dx, bool want_dw_in, bool want_dw_out,
+                                                          const OptStream& stream) {
+  require(d_y, x, w_in, w_out, au, h);
+  const c10::OptionalDeviceGuard guard(x.device());
+  const Call call(stream);
+  const FfnSizes s(x, w_in, w_out);
+  need_like(d_y, x, x.sizes(), x.scalar_type(), "d_y");
+  need_like(au, x, {s.N, 2 * s.F}, x.scalar_type(), "au");
+  need_like(h, x, {s.N, s.F}, x.scalar_type(), "h");
+  OptTensor d_x, d_w_in, d_w_out, ws;
+  if (want_dx) d_x = call.make(x.sizes(), x);
+  if (want_dw_in) d_w_in = call.make(w_in.sizes(), x);
+  if (want_dw_out) d_w_out = call.make(w_out.sizes(), x);
+  const size_t bytes = moga_workspace_bytes(MOGA_OP_GATED_FFN_BWD, s.N, 0, to_int(s.F), 1, to_int(s.C), dt(x));
+  if (bytes && (d_x || d_w_in || d_w_out)) ws = call.workspace(bytes, x);
+  check("moga_gated_ffn_bwd",
+        moga_gated_ffn_bwd(ptr(d_y), ptr(x), ptr(w_in), ptr(w_out), ptr(au), ptr(h), dt(x), s.N, to_int(s.C), to_int(s.F), to_int(act), ptr(d_x),
+                           ptr(d_w_in), ptr(d_w_out), ptr(ws), bytes_of(ws), call.stream()));
+  return {d_x, d_w_in, d_w_out};
+}
+
 // What turns the pairs of a head, or (maps 2) of each half of one: positions [axes, N] (or [N]), radians per position of the pairs, pairs of each axis.
 struct Rotation {
   Tensor pos, freq;
@@ -928,7 +1067,7 @@ Tensor aligned(const Tensor& t) {
 // graph would end there, and a second derivative would come out without their part.
 struct NoDerivative : public torch::autograd::Node {
   variable_list apply(variable_list&&) override {
-    TORCH_CHECK(false, "layer_norm, rotary and moga_diff_attention have no second derivative");
+    TORCH_CHECK(false, "layer_norm, rotary, moga_diff_attention, residual_norm and gated_ffn have no second derivative");
   }
 };
 // Of a backward that runs now: its gradients, what it was given, and whether the former depend on the forward's inputs too.
@@ -971,6 +1110,86 @@ struct LayerNorm : public torch::autograd::Function<LayerNorm> {
     return first_only({d_x.view(d_y.sizes()), s[1].defined() ? or_empty(d_w) : Tensor(), bias ? or_empty(d_b) : Tensor(), Tensor()}, grads);
   }
 };
+
+// Outputs: those of r and h that are there.  Without y, r is x, which goes on by itself.
+struct ResidualNormFunction : public torch::autograd::Function<ResidualNormFunction> {
+  static variable_list forward(AutogradContext* ctx, const Tensor& x, const OptTensor& y, const OptTensor& gate, const OptTensor& post_weight,
+                               const OptTensor& weight, const OptTensor& bias, const OptTensor& scale, const OptTensor& shift, int64_t post, int64_t pre,
+                               double residual_scale, std::optional<int64_t> tokens_per_row, double eps, std::optional<at::ScalarType> dtype, bool train) {
+    require(x, y, gate, post_weight, weight, bias, scale, shift);
+    need(x.dim() >= 1, "x: at least one dimension");
+    const int64_t C = x.size(-1);
+    need(C >= 1, "x: an empty last dimension");
+    need(!y || y->sizes() == x.sizes(), "y: unexpected size");
+    const std::vector<int64_t> rows_c{x.numel() / C, C};
+    auto rows = [&](const Tensor& t) { return aligned(t.view(rows_c)); };
+    const ResidualNorm p(rows(x), y ? OptTensor(rows(*y)) : std::nullopt, aligned(gate), aligned(post_weight), aligned(weight), aligned(bias),
+                         aligned(scale), aligned(shift), post, pre, residual_scale, tokens_per_row, eps, dtype);
+    auto [r, h, stats] = residual_norm_fwd(p, train, std::nullopt);
+    ctx->save_for_backward({p.x, or_empty(p.y), or_empty(p.gate), or_empty(p.post_weight), or_empty(p.weight), or_empty(p.bias), or_empty(p.scale),
+                            or_empty(p.shift), or_empty(stats)});
+    ctx->saved_data["kinds"] = std::vector<int64_t>{post, pre, tokens_per_row.value_or(0), (int64_t)p.type};
+    ctx->saved_data["factors"] = std::vector<double>{residual_scale, eps};
+    ctx->saved_data["sizes"] = x.sizes().vec();
+    ctx->set_materialize_grads(false);
+    variable_list out;
+    if (r) out.push_back(r->view(x.sizes()));
+    if (h) out.push_back(h->view(x.sizes()));
+    return out;
+  }
+  static variable_list backward(AutogradContext* ctx, const variable_list& grads) {
+    const auto s = ctx->get_saved_variables();
+    const std::vector<int64_t> k = ctx->saved_data["kinds"].toIntVector(), sizes = ctx->saved_data["sizes"].toIntVector();
+    const std::vector<double> f = ctx->saved_data["factors"].toDoubleVector();
+    const auto type = (at::ScalarType)k[3];
+    const ResidualNorm p(s[0], or_none(s[1]), or_none(s[2]), or_none(s[3]), or_none(s[4]), or_none(s[5]), or_none(s[6]), or_none(s[7]), k[0], k[1], f[0],
+                         k[2] ? std::optional<int64_t>(k[2]) : std::nullopt, f[1], type);
+    auto rows = [&](const Tensor& t) { return t.defined() ? OptTensor(aligned(t.contiguous().view(p.x.sizes()))) : std::nullopt; };
+    const bool has_r = p.y.has_value(), has_h = p.pre != MOGA_NORM_NONE;
+    const OptTensor d_r = has_r ? rows(grads[0]) : std::nullopt;
+    OptTensor d_h = has_h ? rows(grads[has_r ? 1 : 0]) : std::nullopt;
+    if (has_h && !d_h) d_h = at::zeros(p.x.sizes(), p.x.options().dtype(type));
+    // inputs are counted without those that are absent
+    bool params = false;
+    for (size_t i = 2, at = s[1].defined() ? 2 : 1; i < 8; ++i)
+      if (s[i].defined()) params = ctx->needs_input_grad(at++) || params;
+    auto [d_x, d_y, d_gate, d_post, d_w, d_b, d_scale, d_shift] = residual_norm_bwd(p, d_r, d_h, s[8], params, std::nullopt);
+    variable_list out(15);
+    out[0] = d_x.view(sizes);
+    if (d_y) out[1] = d_y->view(sizes);
+    out[2] = or_empty(d_gate), out[3] = or_empty(d_post), out[4] = or_empty(d_w), out[5] = or_empty(d_b), out[6] = or_empty(d_scale);
+    out[7] = or_empty(d_shift);
+    return first_only(out, grads);
+  }
+};
+
+struct GatedFfn : public torch::autograd::Function<GatedFfn> {
+  static Tensor forward(AutogradContext* ctx, const Tensor& x, const Tensor& w_in, const Tensor& w_out, int64_t act, bool train) {
+    require(x, w_in, w_out);
+    need(x.dim() >= 1, "x: at least one dimension");
+    const int64_t C = x.size(-1);
+    need(C >= 1, "x: an empty last dimension");
+    const Tensor rows = aligned(x.view({x.numel() / C, C})), wi = aligned(w_in), wo = aligned(w_out);
+    auto [y, au, h] = gated_ffn_fwd(rows, wi, wo, act, train, std::nullopt);
+    if (train) ctx->save_for_backward({rows, wi, wo, *au, *h});
+    ctx->saved_data["act"] = act;
+    return y.view(x.sizes());
+  }
+  static variable_list backward(AutogradContext* ctx, const variable_list& grads) {
+    const auto s = ctx->get_saved_variables();
+    const Tensor d_y = aligned(grads[0]);
+    auto [d_x, d_wi, d_wo] = gated_ffn_bwd(d_y.view(s[0].sizes()), s[0], s[1], s[2], s[3], s[4], ctx->saved_data["act"].toInt(),
+                                           ctx->needs_input_grad(0), ctx->needs_input_grad(1), ctx->needs_input_grad(2), std::nullopt);
+    return first_only({d_x ? d_x->view(d_y.sizes()) : Tensor(), or_empty(d_wi), or_empty(d_wo), Tensor(), Tensor()}, grads);
+  }
+};
+
+bool will_train(std::initializer_list<const Tensor*> leaves, std::initializer_list<const OptTensor*> others = {}) {
+  bool any = false;
+  for (const Tensor* t : leaves) any = any || t->requires_grad();
+  for (const OptTensor* t : others) any = any || (*t && (*t)->requires_grad());
+  return any && at::GradMode::is_enabled();
+}
 
 struct Rotary : public torch::autograd::Function<Rotary> {
   // Outputs: of q and k those that are there.
@@ -1163,4 +1382,45 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
       },
       nogil);
   m.def("diff_attention", &diff_attention, nogil);
+  m.def(
+      "residual_norm_fwd",
+      [](const Tensor& x, const OptTensor& y, const OptTensor& gate, const OptTensor& post_weight, const OptTensor& weight, const OptTensor& bias,
+         const OptTensor& scale, const OptTensor& shift, int64_t post, int64_t pre, double residual_scale, std::optional<int64_t> tokens_per_row,
+         double eps, std::optional<at::ScalarType> dtype, bool want_stats, const OptStream& stream) {
+        return residual_norm_fwd(
+            ResidualNorm(x, y, gate, post_weight, weight, bias, scale, shift, post, pre, residual_scale, tokens_per_row, eps, dtype), want_stats, stream);
+      },
+      nogil);
+  m.def(
+      "residual_norm_bwd",
+      [](const OptTensor& d_r, const OptTensor& d_h, const Tensor& x, const Tensor& stats, const OptTensor& y, const OptTensor& gate,
+         const OptTensor& post_weight, const OptTensor& weight, const OptTensor& bias, const OptTensor& scale, const OptTensor& shift, int64_t post,
+         int64_t pre, double residual_scale, std::optional<int64_t> tokens_per_row, double eps, bool want_params, const OptStream& stream) {
+        std::optional<at::ScalarType> type;
+        if (!y && d_h) type = d_h->scalar_type();
+        return residual_norm_bwd(
+            ResidualNorm(x, y, gate, post_weight, weight, bias, scale, shift, post, pre, residual_scale, tokens_per_row, eps, type), d_r, d_h, stats,
+            want_params, stream);
+      },
+      nogil);
+  m.def("gated_ffn_fwd", &gated_ffn_fwd, nogil);
+  m.def("gated_ffn_bwd", &gated_ffn_bwd, nogil);
+  m.def(
+      "residual_norm",
+      [](const Tensor& x, const OptTensor& y, const OptTensor& gate, const OptTensor& post_weight, const OptTensor& weight, const OptTensor& bias,
+         const OptTensor& scale, const OptTensor& shift, int64_t post, int64_t pre, double residual_scale, std::optional<int64_t> tokens_per_row,
+         double eps, std::optional<at::ScalarType> dtype) {
+        need(y || pre != MOGA_NORM_NONE, "y or a norm of x");
+        const bool train = will_train({&x}, {&y, &gate, &post_weight, &weight, &bias, &scale, &shift});
+        const auto out = ResidualNormFunction::apply(x, y, gate, post_weight, weight, bias, scale, shift, post, pre, residual_scale, tokens_per_row, eps,
+                                                     dtype, train);
+        return std::make_tuple(y ? out[0] : x, pre != MOGA_NORM_NONE ? OptTensor(out.back()) : std::nullopt);
+      },
+      nogil);
+  m.def(
+      "gated_ffn",
+      [](const Tensor& x, const Tensor& w_in, const Tensor& w_out, int64_t act) {
+        return GatedFfn::apply(x, w_in, w_out, act, will_train({&x, &w_in, &w_out}));
+      },
+      nogil);
 }
