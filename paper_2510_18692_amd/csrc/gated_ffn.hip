@@ -4,6 +4,7 @@
 //   dh = d_y W_out,  da = dh u act'(a),  du = dh act(a),  d_x = [da, du] W_in,  d_W_in = [da, du]^T x,  d_W_out = d_y^T h
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "matmul_tiles.h"
 
@@ -20,23 +21,46 @@ template <typename T> __device__ __forceinline__ float inverse(float v);
 template <> __device__ __forceinline__ float inverse<unsigned short>(float v) { return __builtin_amdgcn_rcpf(v); }
 template <> __device__ __forceinline__ float inverse<float>(float v) { return 1.f / v; }
 
+// Phi(a), the normal distribution, and e^(-a^2 / 2).  bf16: Abramowitz and Stegun 7.1.26, erfc z = (a1 t + .. + a5 t^5) e^(-z^2) with
+// t = 1 / (1 + 0.3275911 z), off by 1.5e-7 at most: 12 instructions on an exponential that the derivative needs anyway.
+template <typename T> __device__ __forceinline__ float normal(float a, float& e);
+template <> __device__ __forceinline__ float normal<unsigned short>(float a, float& e) {
+  e = exp_neg<unsigned short>(0.5f * a * a);
+  const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(a), 0.3275911f * 0.70710678118654752f, 1.f));
+  const float q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5f * 1.061405429f, -0.5f * 1.453152027f), 0.5f * 1.421413741f), -0.5f * 0.284496736f),
+                           0.5f * 0.254829592f) * e;
+  return a < 0.f ? q : 1.f - q;
+}
+template <> __device__ __forceinline__ float normal<float>(float a, float& e) {
+  e = expf(-0.5f * a * a);
+  return 0.5f + 0.5f * erff(a * 0.70710678118654752f);
+}
+
 // act(a) and act'(a).  tanh's form is a sigmoid: (1 + tanh v) / 2 = 1 / (1 + e^-2v).
-template <typename T>
-__device__ __forceinline__ void activate(int act, float a, float& f, float& slope) {
-  if (act == MOGA_ACT_SILU) {
+template <typename T, int ACT>
+__device__ __forceinline__ void activate(float a, float& f, float& slope) {
+  if constexpr (ACT == MOGA_ACT_SILU) {
     const float p = inverse<T>(1.f + exp_neg<T>(a));
     f = a * p;
     slope = fmaf(f, 1.f - p, p);
-  } else if (act == MOGA_ACT_GELU) {
-    const float p = 0.5f + 0.5f * erff(a * 0.70710678118654752f);
+  } else if constexpr (ACT == MOGA_ACT_GELU) {
+    float e;
+    const float p = normal<T>(a, e);
     f = a * p;
-    slope = fmaf(a * 0.39894228040143268f, exp_neg<T>(0.5f * a * a), p);
+    slope = fmaf(a * 0.39894228040143268f, e, p);
   } else {
     constexpr float k = 1.5957691216057308f, c = 0.044715f;   // 2 sqrt(2 / pi)
     const float a2 = a * a, p = inverse<T>(1.f + exp_neg<T>(k * a * fmaf(c, a2, 1.f)));
     f = a * p;
     slope = fmaf(f * (1.f - p), k * fmaf(3.f * c, a2, 1.f), p);
   }
+}
+// f(activation) as a constant: one branch for all of a block's values
+template <typename F>
+__device__ __forceinline__ void with_activation(int act, F&& f) {
+  if (act == MOGA_ACT_SILU) f(std::integral_constant<int, MOGA_ACT_SILU>{});
+  else if (act == MOGA_ACT_GELU) f(std::integral_constant<int, MOGA_ACT_GELU>{});
+  else f(std::integral_constant<int, MOGA_ACT_GELU_TANH>{});
 }
 
 // ---- tiles ----
@@ -57,77 +81,114 @@ struct Product {
   unsigned tiles_m, tiles_n;
 };
 
-template <typename T> __device__ __forceinline__ void store4(T* p, floatx4_t v);
-template <> __device__ __forceinline__ void store4<float>(float* p, floatx4_t v) { *(floatx4_t*)p = v; }
-
 __device__ __forceinline__ uintx2_t pack4(floatx4_t v) { return uintx2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}; }
-// Lane group g holds columns 4 g .. 4 g + 3 of two neighbouring tiles, and gets eight neighbouring columns from column() on.
-__device__ __forceinline__ int pair_column(int g) { return (g & 1) * 16 + (g >> 1) * 8; }
-__device__ __forceinline__ uintx4_t pair_up(uintx2_t p, uintx2_t q) {
-  const auto x = __builtin_amdgcn_permlane16_swap(p[0], q[0], false, false), y = __builtin_amdgcn_permlane16_swap(p[1], q[1], false, false);
-  return uintx4_t{x[0], y[0], x[1], y[1]};
+
+// The columns of a wave's sums in units of two neighbouring tiles: lane group g holds columns 4 g .. of either.  Lanes exchange fours, after which
+// each has eight neighbouring columns, from unit_column(g) on.
+__device__ __forceinline__ int unit_column(int g) { return (g & 1) * 16 + (g >> 1) * 8; }
+__device__ __forceinline__ void exchange(unsigned& p, unsigned& q) {
+  const auto x = __builtin_amdgcn_permlane16_swap(p, q, false, false);
+  p = x[0], q = x[1];
 }
-__device__ __forceinline__ void pair_up(floatx4_t p, floatx4_t q, float (&v)[8]) {
+__device__ __forceinline__ uintx4_t unit_packed(floatx4_t p, floatx4_t q) {
+  const uintx2_t x = pack4(p), y = pack4(q);
+  unsigned v[4] = {x[0], x[1], y[0], y[1]};
+  exchange(v[0], v[2]);
+  exchange(v[1], v[3]);
+  return uintx4_t{v[0], v[1], v[2], v[3]};
+}
+__device__ __forceinline__ void unit_eight(floatx4_t p, floatx4_t q, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(p[i]), __float_as_uint(q[i]), false, false);
-    v[i] = __uint_as_float(x[0]);
-    v[4 + i] = __uint_as_float(x[1]);
+    unsigned x = __float_as_uint(p[i]), y = __float_as_uint(q[i]);
+    exchange(x, y);
+    v[i] = __uint_as_float(x);
+    v[4 + i] = __uint_as_float(y);
   }
 }
 
-// Two neighbouring tiles of a row of C, rounded once: 16 bytes a lane at p + column.
-__device__ __forceinline__ void put_pair(unsigned short* row, int col, int g, int64_t N, floatx4_t p, floatx4_t q) {
-  const uintx4_t v = pair_up(pack4(p), pack4(q));
-  col += pair_column(g);
-  if (col < N) *(uintx4_t*)(row + col) = v;
+// A unit of a row of C from column col on, rounded once: 16 bytes a lane.
+__device__ __forceinline__ void put_unit(unsigned short* row, int col, int g, int64_t N, bool ok, floatx4_t p, floatx4_t q) {
+  const uintx4_t v = unit_packed(p, q);
+  col += unit_column(g);
+  if (ok && col < N) *(uintx4_t*)(row + col) = v;
 }
-__device__ __forceinline__ void put_pair(float* row, int col, int g, int64_t N, floatx4_t p, floatx4_t q) {
+__device__ __forceinline__ void put_unit(float* row, int col, int g, int64_t N, bool ok, floatx4_t p, floatx4_t q) {
   col += 4 * g;
-  if (col < N) *(floatx4_t*)(row + col) = p;
-  if (col + 16 < N) *(floatx4_t*)(row + col + 16) = q;
+  if (ok && col < N) *(floatx4_t*)(row + col) = p;
+  if (ok && col + 16 < N) *(floatx4_t*)(row + col + 16) = q;
 }
 
-__device__ __forceinline__ void grad_pair(const unsigned short* saved, unsigned short* out, int64_t F, int col, int g, int act, floatx4_t p, floatx4_t q) {
-  float dh[8];
-  pair_up(p, q, dh);
-  col += pair_column(g);
-  if (col >= F) return;
-  const uintx4_t a4 = *(const uintx4_t*)(saved + col), u4 = *(const uintx4_t*)(saved + F + col);
-  uintx4_t da4, du4;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float f0, s0, f1, s1;
-    activate<unsigned short>(act, bf16_lo_to_f32(a4[i]), f0, s0);
-    activate<unsigned short>(act, bf16_hi_to_f32(a4[i]), f1, s1);
-    da4[i] = pack_bf16x2(dh[2 * i] * bf16_lo_to_f32(u4[i]) * s0, dh[2 * i + 1] * bf16_hi_to_f32(u4[i]) * s1);
-    du4[i] = pack_bf16x2(dh[2 * i] * f0, dh[2 * i + 1] * f1);
+// a and u of a unit of a row, as a lane needs them for their gradients.
+template <typename T> struct Saved;
+template <> struct Saved<unsigned short> {
+  uintx4_t a, u;
+  __device__ __forceinline__ void load(const unsigned short* row, int64_t F, int col, int g, bool ok) {
+    col += unit_column(g);
+    a = u = uintx4_t{0, 0, 0, 0};
+    if (ok && col < F) {
+      a = *(const uintx4_t*)(row + col);
+      u = *(const uintx4_t*)(row + F + col);
+    }
   }
-  *(uintx4_t*)(out + col) = da4;
-  *(uintx4_t*)(out + F + col) = du4;
-}
-__device__ __forceinline__ void grad_pair(const float* saved, float* out, int64_t F, int col, int g, int act, floatx4_t p, floatx4_t q) {
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int at = col + 16 * t + 4 * g;
-    if (at >= F) return;
-    const floatx4_t dh = t ? q : p, a = *(const floatx4_t*)(saved + at), u = *(const floatx4_t*)(saved + F + at);
-    floatx4_t da, du;
+  template <int ACT>
+  __device__ __forceinline__ void put(unsigned short* row, int64_t F, int col, int g, bool ok, floatx4_t p, floatx4_t q) const {
+    float dh[8];
+    unit_eight(p, q, dh);
+    uintx4_t da4, du4;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      float f, s;
-      activate<float>(act, a[i], f, s);
-      da[i] = dh[i] * u[i] * s;
-      du[i] = dh[i] * f;
+      float f0, s0, f1, s1;
+      activate<unsigned short, ACT>(bf16_lo_to_f32(a[i]), f0, s0);
+      activate<unsigned short, ACT>(bf16_hi_to_f32(a[i]), f1, s1);
+      da4[i] = pack_bf16x2(dh[2 * i] * bf16_lo_to_f32(u[i]) * s0, dh[2 * i + 1] * bf16_hi_to_f32(u[i]) * s1);
+      du4[i] = pack_bf16x2(dh[2 * i] * f0, dh[2 * i + 1] * f1);
     }
-    *(floatx4_t*)(out + at) = da;
-    *(floatx4_t*)(out + F + at) = du;
+    col += unit_column(g);
+    if (ok && col < F) {
+      *(uintx4_t*)(row + col) = da4;
+      *(uintx4_t*)(row + F + col) = du4;
+    }
   }
-}
+};
+template <> struct Saved<float> {
+  floatx4_t a[2], u[2];
+  __device__ __forceinline__ void load(const float* row, int64_t F, int col, int g, bool ok) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int at = col + 16 * t + 4 * g;
+      a[t] = u[t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+      if (ok && at < F) {
+        a[t] = *(const floatx4_t*)(row + at);
+        u[t] = *(const floatx4_t*)(row + F + at);
+      }
+    }
+  }
+  template <int ACT>
+  __device__ __forceinline__ void put(float* row, int64_t F, int col, int g, bool ok, floatx4_t p, floatx4_t q) const {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int at = col + 16 * t + 4 * g;
+      const floatx4_t dh = t ? q : p;
+      floatx4_t da, du;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float f, s;
+        activate<float, ACT>(a[t][i], f, s);
+        da[i] = dh[i] * u[t][i] * s;
+        du[i] = dh[i] * f;
+      }
+      if (ok && at < F) {
+        *(floatx4_t*)(row + at) = da;
+        *(floatx4_t*)(row + F + at) = du;
+      }
+    }
+  }
+};
 
-// WM x WN waves, TM x TN tiles of 16 each
+// WM x WN waves, TM x TN tiles of 16 x 16 each
 template <typename T, Kind KIND, bool A_KFIRST, bool B_KFIRST, int WM, int WN, int TM, int TN>
-__global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void product_kernel(const Product<T> p) {
+__global__ __launch_bounds__(64 * WM * WN, 2) void product_kernel(const Product<T> p) {
   constexpr int THREADS = 64 * WM * WN, BM = 16 * WM * TM, BN = 16 * WN * TN;
   using OpA = Operand<T, A_KFIRST, BM, THREADS, TM>;
   using OpB = Operand<T, B_KFIRST, BN, THREADS, TN>;
@@ -137,28 +198,27 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void product_ke
   const unsigned lds = lds_addr_uniform(s_mem);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
 
-  // tiles in panels of 8 rows of tiles, down a panel's columns
   const unsigned tiles = p.tiles_m * p.tiles_n, split = blockIdx.x / tiles;
-  unsigned b = xcd_order(blockIdx.x % tiles, tiles);
-  const unsigned panel = b / (8 * p.tiles_n), in = b - panel * 8 * p.tiles_n, high = min(8u, p.tiles_m - panel * 8);
-  const unsigned bm = panel * 8 + in % high, bn = in / high;
+  unsigned bm, bn;
+  tile_of(blockIdx.x % tiles, p.tiles_m, p.tiles_n, bm, bn);
 
   const int64_t m0 = (int64_t)bm * BM, k0 = split * p.k_each;
   const int n0 = bn * (KIND == kGated ? BN / 2 : BN), k_count = (int)min(p.k_each, p.K - k0);
-  constexpr bool PAIRED = KIND == kGated;
   OpA oa;
   OpB ob;
-  oa.init(p.a, p.lda, m0, p.M, k0, k_count, wm * TM);
-  if constexpr (PAIRED) ob.init_paired(p.b, p.ldb, n0, p.N, k_count, wn * TN);
-  else ob.init(p.b, p.ldb, n0, p.N, k0, k_count, wn * TN);
+  oa.init(p.a, p.lda, m0, p.M, k0, k_count, wm * TM, lds);
+  if constexpr (KIND == kGated) ob.init_paired(p.b, p.ldb, n0, p.N, k_count, wn * TN, lds + OpA::kBytes);
+  else ob.init(p.b, p.ldb, n0, p.N, k0, k_count, wn * TN, lds + OpA::kBytes);
 
-  auto stage = [&](unsigned at) {
-#pragma unroll
-    for (int i = 0; i < OpA::L; ++i) oa.stage(at, i);
-#pragma unroll
-    for (int i = 0; i < OpB::L; ++i) ob.template stage<PAIRED>(at + OpA::kBytes, i);
-    oa.advance();
-    ob.template advance<PAIRED>();
+  // the i-th of the thread's loads of a step; past the last step they are zeros
+  constexpr int LOADS = OpA::L + OpB::L;
+  auto load = [&](int i) {
+    if (i < OpA::L) oa.stage(i);
+    else ob.template stage<KIND == kGated>(i - OpA::L);
+  };
+  auto advance = [&](int other) {
+    oa.advance(other);
+    ob.template advance<KIND == kGated>(other);
   };
 
   floatx4_t acc[TM][TN];
@@ -167,73 +227,118 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void product_ke
 #pragma unroll
     for (int n = 0; n < TN; ++n) acc[m][n] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 
-  const int steps = (k_count + BK - 1) / BK;
-  stage(lds);
-  unsigned at = lds, other = lds + kStage;
-  for (int s = 0; s < steps; ++s) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (s + 1 < steps) stage(other);
+  // While the products of half a step run, the operands of the next half are read, each into the registers of the one just used.  Behind the first
+  // products of the second half one barrier: all of the step's buffer is in registers, so that the loads of the step after next go out into it, and
+  // the next step's has landed.
+  Frag<T> fa[TM], fb[2][TN];
+  auto half = [&](auto which) {
+    constexpr int H = which.value, PER = (LOADS + TM - 1) / TM;
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      Frag<T> fa[TM], fb[TN];
+    for (int m = 0; m < TM; ++m) {
 #pragma unroll
-      for (int n = 0; n < TN; ++n) fb[n] = ob.get(at + OpA::kBytes, n, kk);
+      for (int n = 0; n < TN; ++n) mfma_frag(acc[m][n], fb[H][n], fa[m]);
+      if (H == 1 && m == 0) {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      }
+      if (H == 1)
 #pragma unroll
-      for (int m = 0; m < TM; ++m) fa[m] = oa.get(at, m, kk);
-#pragma unroll
-      for (int m = 0; m < TM; ++m)
-#pragma unroll
-        for (int n = 0; n < TN; ++n) acc[m][n] = mfma_frag(fb[n], fa[m], acc[m][n]);
+        for (int i = m * PER; i < (m + 1) * PER && i < LOADS; ++i) load(i);
+      fa[m] = oa.get(m, 1 - H);
+      if (m < TN) fb[1 - H][m] = ob.get(m, 1 - H);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    const unsigned t = at;
-    at = other;
-    other = t;
+  };
+  static_assert(TN <= TM);
+  int other = kStage;
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) load(i);
+  advance(other);
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) load(i);
+  advance(-other);
+  __builtin_amdgcn_s_waitcnt(waitcnt_vm(LOADS));
+  block_barrier();
+#pragma unroll
+  for (int n = 0; n < TN; ++n) fb[0][n] = ob.get(n, 0);
+#pragma unroll
+  for (int m = 0; m < TM; ++m) fa[m] = oa.get(m, 0);
+  if constexpr (!A_KFIRST) oa.turn(0, other);
+  if constexpr (!B_KFIRST) ob.turn(0, other);
+  for (int s = 0; s < k_count; s += BK) {
+    half(std::integral_constant<int, 0>{});
+    if constexpr (A_KFIRST) oa.turn(0, other);
+    if constexpr (B_KFIRST) ob.turn(0, other);
+    half(std::integral_constant<int, 1>{});
+    oa.turn(1, other);
+    ob.turn(1, other);
+    advance(other);
+    other = -other;
+    if constexpr (!A_KFIRST) oa.turn(0, other);
+    if constexpr (!B_KFIRST) ob.turn(0, other);
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing is on its way into this block's LDS when it ends
 
   // lane: row r of a tile, columns 4 g .. 4 g + 3
+  constexpr int UNITS = TN / 2;
   const int r = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
   const int64_t N = p.N;
-#pragma unroll
-  for (int m = 0; m < TM; ++m) {
+  const int col0 = n0 + wn * TN * 16;
+  // the saved rows of AHEAD rows of tiles are on their way
+  constexpr int AHEAD = KIND == kGatedBwd ? 3 : 1, FETCHED = KIND == kGatedBwd ? UNITS : 1;
+  Saved<T> saved[AHEAD][FETCHED];
+  auto fetch_saved = [&](int m) {
     const int64_t row = m0 + (wm * TM + m) * 16 + r;
-    const bool ok = row < p.M;
-    if constexpr (KIND == kPlain) {
-      const int col = n0 + wn * TN * 16;
-      if (p.part) {
-        float* out = p.part + ((int64_t)split * p.M + row) * N;
 #pragma unroll
-        for (int n = 0; n < TN; ++n)
-          if (ok && col + 16 * n + 4 * g < N) *(floatx4_t*)(out + col + 16 * n + 4 * g) = acc[m][n];
+    for (int u = 0; u < FETCHED; ++u) saved[m % AHEAD][u].load(p.saved + row * 2 * N, N, col0 + 32 * u, g, row < p.M);
+  };
+  auto rows = [&](auto act) {
+    constexpr int ACT = act.value;
+#pragma unroll
+    for (int m = 0; m < TM; ++m) {
+      const int64_t row = m0 + (wm * TM + m) * 16 + r;
+      const bool ok = row < p.M;
+      __builtin_amdgcn_sched_barrier(0);   // a row of tiles at a time: all of them do not fit the registers
+      if constexpr (KIND == kPlain) {
+        if (p.part) {
+          float* out = p.part + ((int64_t)split * p.M + row) * N;
+#pragma unroll
+          for (int u = 0; u < UNITS; ++u) put_unit(out, col0 + 32 * u, g, N, ok, acc[m][2 * u], acc[m][2 * u + 1]);
+        } else {
+#pragma unroll
+          for (int u = 0; u < UNITS; ++u) put_unit(p.c + row * N, col0 + 32 * u, g, N, ok, acc[m][2 * u], acc[m][2 * u + 1]);
+        }
+      } else if constexpr (KIND == kGated) {
+        static_assert(UNITS == 2);   // of 64 columns the first unit is a's, the second u's
+        const int col = n0 + wn * TN * 8;
+        floatx4_t h[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float f, slope;
+            activate<T, ACT>(acc[m][t][i], f, slope);
+            h[t][i] = f * acc[m][t + 2][i];
+          }
+        put_unit(p.c + row * N, col, g, N, ok, h[0], h[1]);
+        if (p.c2) {
+          put_unit(p.c2 + row * 2 * N, col, g, N, ok, acc[m][0], acc[m][1]);
+          put_unit(p.c2 + row * 2 * N + N, col, g, N, ok, acc[m][2], acc[m][3]);
+        }
       } else {
 #pragma unroll
-        for (int n = 0; n < TN; n += 2) put_pair(p.c + row * N, col + 16 * n, g, ok ? N : 0, acc[m][n], acc[m][n + 1]);
+        for (int u = 0; u < UNITS; ++u)
+          saved[m % AHEAD][u].template put<ACT>(p.c + row * 2 * N, N, col0 + 32 * u, g, ok, acc[m][2 * u], acc[m][2 * u + 1]);
+        if (m + AHEAD < TM) fetch_saved(m + AHEAD);
       }
-    } else if constexpr (KIND == kGated) {
-      const int col = n0 + wn * TN * 8;
-      static_assert(TN == 4);
-      floatx4_t h[2];
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float f, slope;
-          activate<T>(p.act, acc[m][n][i], f, slope);
-          h[n][i] = f * acc[m][n + 2][i];
-        }
-      put_pair(p.c + row * N, col, g, ok ? N : 0, h[0], h[1]);
-      if (p.c2) {
-        put_pair(p.c2 + row * 2 * N, col, g, ok ? N : 0, acc[m][0], acc[m][1]);
-        put_pair(p.c2 + row * 2 * N + N, col, g, ok ? N : 0, acc[m][2], acc[m][3]);
-      }
-    } else {
-      const int col = n0 + wn * TN * 16;
-#pragma unroll
-      for (int n = 0; n < TN; n += 2)
-        grad_pair(p.saved + (ok ? row : 0) * 2 * N, p.c + (ok ? row : 0) * 2 * N, ok ? N : 0, col + 16 * n, g, p.act, acc[m][n], acc[m][n + 1]);
     }
-  }
+  };
+  if constexpr (KIND == kGatedBwd)
+#pragma unroll
+    for (int m = 0; m < AHEAD && m < TM; ++m) fetch_saved(m);
+  if constexpr (KIND == kPlain) rows(std::integral_constant<int, 0>{});
+  else with_activation(p.act, rows);
 }
-
 
 // Sums of the splits, in their order, rounded once.
 template <typename T>
@@ -291,7 +396,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(const Product<T> p) {
 #pragma unroll
         for (int t = 0; t < TT; ++t)
 #pragma unroll
-          for (int s = 0; s < SETS; ++s) acc[s][t] = mfma_frag(fb[u][h][s], fa[u][h][t], acc[s][t]);
+          for (int s = 0; s < SETS; ++s) mfma_frag(acc[s][t], fb[u][h][s], fa[u][h][t]);
   }
 #pragma unroll
   for (int s = 0; s < SETS; ++s)
@@ -315,12 +420,14 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(const Product<T> p) {
     };
     if constexpr (GATED) {
       floatx4_t h;
+      with_activation(p.act, [&](auto act) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float f, slope;
-        activate<T>(p.act, v[0][i], f, slope);
-        h[i] = f * v[1][i];
-      }
+        for (int i = 0; i < 4; ++i) {
+          float f, slope;
+          activate<T, act.value>(v[0][i], f, slope);
+          h[i] = f * v[1][i];
+        }
+      });
       put(p.c + row * N + col, h);
       if (p.c2) {
         put(p.c2 + row * 2 * N + col, v[0]);
