@@ -76,11 +76,14 @@ struct Product {
   T* c;                  // [M][N]; kGated: h; kGatedBwd: [da, du], [M][2 N]
   T* c2;                 // kGated: [a, u], [M][2 N], or NULL
   const T* saved;        // kGatedBwd: [a, u]
-  float* part;           // of split products: [split][M][N], or NULL
+  // blocks below `whole` have a tile each, the `left` tiles behind them are split along k: block whole + split * left + tile
+  unsigned tiles_m, tiles_n, whole, left;
   int64_t k_each;        // k of a split
-  unsigned tiles_m, tiles_n;
+  float* part;           // their sums, [split][left][BM][BN], or NULL for splits of all of k
 };
 
+__device__ __forceinline__ float value_of(float v) { return v; }
+__device__ __forceinline__ float value_of(unsigned short v) { return bf16_bits_to_f32(v); }
 __device__ __forceinline__ uintx2_t pack4(floatx4_t v) { return uintx2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}; }
 
 // The columns of a wave's sums in units of two neighbouring tiles: lane group g holds columns 4 g .. of either.  Lanes exchange fours, after which
@@ -198,16 +201,17 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_kernel(const Product<
   const unsigned lds = lds_addr_uniform(s_mem);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
 
-  const unsigned tiles = p.tiles_m * p.tiles_n, split = blockIdx.x / tiles;
+  const bool is_split = p.part && blockIdx.x >= p.whole;
+  const unsigned behind = is_split ? blockIdx.x - p.whole : 0, split = is_split ? behind / p.left : 0;
   unsigned bm, bn;
-  tile_of(blockIdx.x % tiles, p.tiles_m, p.tiles_n, bm, bn);
+  tile_of(is_split ? p.whole + behind - split * p.left : blockIdx.x, p.tiles_m, p.tiles_n, bm, bn);
 
   const int64_t m0 = (int64_t)bm * BM, k0 = split * p.k_each;
-  const int n0 = bn * (KIND == kGated ? BN / 2 : BN), k_count = (int)min(p.k_each, p.K - k0);
+  const int n0 = bn * (KIND == kGated ? BN / 2 : BN), k_count = (int)(is_split ? min(p.k_each, p.K - k0) : p.K);
   OpA oa;
   OpB ob;
   oa.init(p.a, p.lda, m0, p.M, k0, k_count, wm * TM, lds);
-  if constexpr (KIND == kGated) ob.init_paired(p.b, p.ldb, n0, p.N, k_count, wn * TN, lds + OpA::kBytes);
+  if constexpr (KIND == kGated) ob.init_paired(p.b + k0, p.ldb, n0, p.N, k_count, wn * TN, lds + OpA::kBytes);
   else ob.init(p.b, p.ldb, n0, p.N, k0, k_count, wn * TN, lds + OpA::kBytes);
 
   // the i-th of the thread's loads of a step; past the last step they are zeros
@@ -284,6 +288,14 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_kernel(const Product<
   const int r = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
   const int64_t N = p.N;
   const int col0 = n0 + wn * TN * 16;
+  if (is_split) {
+    float* out = p.part + (size_t)behind * BM * BN + wn * TN * 16;
+#pragma unroll
+    for (int m = 0; m < TM; ++m)
+#pragma unroll
+      for (int n = 0; n < TN; ++n) *(floatx4_t*)(out + ((wm * TM + m) * 16 + r) * BN + 16 * n + 4 * g) = acc[m][n];
+    return;
+  }
   // the saved rows of AHEAD rows of tiles are on their way
   constexpr int AHEAD = KIND == kGatedBwd ? 3 : 1, FETCHED = KIND == kGatedBwd ? UNITS : 1;
   Saved<T> saved[AHEAD][FETCHED];
@@ -300,14 +312,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_kernel(const Product<
       const bool ok = row < p.M;
       __builtin_amdgcn_sched_barrier(0);   // a row of tiles at a time: all of them do not fit the registers
       if constexpr (KIND == kPlain) {
-        if (p.part) {
-          float* out = p.part + ((int64_t)split * p.M + row) * N;
 #pragma unroll
-          for (int u = 0; u < UNITS; ++u) put_unit(out, col0 + 32 * u, g, N, ok, acc[m][2 * u], acc[m][2 * u + 1]);
-        } else {
-#pragma unroll
-          for (int u = 0; u < UNITS; ++u) put_unit(p.c + row * N, col0 + 32 * u, g, N, ok, acc[m][2 * u], acc[m][2 * u + 1]);
-        }
+        for (int u = 0; u < UNITS; ++u) put_unit(p.c + row * N, col0 + 32 * u, g, N, ok, acc[m][2 * u], acc[m][2 * u + 1]);
       } else if constexpr (KIND == kGated) {
         static_assert(UNITS == 2);   // of 64 columns the first unit is a's, the second u's
         const int col = n0 + wn * TN * 8;
@@ -340,15 +346,75 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_kernel(const Product<
   else with_activation(p.act, rows);
 }
 
-// Sums of the splits, in their order, rounded once.
-template <typename T>
-__global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ part, int splits, int64_t n, T* __restrict__ c) {
-  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * 1024) {
-    floatx4_t s = *(const floatx4_t*)(part + i);
+// Tiles that were split along k: the sums of their splits, in order, and what a block does with its sums.  A thread has eight columns of a row (kGated:
+// of a, and the same eight of u); blockIdx.x is the tile, blockIdx.y a run of its rows.
+template <typename T, Kind KIND, int BM, int BN>
+__global__ __launch_bounds__(256) void join_kernel(const Product<T> p, int splits) {
+  constexpr int COLS = KIND == kGated ? BN / 2 : BN, SETS = KIND == kGated ? 2 : 1, PER = COLS / 8;
+  unsigned bm, bn;
+  tile_of(p.whole + blockIdx.x, p.tiles_m, p.tiles_n, bm, bn);
+  const int at = blockIdx.y * 256 + threadIdx.x, r = at / PER, c = at % PER * 8;
+  const int64_t row = (int64_t)bm * BM + r, N = p.N;
+  const int col = bn * COLS + c;
+  if (row >= p.M || col >= N) return;
+  floatx4_t v[SETS][2];
+#pragma unroll
+  for (int s = 0; s < SETS; ++s) {
+    // of each 64 staged columns 32 are a's, 32 u's
+    const float* in = p.part + ((size_t)blockIdx.x * BM + r) * BN + (KIND == kGated ? (c >> 5) * 64 + s * 32 + (c & 31) : c);
+    v[s][0] = v[s][1] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int k = 1; k < splits; ++k) s += *(const floatx4_t*)(part + k * n + i);
-    if constexpr (sizeof(T) == 4) *(floatx4_t*)(c + i) = s;
-    else *(uintx2_t*)(c + i) = pack4(s);
+    for (int k = 0; k < splits; ++k) {
+      v[s][0] += *(const floatx4_t*)(in + (size_t)k * p.left * BM * BN);
+      v[s][1] += *(const floatx4_t*)(in + (size_t)k * p.left * BM * BN + 4);
+    }
+  }
+  // fp32: N is a multiple of 4
+  auto put = [&](T* to, floatx4_t x, floatx4_t y) {
+    if constexpr (sizeof(T) == 4) {
+      *(floatx4_t*)to = x;
+      if (col + 4 < N) *(floatx4_t*)(to + 4) = y;
+    } else {
+      const uintx2_t a = pack4(x), b = pack4(y);
+      *(uintx4_t*)to = uintx4_t{a[0], a[1], b[0], b[1]};
+    }
+  };
+  if constexpr (KIND == kPlain) {
+    put(p.c + row * N + col, v[0][0], v[0][1]);
+  } else {
+    with_activation(p.act, [&](auto act) {
+      if constexpr (KIND == kGated) {
+        floatx4_t h[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float f, slope;
+            activate<T, act.value>(v[0][t][i], f, slope);
+            h[t][i] = f * v[1][t][i];
+          }
+        put(p.c + row * N + col, h[0], h[1]);
+        if (p.c2) {
+          put(p.c2 + row * 2 * N + col, v[0][0], v[0][1]);
+          put(p.c2 + row * 2 * N + N + col, v[1][0], v[1][1]);
+        }
+      } else {
+        const T *a = p.saved + row * 2 * N + col, *u = a + N;
+        floatx4_t da[2], du[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (sizeof(T) == 4 && col + 4 * t >= N) break;
+            float f, slope;
+            activate<T, act.value>(value_of(a[4 * t + i]), f, slope);
+            da[t][i] = v[0][t][i] * value_of(u[4 * t + i]) * slope;
+            du[t][i] = v[0][t][i] * f;
+          }
+        put(p.c + row * 2 * N + col, da[0], da[1]);
+        put(p.c + row * 2 * N + N + col, du[0], du[1]);
+      }
+    });
   }
 }
 
@@ -442,12 +508,13 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(const Product<T> p) {
 // ---- host ----
 constexpr int kFewTokens = 64;
 
-// How a product is cut: blocks of 256 x 256 or 128 x 128, K in `splits` runs of k_each.
+// How a product is cut: blocks of 256 x 256 or 128 x 128; whole rounds of them, and the tiles behind those in `splits` runs of k_each along k.
 struct Cut {
   bool big;
   int splits;
   int64_t k_each;
-  unsigned tiles_m, tiles_n;
+  unsigned tiles_m, tiles_n, whole, left;
+  size_t part_bytes() const { return splits > 1 ? (size_t)splits * left * (big ? 65536 : 16384) * sizeof(float) : 0; }
 };
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -459,44 +526,45 @@ Cut cut_of(int64_t M, int64_t N, int64_t K, int dtype, Kind kind) {
   for (int big = 0; big < (dtype == MOGA_F32 ? 1 : 2); ++big) {
     const int bm = big ? 256 : 128, bn = (big ? 256 : 128) / (kind == kGated ? 2 : 1);
     const int64_t tiles = ceil_div(M, bm) * ceil_div(N, bn);
-    // microseconds: a step of a full chip's blocks, a block's start and end, and the sums of the splits written and read
-    const double step = big ? 1.7 : 1.0, ends = big ? 8 : 4, resident = big ? 256 : 512;
-    for (int s = 1; s <= (kind == kPlain ? 32 : 1); ++s) {
+    // microseconds: a step of a full chip's blocks, a block's start and end, what writing a split's sums adds to it
+    const double step = (big ? 1.45 : 1.0) * (dtype == MOGA_F32 ? 4 : 1), ends = big ? 12 : 7, sums = big ? 6 : 3;
+    const int64_t resident = big ? 256 : 512, whole = tiles / resident * resident, left = tiles - whole;
+    for (int s = 1; s <= 32; ++s) {
       const int64_t each = ceil_div(steps, s);
-      if (s > 1 && (each < 8 || ceil_div(steps, each) != s)) continue;
-      const double cost = std::ceil(tiles * s / resident) * (each * step + ends) + (s > 1 ? 6 + M * N * 4. * (2 * s) / 4e6 : 0);
+      if (s > 1 && (left == 0 || each < 4 || ceil_div(steps, each) != s)) continue;
+      double cost = whole / resident * (steps * step + ends);
+      if (left) cost += ceil_div(left * s, resident) * (each * step + ends);
+      if (s > 1) cost += 5 + ceil_div(left * s, resident) * sums + left * s * (big ? 0.07 : 0.018);
       if (least == 0 || cost < least) {
         least = cost;
-        best = {big != 0, s, s > 1 ? each * bk : K, (unsigned)ceil_div(M, bm), (unsigned)ceil_div(N, bn)};
+        best = {big != 0, s, s > 1 ? each * bk : K, (unsigned)ceil_div(M, bm), (unsigned)ceil_div(N, bn), (unsigned)(s > 1 ? whole : tiles),
+                (unsigned)(s > 1 ? left : 0)};
       }
     }
   }
   return best;
 }
 
-size_t part_bytes(int64_t M, int64_t N, int64_t K, int dtype) {
-  const Cut c = cut_of(M, N, K, dtype, kPlain);
-  return c.splits > 1 ? round_up((size_t)c.splits * M * N * sizeof(float), 256) : 0;
+template <typename T, Kind KIND, bool AK, bool BK, int WN, int TM>
+void launch_tiles(const Product<T>& p, int splits, hipStream_t st) {
+  constexpr int BM = 32 * TM, BN = 64 * WN;
+  product_kernel<T, KIND, AK, BK, 2, WN, TM, 4><<<p.whole + p.left * splits, 128 * WN, 0, st>>>(p);
+  if (p.left) join_kernel<T, KIND, BM, BN><<<dim3(p.left, BM * BN / (KIND == kGated ? 4096 : 2048)), 256, 0, st>>>(p, splits);
 }
 
 template <typename T, Kind KIND, bool AK, bool BK>
-void launch_product(Product<T> p, int dtype, float* part, hipStream_t st) {
+void launch_product(Product<T> p, int dtype, void* part, hipStream_t st) {
   const Cut c = cut_of(p.M, p.N, p.K, dtype, KIND);
   p.tiles_m = c.tiles_m;
   p.tiles_n = c.tiles_n;
+  p.whole = c.whole;
+  p.left = c.left;
   p.k_each = c.k_each;
-  p.part = c.splits > 1 ? part : nullptr;
-  const unsigned blocks = c.tiles_m * c.tiles_n * c.splits;
+  p.part = c.splits > 1 ? (float*)part : nullptr;
   if constexpr (sizeof(T) == 2) {
-    if (c.big) product_kernel<T, KIND, AK, BK, 2, 4, 8, 4><<<blocks, 512, 0, st>>>(p);
-    else product_kernel<T, KIND, AK, BK, 2, 2, 4, 4><<<blocks, 256, 0, st>>>(p);
-  } else {
-    product_kernel<T, KIND, AK, BK, 2, 2, 4, 4><<<blocks, 256, 0, st>>>(p);
+    if (c.big) return launch_tiles<T, KIND, AK, BK, 4, 8>(p, c.splits, st);
   }
-  if (c.splits > 1) {
-    const int64_t n = p.M * p.N;
-    join_kernel<T><<<(unsigned)std::min<int64_t>(4096, ceil_div(n, 1024)), 256, 0, st>>>(part, c.splits, n, p.c);
-  }
+  launch_tiles<T, KIND, AK, BK, 2, 4>(p, c.splits, st);
 }
 
 template <typename T, bool GATED>
@@ -540,29 +608,31 @@ void ffn_fwd(const void* x, const void* w_in, const void* w_out, int dtype, int6
     launch_few<T, true>(in, st);
     launch_few<T, false>(out, st);
   } else {
-    launch_product<T, kGated, false, false>(in, dtype, nullptr, st);
-    launch_product<T, kPlain, false, false>(out, dtype, (float*)ws, st);
+    launch_product<T, kGated, false, false>(in, dtype, ws, st);
+    launch_product<T, kPlain, false, false>(out, dtype, ws, st);
   }
 }
 
-// Workspace of the backward: [da, du], and the splits of one product after the other.
-struct FfnBwdWs {
-  size_t part, bytes;   // offset of the splits; all
-  FfnBwdWs(int64_t N, int C, int F, int dtype) {
-    part = round_up((size_t)N * 2 * F * elem_size(dtype), 256);
-    bytes = part + std::max({part_bytes(N, C, 2 * (int64_t)F, dtype), part_bytes(2 * (int64_t)F, C, N, dtype), part_bytes(C, F, N, dtype)});
-  }
-};
+// Workspaces hold the splits of one product after the other, the backward's [da, du] before them.
+size_t ffn_fwd_ws(int64_t N, int C, int F, int dtype) {
+  return N <= kFewTokens ? 0 : std::max(cut_of(N, F, C, dtype, kGated).part_bytes(), cut_of(N, C, F, dtype, kPlain).part_bytes());
+}
+size_t ffn_bwd_part(int64_t N, int F, int dtype) { return round_up((size_t)N * 2 * F * elem_size(dtype), 256); }
+size_t ffn_bwd_ws(int64_t N, int C, int F, int dtype) {
+  const int64_t F2 = 2 * (int64_t)F;
+  return ffn_bwd_part(N, F, dtype) + std::max({cut_of(N, F, C, dtype, kGatedBwd).part_bytes(), cut_of(N, C, F2, dtype, kPlain).part_bytes(),
+                                               cut_of(F2, C, N, dtype, kPlain).part_bytes(), cut_of(C, F, N, dtype, kPlain).part_bytes()});
+}
 
 template <typename T>
 void ffn_bwd(const void* d_y, const void* x, const void* w_in, const void* w_out, const void* au, const void* h, int dtype, int64_t N, int C, int F,
              int act, void* d_x, void* d_w_in, void* d_w_out, void* ws, hipStream_t st) {
-  float* part = (float*)((char*)ws + FfnBwdWs(N, C, F, dtype).part);
+  void* part = (char*)ws + ffn_bwd_part(N, F, dtype);
   if (d_x || d_w_in) {
     Product<T> dh = product<T>(d_y, C, w_out, F, N, F, C, ws);
     dh.saved = (const T*)au;
     dh.act = act;
-    launch_product<T, kGatedBwd, false, true>(dh, dtype, nullptr, st);
+    launch_product<T, kGatedBwd, false, true>(dh, dtype, part, st);
   }
   if (d_x) launch_product<T, kPlain, false, true>(product<T>(ws, 2 * (int64_t)F, w_in, C, N, C, 2 * (int64_t)F, d_x), dtype, part, st);
   if (d_w_in) launch_product<T, kPlain, true, true>(product<T>(ws, 2 * (int64_t)F, x, C, 2 * (int64_t)F, C, N, d_w_in), dtype, part, st);
@@ -586,12 +656,10 @@ int check_ffn(int64_t N, int C, int F, int dtype, int act) {
 using namespace moga;
 
 extern "C" size_t moga_gated_ffn_fwd_ws_bytes(int64_t N, int C, int F, int dtype) {
-  if (check_ffn(N, C, F, dtype, MOGA_ACT_SILU) != MOGA_OK || N <= kFewTokens) return 0;
-  return part_bytes(N, C, F, dtype);
+  return check_ffn(N, C, F, dtype, MOGA_ACT_SILU) == MOGA_OK && N > 0 ? ffn_fwd_ws(N, C, F, dtype) : 0;
 }
 extern "C" size_t moga_gated_ffn_bwd_ws_bytes(int64_t N, int C, int F, int dtype) {
-  if (check_ffn(N, C, F, dtype, MOGA_ACT_SILU) != MOGA_OK || N == 0) return 0;
-  return FfnBwdWs(N, C, F, dtype).bytes;
+  return check_ffn(N, C, F, dtype, MOGA_ACT_SILU) == MOGA_OK && N > 0 ? ffn_bwd_ws(N, C, F, dtype) : 0;
 }
 
 extern "C" int moga_gated_ffn_fwd(const void* x, const void* w_in, const void* w_out, int dtype, int64_t N, int C, int F, int activation, void* h,
