@@ -191,7 +191,7 @@ template <> struct Saved<float> {
 
 // WM x WN waves, TM x TN tiles of 16 x 16 each
 template <typename T, Kind KIND, bool A_KFIRST, bool B_KFIRST, int WM, int WN, int TM, int TN>
-__global__ __launch_bounds__(64 * WM * WN, 2) void product_kernel(const Product<T> p) {
+__global__ __launch_bounds__(64 * WM * WN, TM == 2 ? 3 : 2) void product_kernel(const Product<T> p) {
   constexpr int THREADS = 64 * WM * WN, BM = 16 * WM * TM, BN = 16 * WN * TN;
   using OpA = Operand<T, A_KFIRST, BM, THREADS, TM>;
   using OpB = Operand<T, B_KFIRST, BN, THREADS, TN>;
@@ -236,7 +236,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_kernel(const Product<
   // the next step's has landed.
   Frag<T> fa[TM], fb[2][TN];
   auto half = [&](auto which) {
-    constexpr int H = which.value, PER = (LOADS + TM - 1) / TM;
+    constexpr int H = which.value, PER = (LOADS + TM - 1) / TM, FB = (TN + TM - 1) / TM;
 #pragma unroll
     for (int m = 0; m < TM; ++m) {
 #pragma unroll
@@ -249,11 +249,11 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_kernel(const Product<
 #pragma unroll
         for (int i = m * PER; i < (m + 1) * PER && i < LOADS; ++i) load(i);
       fa[m] = oa.get(m, 1 - H);
-      if (m < TN) fb[1 - H][m] = ob.get(m, 1 - H);
+#pragma unroll
+      for (int n = m * FB; n < (m + 1) * FB && n < TN; ++n) fb[1 - H][n] = ob.get(n, 1 - H);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  static_assert(TN <= TM);
   int other = kStage;
 #pragma unroll
   for (int i = 0; i < LOADS; ++i) load(i);
@@ -421,13 +421,15 @@ __global__ __launch_bounds__(256) void join_kernel(const Product<T> p, int split
 // ---- few tokens ----
 // A block owns 16 columns of C (GATED: 16 of a and the same 16 of u) for up to 16 TT tokens.  Its waves take turns of 128 bytes of k, so that a weight
 // is read once, a line at a time, and their sums meet in LDS.  Loads past k, F or the last token give zeros (buffer bounds).
-template <typename T, bool GATED, int TT, int WAVES>
+template <typename T, bool GATED, int TT, int WAVES, int U>
 __global__ __launch_bounds__(64 * WAVES) void few_kernel(const Product<T> p) {
-  constexpr int ES = sizeof(T), V = 16 / ES, SETS = GATED ? 2 : 1, U = TT == 1 ? 4 : 2;
+  constexpr int ES = sizeof(T), SETS = GATED ? 2 : 1;
   __shared__ floatx4_t s_sum[WAVES][SETS * TT][64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, r = l & 15, g = l >> 4;
   const int n0 = blockIdx.x * 16, N = p.N;
-  const int row_bytes = (int)(p.K * ES);
+  const int row_bytes = (int)(p.ldb * ES);
+  // this block's bytes of a row
+  const int first = (int)(blockIdx.y * p.k_each * ES), end = min(row_bytes, first + (int)(p.k_each * ES));
   auto rsrc = [](const T* base) { return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)kBufferBytes, 0x00020000); };
   const auto ra = rsrc(p.a);
   const auto rb = rsrc(p.b + (int64_t)n0 * p.ldb), rb2 = rsrc(p.b + ((int64_t)N + n0) * p.ldb);
@@ -440,21 +442,26 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(const Product<T> p) {
   for (int s = 0; s < SETS; ++s)
 #pragma unroll
     for (int t = 0; t < TT; ++t) acc[s][t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-  for (int k = wave * 128; k < row_bytes; k += WAVES * 128 * U) {
-    Frag<T> fb[U][2][SETS], fa[U][2][TT];
+  // two sets of U lines in turn: one on its way while the products of the other run
+  Frag<T> fb[2][U][2][SETS], fa[2][U][2][TT];
+  auto fetch = [&](auto which, int k) {
+    constexpr int H = which.value;
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int at = k + u * WAVES * 128 + h * 64;
-        const bool in = at + g * 16 < row_bytes;
+        const bool in = at + g * 16 < end;
         const unsigned b = in ? vb : kPastBuffer;
-        fb[u][h][0].v = __builtin_bit_cast(decltype(fb[u][h][0].v), __builtin_amdgcn_raw_buffer_load_b128(rb, b, at, 0));
-        if constexpr (GATED) fb[u][h][1].v = __builtin_bit_cast(decltype(fb[u][h][1].v), __builtin_amdgcn_raw_buffer_load_b128(rb2, b, at, 0));
+        auto get = [&](auto& f, auto rs, unsigned v) { f.v = __builtin_bit_cast(decltype(f.v), __builtin_amdgcn_raw_buffer_load_b128(rs, v, at, 0)); };
+        get(fb[H][u][h][0], rb, b);
+        if constexpr (GATED) get(fb[H][u][h][1], rb2, b);
 #pragma unroll
-        for (int t = 0; t < TT; ++t)
-          fa[u][h][t].v = __builtin_bit_cast(decltype(fa[u][h][t].v), __builtin_amdgcn_raw_buffer_load_b128(ra, in ? va[t] : kPastBuffer, at, 0));
+        for (int t = 0; t < TT; ++t) get(fa[H][u][h][t], ra, in ? va[t] : kPastBuffer);
       }
+  };
+  auto multiply = [&](auto which) {
+    constexpr int H = which.value;
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -462,7 +469,19 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(const Product<T> p) {
 #pragma unroll
         for (int t = 0; t < TT; ++t)
 #pragma unroll
-          for (int s = 0; s < SETS; ++s) mfma_frag(acc[s][t], fb[u][h][s], fa[u][h][t]);
+          for (int s = 0; s < SETS; ++s) mfma_frag(acc[s][t], fb[H][u][h][s], fa[H][u][h][t]);
+  };
+  constexpr int STEP = WAVES * 128 * U;
+  const std::integral_constant<int, 0> even;
+  const std::integral_constant<int, 1> odd;
+  int k = first + wave * 128;
+  if (k < end) fetch(even, k);
+  for (; k < end; k += 2 * STEP) {
+    if (k + STEP < end) fetch(odd, k + STEP);
+    multiply(even);
+    if (k + STEP >= end) break;
+    if (k + 2 * STEP < end) fetch(even, k + 2 * STEP);
+    multiply(odd);
   }
 #pragma unroll
   for (int s = 0; s < SETS; ++s)
@@ -480,6 +499,10 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(const Product<T> p) {
       for (int w = 1; w < WAVES; ++w) v[s] += s_sum[w][s * TT + t][l];
     }
     if (row >= p.M || col >= N) continue;
+    if (!GATED && p.part) {
+      *(floatx4_t*)(p.part + ((int64_t)blockIdx.y * p.M + row) * N + col) = v[0];
+      continue;
+    }
     auto put = [&](T* at, floatx4_t x) {
       if constexpr (ES == 4) *(floatx4_t*)at = x;
       else *(uintx2_t*)at = pack4(x);
@@ -505,16 +528,42 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(const Product<T> p) {
   }
 }
 
-// ---- host ----
-constexpr int kFewTokens = 64;
+// Sums of the splits of few tokens' rows, in order, rounded once.
+template <typename T>
+__global__ __launch_bounds__(64) void few_join_kernel(const float* __restrict__ part, int splits, int64_t n, T* __restrict__ c) {
+  const int64_t i = ((int64_t)blockIdx.x * 64 + threadIdx.x) * 4;
+  if (i >= n) return;
+  floatx4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int k = 0; k < splits; ++k) s += *(const floatx4_t*)(part + k * n + i);
+  if constexpr (sizeof(T) == 4) *(floatx4_t*)(c + i) = s;
+  else *(uintx2_t*)(c + i) = pack4(s);
+}
 
-// How a product is cut: blocks of 256 x 256 or 128 x 128; whole rounds of them, and the tiles behind those in `splits` runs of k_each along k.
+// ---- host ----
+constexpr int kFewTokens = 64, kFewBlocks = 1280;
+
+// Few tokens go by the weights' rows: 16 at least, more while what their blocks read of x (N C F / 8 values, some 9 TB/s from the caches) takes less
+// than what tiles cost beside the weights, 10 us and a tenth of their time.  bf16, us by rows and by tiles: 64 x 1536 x 4096 23 and 26, 16 x 5120 x
+// 13696 103 and 112, 17 tokens 123 and 112; fp32, where tiles of 128 are bound by their products: 64 x 1536 x 4096 41 and 67.
+bool few_tokens(int64_t N, int C, int F, int dtype) {
+  if (N <= 16 || dtype == MOGA_F32) return N <= kFewTokens;
+  const double weights = 3. * C * F * 2 / 4.7e6;
+  return N <= kFewTokens && (double)N * C * F / 8 * 2 / 9e6 <= 10 + 0.1 * weights;
+}
+
+// How a product is cut: blocks of 256 x 256, 128 x 128 or 64 x 128, whole rounds of them, and the tiles behind those in `splits` runs of k_each along k.
+struct TileShape {
+  int bm, bn, resident;       // rows and columns; blocks on the chip at a time
+  // microseconds: a step of bf16 and of fp32 with all of them running, a block's start and end, what writing a split's sums adds to it
+  double step, step32, ends, sums;
+};
+constexpr TileShape kTiles[] = {{256, 256, 256, 1.45, 0, 12, 6}, {128, 128, 512, 1.0, 4.1, 7, 3}, {64, 128, 768, 0.9, 3.2, 6, 2}};
 struct Cut {
-  bool big;
-  int splits;
+  int shape, splits;
   int64_t k_each;
   unsigned tiles_m, tiles_n, whole, left;
-  size_t part_bytes() const { return splits > 1 ? (size_t)splits * left * (big ? 65536 : 16384) * sizeof(float) : 0; }
+  size_t part_bytes() const { return splits > 1 ? (size_t)splits * left * kTiles[shape].bm * kTiles[shape].bn * sizeof(float) : 0; }
 };
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -523,22 +572,20 @@ Cut cut_of(int64_t M, int64_t N, int64_t K, int dtype, Kind kind) {
   const int64_t steps = ceil_div(K, bk);
   Cut best{};
   double least = 0;
-  for (int big = 0; big < (dtype == MOGA_F32 ? 1 : 2); ++big) {
-    const int bm = big ? 256 : 128, bn = (big ? 256 : 128) / (kind == kGated ? 2 : 1);
-    const int64_t tiles = ceil_div(M, bm) * ceil_div(N, bn);
-    // microseconds: a step of a full chip's blocks, a block's start and end, what writing a split's sums adds to it
-    const double step = (big ? 1.45 : 1.0) * (dtype == MOGA_F32 ? 4 : 1), ends = big ? 12 : 7, sums = big ? 6 : 3;
-    const int64_t resident = big ? 256 : 512, whole = tiles / resident * resident, left = tiles - whole;
+  for (int shape = dtype == MOGA_F32 ? 1 : 0; shape < 3; ++shape) {
+    const TileShape& t = kTiles[shape];
+    const double step = dtype == MOGA_F32 ? t.step32 : t.step, mb = t.bm * t.bn * 4e-6;   // a tile's sums in MB
+    const int64_t tiles_m = ceil_div(M, t.bm), tiles_n = ceil_div(N, kind == kGated ? t.bn / 2 : t.bn), tiles = tiles_m * tiles_n;
+    const int64_t whole = tiles / t.resident * t.resident, left = tiles - whole;
     for (int s = 1; s <= 32; ++s) {
       const int64_t each = ceil_div(steps, s);
       if (s > 1 && (left == 0 || each < 4 || ceil_div(steps, each) != s)) continue;
-      double cost = whole / resident * (steps * step + ends);
-      if (left) cost += ceil_div(left * s, resident) * (each * step + ends);
-      if (s > 1) cost += 5 + ceil_div(left * s, resident) * sums + left * s * (big ? 0.07 : 0.018);
+      double cost = whole / t.resident * (steps * step + t.ends);
+      if (left) cost += ceil_div(left * s, t.resident) * (each * step + t.ends);
+      if (s > 1) cost += 5 + ceil_div(left * s, t.resident) * t.sums + left * s * mb * 0.27;
       if (least == 0 || cost < least) {
         least = cost;
-        best = {big != 0, s, s > 1 ? each * bk : K, (unsigned)ceil_div(M, bm), (unsigned)ceil_div(N, bn), (unsigned)(s > 1 ? whole : tiles),
-                (unsigned)(s > 1 ? left : 0)};
+        best = {shape, s, s > 1 ? each * bk : K, (unsigned)tiles_m, (unsigned)tiles_n, (unsigned)(s > 1 ? whole : tiles), (unsigned)(s > 1 ? left : 0)};
       }
     }
   }
@@ -562,24 +609,35 @@ void launch_product(Product<T> p, int dtype, void* part, hipStream_t st) {
   p.k_each = c.k_each;
   p.part = c.splits > 1 ? (float*)part : nullptr;
   if constexpr (sizeof(T) == 2) {
-    if (c.big) return launch_tiles<T, KIND, AK, BK, 4, 8>(p, c.splits, st);
+    if (c.shape == 0) return launch_tiles<T, KIND, AK, BK, 4, 8>(p, c.splits, st);
   }
-  launch_tiles<T, KIND, AK, BK, 2, 4>(p, c.splits, st);
+  if (c.shape == 1) launch_tiles<T, KIND, AK, BK, 2, 4>(p, c.splits, st);
+  else launch_tiles<T, KIND, AK, BK, 2, 2>(p, c.splits, st);
+}
+
+// Few tokens: a block for every 16 columns and, of a plain product with fewer than kFewBlocks of those, every run of k, no shorter than 1 KB.
+int64_t few_splits(int N, int64_t K, int dtype) {
+  const int64_t blocks = ceil_div(N, 16), bytes = K * elem_size(dtype);
+  const int64_t s = std::max<int64_t>(1, std::min({(int64_t)16, kFewBlocks / blocks, bytes / 1024}));
+  return ceil_div(bytes, ceil_div(ceil_div(bytes, s), 1024) * 1024);
+}
+size_t few_part_bytes(int64_t M, int N, int64_t K, int dtype) {
+  const int64_t s = few_splits(N, K, dtype);
+  return s > 1 ? (size_t)s * M * N * sizeof(float) : 0;
 }
 
 template <typename T, bool GATED>
-void launch_few(const Product<T>& p, hipStream_t st) {
-  const unsigned blocks = (unsigned)ceil_div(p.N, 16);
-  if (p.M <= 16) {
-    if (blocks >= 512) few_kernel<T, GATED, 1, 4><<<blocks, 256, 0, st>>>(p);
-    else if (blocks >= 192) few_kernel<T, GATED, 1, 8><<<blocks, 512, 0, st>>>(p);
-    else few_kernel<T, GATED, 1, 16><<<blocks, 1024, 0, st>>>(p);
-  } else if (p.M <= 32) {
-    if (blocks >= 512) few_kernel<T, GATED, 2, 4><<<blocks, 256, 0, st>>>(p);
-    else few_kernel<T, GATED, 2, 8><<<blocks, 512, 0, st>>>(p);
-  } else {
-    if (blocks >= 512) few_kernel<T, GATED, 4, 4><<<blocks, 256, 0, st>>>(p);
-    else few_kernel<T, GATED, 4, 8><<<blocks, 512, 0, st>>>(p);
+void launch_few(Product<T> p, int dtype, void* part, hipStream_t st) {
+  const int64_t splits = GATED ? 1 : few_splits(p.N, p.K, dtype), bytes = p.K * sizeof(T);
+  p.k_each = splits > 1 ? ceil_div(ceil_div(bytes, splits), 1024) * 1024 / sizeof(T) : p.K;
+  p.part = splits > 1 ? (float*)part : nullptr;
+  const dim3 blocks((unsigned)ceil_div(p.N, 16), (unsigned)splits);
+  if (p.M <= 16) few_kernel<T, GATED, 1, 4, 2><<<blocks, 256, 0, st>>>(p);
+  else if (p.M <= 32) few_kernel<T, GATED, 2, 4, 1><<<blocks, 256, 0, st>>>(p);
+  else few_kernel<T, GATED, 4, 4, 1><<<blocks, 256, 0, st>>>(p);
+  if (splits > 1) {
+    const int64_t n = p.M * p.N;
+    few_join_kernel<T><<<(unsigned)ceil_div(n, 256), 64, 0, st>>>(p.part, (int)splits, n, p.c);
   }
 }
 
@@ -604,9 +662,9 @@ void ffn_fwd(const void* x, const void* w_in, const void* w_out, int dtype, int6
   in.c2 = (T*)au;
   in.act = act;
   const Product<T> out = product<T>(h, F, w_out, F, N, C, F, y);
-  if (N <= kFewTokens) {
-    launch_few<T, true>(in, st);
-    launch_few<T, false>(out, st);
+  if (few_tokens(N, C, F, dtype)) {
+    launch_few<T, true>(in, dtype, nullptr, st);
+    launch_few<T, false>(out, dtype, ws, st);
   } else {
     launch_product<T, kGated, false, false>(in, dtype, ws, st);
     launch_product<T, kPlain, false, false>(out, dtype, ws, st);
@@ -615,7 +673,7 @@ void ffn_fwd(const void* x, const void* w_in, const void* w_out, int dtype, int6
 
 // Workspaces hold the splits of one product after the other, the backward's [da, du] before them.
 size_t ffn_fwd_ws(int64_t N, int C, int F, int dtype) {
-  return N <= kFewTokens ? 0 : std::max(cut_of(N, F, C, dtype, kGated).part_bytes(), cut_of(N, C, F, dtype, kPlain).part_bytes());
+  return few_tokens(N, C, F, dtype) ? few_part_bytes(N, C, F, dtype) : std::max(cut_of(N, F, C, dtype, kGated).part_bytes(), cut_of(N, C, F, dtype, kPlain).part_bytes());
 }
 size_t ffn_bwd_part(int64_t N, int F, int dtype) { return round_up((size_t)N * 2 * F * elem_size(dtype), 256); }
 size_t ffn_bwd_ws(int64_t N, int C, int F, int dtype) {
@@ -646,8 +704,8 @@ int check_ffn(int64_t N, int C, int F, int dtype, int act) {
   const int v = dtype == MOGA_F32 ? 4 : 8;
   if (C % v || F % v || C > kFfnMaxC || F > kFfnMaxF || N >= ((int64_t)1 << 31)) return MOGA_ERR_UNSUPPORTED;
   // blocks of the largest grids, and bytes of 256 rows within 31 bits
-  const int64_t most = std::max({ceil_div(N, 128) * ceil_div(F, 64), ceil_div(N, 128) * ceil_div(C, 128), ceil_div(2 * (int64_t)F, 128) * ceil_div(C, 128)});
-  return grid_fits(32 * most, 512) ? MOGA_OK : MOGA_ERR_UNSUPPORTED;
+  const int64_t most = std::max({ceil_div(N, 64) * ceil_div(F, 64), ceil_div(N, 64) * ceil_div(C, 128), ceil_div(2 * (int64_t)F, 64) * ceil_div(C, 128)});
+  return grid_fits(most + 32 * 768, 512) ? MOGA_OK : MOGA_ERR_UNSUPPORTED;
 }
 
 }  // namespace

@@ -51,7 +51,7 @@ template <typename T, bool KFIRST, int ROWS, int THREADS, int TILES>
 struct Operand {
   static constexpr int ES = sizeof(T), V = 16 / ES, BK = 128 / ES, L = ROWS * 8 / THREADS, CPR = ROWS * ES / 16;
   static constexpr unsigned kBytes = ROWS * 128;
-  static constexpr bool kKFirst = KFIRST;
+  static_assert(ROWS == 64 || ROWS == 128 || ROWS == 256);   // exchanges stay within a row
   uint64_t base;     // address of this block's rows at the k of the next step to be staged
   uint64_t base2;    // of the second half of the rows of each 64 (init_paired)
   int64_t step_bytes;
@@ -62,8 +62,9 @@ struct Operand {
   int k_left;                          // from the next step to be staged on
 
   __device__ __forceinline__ static int swizzle(int k) {   // columns: exchanged 16-byte chunks of row k
-    // the rows that a read's half wave touches: bf16 k 0 .. 3 and 8 .. 11 by 32 bytes, fp32 k 0, 4, 8, 12 by 64
-    return ES == 2 ? ((k & 3) | ((k >> 1) & 4)) * 2 : ((k >> 2) & 3) * 4;
+    // a read's half wave touches, bf16, k 0 .. 3 and 8 .. 11 by 32 bytes, of rows of 128 bytes two beside each other; fp32, k 0, 4, 8, 12 by 64
+    if (ES == 4) return ((k >> 2) & 3) * 4;
+    return ROWS == 64 ? (((k >> 1) & 1) | ((k >> 2) & 2)) * 2 : ((k & 3) | ((k >> 1) & 4)) * 2;
   }
   __device__ __forceinline__ static int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
