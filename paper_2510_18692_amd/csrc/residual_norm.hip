@@ -30,30 +30,67 @@ struct ResNorm {
 
 constexpr int kBlockWaves = 16;   // of a block that owns a token, at most
 
-// Eight columns of a row.
-template <typename T> struct Eight;
-template <> struct Eight<unsigned short> {
+// Eight columns of a row.  EVEN: rows are whole eights, and a lane has all of one or none; else the row's last piece is looked at column by column.
+template <typename T, bool EVEN> struct Eight;
+template <bool EVEN> struct Eight<unsigned short, EVEN> {
   Bytes16<unsigned short> b;
-  __device__ __forceinline__ void load(const unsigned short* row, int col, int C, bool last) { b = load_part(row, col, C, last); }
-  __device__ __forceinline__ void get(float (&f)[8]) const { unpack(b, f); }
+  __device__ __forceinline__ void load(const unsigned short* row, int col, int C, bool last) {
+    if constexpr (EVEN) b = col < C ? *(const Bytes16<unsigned short>*)(row + col) : Bytes16<unsigned short>{};
+    else b = load_part(row, col, C, last);
+  }
+  __device__ __forceinline__ void get(float (&f)[8], int col, int C) const {
+    unpack(b, f);
+    if constexpr (!EVEN) clear_past(f, col, C);
+  }
 };
-template <> struct Eight<float> {
+template <bool EVEN> struct Eight<float, EVEN> {
   Bytes16<float> b[2];
   __device__ __forceinline__ void load(const float* row, int col, int C, bool last) {
-    b[0] = load_part(row, col, C, last);
-    b[1] = load_part(row, col + 4, C, last);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if constexpr (EVEN) b[i] = col < C ? *(const Bytes16<float>*)(row + col + 4 * i) : Bytes16<float>{};
+      else b[i] = load_part(row, col + 4 * i, C, last);
+    }
   }
-  __device__ __forceinline__ void get(float (&f)[8]) const {
+  __device__ __forceinline__ void get(float (&f)[8], int col, int C) const {
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(b[i / 4].w[i % 4]);
+    if constexpr (!EVEN) clear_past(f, col, C);
   }
 };
-__device__ __forceinline__ void store8(unsigned short* row, int col, int C, const float (&f)[8]) { store_part(row, col, C, f); }
+template <bool EVEN>
+__device__ __forceinline__ void store8(unsigned short* row, int col, int C, const float (&f)[8]) {
+  if constexpr (!EVEN) store_part(row, col, C, f);
+  else if (col < C) *(Bytes16<unsigned short>*)(row + col) = pack(f);
+}
+template <bool EVEN>
 __device__ __forceinline__ void store8(float* row, int col, int C, const float (&f)[8]) {
   const float lo[4] = {f[0], f[1], f[2], f[3]}, hi[4] = {f[4], f[5], f[6], f[7]};
-  store_part(row, col, C, lo);
-  store_part(row, col + 4, C, hi);
+  if constexpr (!EVEN) {
+    store_part(row, col, C, lo);
+    store_part(row, col + 4, C, hi);
+  } else if (col < C) {
+    *(Bytes16<float>*)(row + col) = pack(lo);
+    *(Bytes16<float>*)(row + col + 4) = pack(hi);
+  }
 }
+
+// Eight floats of a lane's own between tokens, in LDS: the registers go to more waves.  99,840 x 5120 bf16, RMS norms before and after: 869 us with the
+// forward's three factors there, 947 in registers; the backward gains nothing.
+struct Parked {
+  floatx4_t* at;   // [2][threads], of this lane
+  int threads;
+  __device__ __forceinline__ Parked(floatx4_t* lds, int slot) : at(lds + (size_t)slot * 2 * blockDim.x + threadIdx.x), threads(blockDim.x) {}
+  __device__ __forceinline__ void put(const float (&v)[8]) const {
+    at[0] = floatx4_t{v[0], v[1], v[2], v[3]};
+    at[threads] = floatx4_t{v[4], v[5], v[6], v[7]};
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    const floatx4_t a = at[0], b = at[threads];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+  }
+};
 
 // How the tokens of a piece are dealt out: LANES = 16 or 64 to a token, four waves a block; LANES = 0: a token to a block.
 template <int LANES>
@@ -78,21 +115,17 @@ struct Piece {
   }
 };
 
-// G, W and the additive term of the lane's columns, for one row of gate, scale and shift.
-template <int PARTS>
-__device__ __forceinline__ void load_factors(const ResNorm& p, int64_t row, const int (&col)[PARTS], float (&G)[PARTS][8], float (&W)[PARTS][8]) {
+// G and W of eight columns, for one row of gate, scale and shift.
+__device__ __forceinline__ void load_factors(const ResNorm& p, int64_t row, int col, float (&G)[8], float (&W)[8]) {
+  float t[8];
+  load_weights(p.gate ? p.gate + row * p.C : nullptr, col, p.C, 1.f, G);
+  load_weights(p.post_weight, col, p.C, 1.f, t);
 #pragma unroll
-  for (int q = 0; q < PARTS; ++q) {
-    float t[8];
-    load_weights(p.gate ? p.gate + row * p.C : nullptr, col[q], p.C, 1.f, G[q]);
-    load_weights(p.post_weight, col[q], p.C, 1.f, t);
+  for (int i = 0; i < 8; ++i) G[i] *= p.alpha * t[i];
+  load_weights(p.weight, col, p.C, 1.f, W);
+  load_weights(p.scale ? p.scale + row * p.C : nullptr, col, p.C, 0.f, t);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) G[q][i] *= p.alpha * t[i];
-    load_weights(p.weight, col[q], p.C, 1.f, W[q]);
-    load_weights(p.scale ? p.scale + row * p.C : nullptr, col[q], p.C, 0.f, t);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) W[q][i] *= 1.f + t[i];
-  }
+  for (int i = 0; i < 8; ++i) W[i] *= 1.f + t[i];
 }
 
 // Mean (0 of an RMS norm) and 1 / deviation of a row; v is centred.  Columns past the row's end are 0 and stay 0.
@@ -124,7 +157,7 @@ __device__ __forceinline__ void row_stats(float (&v)[PARTS][8], int kind, int C,
 }
 
 // TX: x and r; TY: y and h.  PARTS pieces of eight columns a lane; lane t holds the columns (part * lanes + t) * 8 ..
-template <typename TX, typename TY, int LANES, int PARTS, int WAVES>
+template <typename TX, typename TY, int LANES, int PARTS, int WAVES, bool EVEN>
 __global__ __launch_bounds__(64 * WAVES, WAVES > 4 && PARTS == 1 ? 5 : 4) void residual_norm_fwd_kernel(const ResNorm p, TX* __restrict__ r_out, TY* __restrict__ h_out,
                                                                                         float* __restrict__ stats) {
   __shared__ float lds[2][WAVES][1];
@@ -137,13 +170,32 @@ __global__ __launch_bounds__(64 * WAVES, WAVES > 4 && PARTS == 1 ? 5 : 4) void r
   int col[PARTS];
 #pragma unroll
   for (int q = 0; q < PARTS; ++q) col[q] = (q * d.lanes + d.lane) * 8;
-  float G[PARTS][8], W[PARTS][8], S[PARTS][8];
+  // G, W and the additive term; of two pieces a lane they would take more LDS than there is
+  constexpr bool PARKED = PARTS == 1;
+  extern __shared__ floatx4_t s_kept[];
+  float kept[PARKED ? 1 : PARTS][3][8];
+  auto keep = [&](int q, int k, const float (&v)[8]) {
+    if constexpr (PARKED) {
+      Parked(s_kept, k).put(v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) kept[q][k][i] = v[i];
+    }
+  };
+  auto recall = [&](int q, int k, float (&v)[8]) {
+    if constexpr (PARKED) {
+      Parked(s_kept, k).get(v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = kept[q][k][i];
+    }
+  };
   int64_t held = -1;
   for (int64_t item = blockIdx.x; item < p.items; item += gridDim.x) {
     const Piece piece(p, item);
     int64_t row = piece.first + d.slot;
-    Eight<TX> nx[PARTS];
-    Eight<TY> ny[PARTS];
+    Eight<TX, EVEN> nx[PARTS];
+    Eight<TY, EVEN> ny[PARTS];
     auto fetch = [&](int64_t at) {
 #pragma unroll
       for (int q = 0; q < PARTS; ++q) nx[q].load(x + at * C, col[q], C, at + 1 == p.N);
@@ -154,28 +206,29 @@ __global__ __launch_bounds__(64 * WAVES, WAVES > 4 && PARTS == 1 ? 5 : 4) void r
     if (row < piece.end) fetch(row);
     if (held != piece.row) {
       held = piece.row;
-      load_factors(p, held, col, G, W);
 #pragma unroll
       for (int q = 0; q < PARTS; ++q) {
-        float t[8];
+        float G[8], W[8], S[8], t[8];
+        load_factors(p, held, col[q], G, W);
+        keep(q, 0, G);
+        keep(q, 1, W);
         load_weights(p.scale ? p.scale + held * C : nullptr, col[q], C, 0.f, t);
-        load_weights(p.bias, col[q], C, 0.f, S[q]);
+        load_weights(p.bias, col[q], C, 0.f, S);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) S[q][i] *= 1.f + t[i];
+        for (int i = 0; i < 8; ++i) S[i] *= 1.f + t[i];
         load_weights(p.shift ? p.shift + held * C : nullptr, col[q], C, 0.f, t);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) S[q][i] += t[i];
+        for (int i = 0; i < 8; ++i) S[i] += t[i];
+        keep(q, 2, S);
       }
     }
     for (; row < piece.end; row += Lanes<LANES>::kRows) {
       float f[PARTS][8], v[PARTS][8];
 #pragma unroll
       for (int q = 0; q < PARTS; ++q) {
-        nx[q].get(f[q]);
-        clear_past(f[q], col[q], C);
+        nx[q].get(f[q], col[q], C);
         if (y) {
-          ny[q].get(v[q]);
-          clear_past(v[q], col[q], C);
+          ny[q].get(v[q], col[q], C);
         }
       }
       if (row + Lanes<LANES>::kRows < piece.end) fetch(row + Lanes<LANES>::kRows);
@@ -190,9 +243,11 @@ __global__ __launch_bounds__(64 * WAVES, WAVES > 4 && PARTS == 1 ? 5 : 4) void r
         }
 #pragma unroll
         for (int q = 0; q < PARTS; ++q) {
+          float G[8];
+          recall(q, 0, G);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) f[q][i] = fmaf(v[q][i] * rstd, G[q][i], f[q][i]);
-          store8(r_out + row * C, col[q], C, f[q]);
+          for (int i = 0; i < 8; ++i) f[q][i] = fmaf(v[q][i] * rstd, G[i], f[q][i]);
+          store8<EVEN>(r_out + row * C, col[q], C, f[q]);
         }
       }
       if (p.pre != MOGA_NORM_NONE) {
@@ -203,9 +258,12 @@ __global__ __launch_bounds__(64 * WAVES, WAVES > 4 && PARTS == 1 ? 5 : 4) void r
         }
 #pragma unroll
         for (int q = 0; q < PARTS; ++q) {
+          float W[8], S[8];
+          recall(q, 1, W);
+          recall(q, 2, S);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) f[q][i] = fmaf(f[q][i] * rstd, W[q][i], S[q][i]);
-          store8(h_out + row * C, col[q], C, f[q]);
+          for (int i = 0; i < 8; ++i) f[q][i] = fmaf(f[q][i] * rstd, W[i], S[i]);
+          store8<EVEN>(h_out + row * C, col[q], C, f[q]);
         }
       }
     }
@@ -239,8 +297,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES > 4 ? 4 : 3) void residual_norm_b
   for (int64_t item = blockIdx.x; item < p.items; item += gridDim.x) {
     const Piece piece(p, item);
     int64_t row = piece.first + d.slot;
-    Eight<TX> nx[PARTS], nr[PARTS];
-    Eight<TY> ny[PARTS], nh[PARTS];
+    Eight<TX, false> nx[PARTS], nr[PARTS];
+    Eight<TY, false> ny[PARTS], nh[PARTS];
     float st[4];
     auto fetch = [&](int64_t at) {
       const bool last = at + 1 == p.N;
@@ -265,7 +323,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES > 4 ? 4 : 3) void residual_norm_b
     if (row < piece.end) fetch(row);
     if (held != piece.row) {
       held = piece.row;
-      load_factors(p, held, col, G, W);
+#pragma unroll
+      for (int q = 0; q < PARTS; ++q) load_factors(p, held, col[q], G[q], W[q]);
     }
     float a1[PARTS][8], a2[PARTS][8], bs[PARTS][8];
 #pragma unroll
@@ -277,18 +336,14 @@ __global__ __launch_bounds__(64 * WAVES, WAVES > 4 ? 4 : 3) void residual_norm_b
 #pragma unroll
       for (int q = 0; q < PARTS; ++q) {
         if (dh) {
-          nx[q].get(f[q]);
-          clear_past(f[q], col[q], C);
-          nh[q].get(g[q]);
-          clear_past(g[q], col[q], C);
+          nx[q].get(f[q], col[q], C);
+          nh[q].get(g[q], col[q], C);
         }
         if (y) {
-          ny[q].get(v[q]);
-          clear_past(v[q], col[q], C);
+          ny[q].get(v[q], col[q], C);
         }
         if (dr) {
-          nr[q].get(D[q]);
-          clear_past(D[q], col[q], C);
+          nr[q].get(D[q], col[q], C);
         } else {
 #pragma unroll
           for (int i = 0; i < 8; ++i) D[q][i] = 0.f;
@@ -326,7 +381,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES > 4 ? 4 : 3) void residual_norm_b
         }
       }
 #pragma unroll
-      for (int q = 0; q < PARTS; ++q) store8((TX*)o.d_x + row * C, col[q], C, D[q]);
+      for (int q = 0; q < PARTS; ++q) store8<false>((TX*)o.d_x + row * C, col[q], C, D[q]);
       if (y) {
         float s[2] = {0.f, 0.f};
 #pragma unroll
@@ -347,7 +402,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES > 4 ? 4 : 3) void residual_norm_b
             for (int i = 0; i < 8; ++i) D[q][i] = r_y * (D[q][i] - m0 - v[q][i] * m1);
         }
 #pragma unroll
-        for (int q = 0; q < PARTS; ++q) store8((TY*)o.d_y + row * C, col[q], C, D[q]);
+        for (int q = 0; q < PARTS; ++q) store8<false>((TY*)o.d_y + row * C, col[q], C, D[q]);
       }
     }
     if (!o.part) continue;
@@ -356,9 +411,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES > 4 ? 4 : 3) void residual_norm_b
 #pragma unroll
       for (int q = 0; q < PARTS; ++q)
         if (col[q] + 8 <= C) {
-          store8(out, col[q], C, a1[q]);
-          store8(out + C, col[q], C, a2[q]);
-          store8(out + 2 * C, col[q], C, bs[q]);
+          store8<true>(out, col[q], C, a1[q]);
+          store8<true>(out + C, col[q], C, a2[q]);
+          store8<true>(out + 2 * C, col[q], C, bs[q]);
         } else {
 #pragma unroll
           for (int i = 0; i < 8; ++i)
@@ -408,7 +463,8 @@ struct ResNormSums {
   float* over;   // [groups][3][C]: weighted sums of the rows of a group of blocks, where there are several groups
 };
 
-// Sums over the pieces of each row of the gate: 16 columns a block, whose 16 threads each take every 16th piece; rows in `gridDim.y` groups.
+// Sums over the pieces of each row of the gate: 16 columns a block, whose 16 threads each take every 16th piece; rows in `gridDim.y`
+// groups.  Bound by its chain of loads: of 32 columns and 8 threads, with whole lines, it takes a third longer.
 __global__ __launch_bounds__(256) void residual_norm_sums_kernel(const ResNorm p, const float* __restrict__ part, const ResNormSums o, int64_t rows) {
   __shared__ float acc[3][16][17];
   const int c = threadIdx.x & 15, k = threadIdx.x >> 4, C = p.C;
@@ -417,15 +473,16 @@ __global__ __launch_bounds__(256) void residual_norm_sums_kernel(const ResNorm p
   const float wp = p.post_weight && col < C ? p.post_weight[col] : 1.f;
   float all[3] = {0.f, 0.f, 0.f};
   for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
-    float s[3][8];
+    constexpr int U = 4;   // loads of each on their way
+    float s[3][U];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) s[0][u] = s[1][u] = s[2][u] = 0.f;
+    for (int u = 0; u < U; ++u) s[0][u] = s[1][u] = s[2][u] = 0.f;
     // pieces past the last token were not written
     const int64_t tokens = min(p.each, p.N - row * p.each), used = (tokens + p.len - 1) / p.len;
     if (col < C)
-      for (int64_t i = k; i < used; i += 16 * 8)
+      for (int64_t i = k; i < used; i += 16 * U)
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
+        for (int u = 0; u < U; ++u)
           if (i + 16 * u < used) {
             const float* at = part + (row * p.pieces + i + 16 * u) * 3 * C + col;
             s[0][u] += at[0];
@@ -433,7 +490,7 @@ __global__ __launch_bounds__(256) void residual_norm_sums_kernel(const ResNorm p
             s[2][u] += at[2 * C];
           }
 #pragma unroll
-    for (int h = 4; h > 0; h /= 2)
+    for (int h = U / 2; h > 0; h /= 2)
 #pragma unroll
       for (int u = 0; u < h; ++u)
 #pragma unroll
@@ -499,10 +556,12 @@ constexpr int kOverGroups = 64;   // groups of gate rows whose weighted sums are
 bool has_rows(const moga_residual_norm* a) { return a->gate || a->scale || a->shift; }
 
 // Pieces: as many as fill the chip, of no fewer than `least` tokens a lane group.
-void deal(ResNorm& p, int64_t rows, int blocks, int least) {
+void deal(ResNorm& p, int64_t rows, int blocks, int least, bool sums) {
   const Shape s = shape_of(p.C);
   const int64_t tokens = std::min(p.each, p.N), most = std::max<int64_t>(1, tokens / ((int64_t)s.rows * least));
-  p.pieces = std::min(most, rows == 1 ? blocks : std::max<int64_t>(1, (2 * blocks + rows - 1) / rows));
+  // one round of blocks for one row, and of the backward, whose pieces leave sums, where each row gets four or more; else rounds enough that the last
+  // one is short
+  p.pieces = std::min(most, rows == 1 || (sums && blocks / rows >= 4) ? blocks / rows : (4 * blocks + rows - 1) / rows);
   p.len = (tokens + p.pieces - 1) / p.pieces;
   p.pieces = (tokens + p.len - 1) / p.len;
   p.items = rows * p.pieces;
@@ -514,12 +573,12 @@ ResNorm make(const moga_residual_norm* a) {
   return {a->x, a->y, a->gate, a->post_weight, a->weight, a->bias, a->scale, a->shift, a->N, each, a->C, a->y ? a->post : MOGA_NORM_NONE, a->pre,
           a->residual_scale, a->eps, 1, 1, 1};
 }
-constexpr int kFwdWaves = 24, kBwdWaves = 8;   // of a CU
+constexpr int kFwdWaves = 24, kBwdWaves = 12;   // of a CU
 constexpr int kBwdLeast = 8;                    // tokens of a lane group and piece
 
 ResNorm make_bwd(const moga_residual_norm* a) {
   ResNorm p = make(a);
-  if (a->N > 0) deal(p, (a->N + p.each - 1) / p.each, blocks_of(shape_of(p.C), kBwdWaves), kBwdLeast);
+  if (a->N > 0) deal(p, (a->N + p.each - 1) / p.each, blocks_of(shape_of(p.C), kBwdWaves), kBwdLeast, true);
   return p;
 }
 
@@ -576,13 +635,17 @@ extern "C" int moga_residual_norm_fwd(const moga_residual_norm* a, void* r, void
   const Shape s = shape_of(a->C);
   ResNorm p = make(a);
   const int blocks = blocks_of(s, kFwdWaves);
-  deal(p, (p.N + p.each - 1) / p.each, blocks, 1);
+  deal(p, (p.N + p.each - 1) / p.each, blocks, p.N > blocks * s.rows ? 3 : 1, false);   // 4,099 x 1535 fp32, three rows of the gate: pieces of one token 38 us, of three 27
   const unsigned grid = (unsigned)std::min<int64_t>(p.items, 8 * blocks);
   with_types(a->x_dtype, a->y_dtype, [&](auto tx, auto ty) {
     using TX = decltype(tx);
     using TY = decltype(ty);
     with_shape(s, [&](auto lanes, auto parts, auto waves) {
-      residual_norm_fwd_kernel<TX, TY, lanes.value, parts.value, waves.value><<<grid, 64 * s.waves, 0, (hipStream_t)stream>>>(p, (TX*)r, (TY*)h, stats);
+      const unsigned lds = parts.value == 1 ? 64 * s.waves * 96 : 0;
+      if (p.C % 8 == 0)
+        residual_norm_fwd_kernel<TX, TY, lanes.value, parts.value, waves.value, true><<<grid, 64 * s.waves, lds, (hipStream_t)stream>>>(p, (TX*)r, (TY*)h, stats);
+      else
+        residual_norm_fwd_kernel<TX, TY, lanes.value, parts.value, waves.value, false><<<grid, 64 * s.waves, lds, (hipStream_t)stream>>>(p, (TX*)r, (TY*)h, stats);
     });
   });
   return launch_status();
@@ -592,7 +655,7 @@ extern "C" int moga_residual_norm_fwd(const moga_residual_norm* a, void* r, void
 extern "C" size_t moga_residual_norm_bwd_ws_bytes(int64_t N, int M, int C) {
   if (N <= 0 || M < 1 || M > N || C < 1 || C > kNormMaxC || N >= ((int64_t)1 << 31)) return 0;
   const Shape s = shape_of(C);
-  const int64_t items = M + std::min<int64_t>(2 * blocks_of(s, kBwdWaves), N / (s.rows * kBwdLeast));
+  const int64_t items = M + std::min<int64_t>(4 * blocks_of(s, kBwdWaves), N / (s.rows * kBwdLeast));
   return ((size_t)items + kOverGroups) * 3 * C * sizeof(float);
 }
 
