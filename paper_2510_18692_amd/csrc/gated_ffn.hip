@@ -82,8 +82,6 @@ struct Product {
   float* part;           // their sums, [split][left][BM][BN], or NULL for splits of all of k
 };
 
-__device__ __forceinline__ float value_of(float v) { return v; }
-__device__ __forceinline__ float value_of(unsigned short v) { return bf16_bits_to_f32(v); }
 __device__ __forceinline__ uintx2_t pack4(floatx4_t v) { return uintx2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}; }
 
 // The columns of a wave's sums in units of two neighbouring tiles: lane group g holds columns 4 g .. of either.  Lanes exchange fours, after which
@@ -379,6 +377,18 @@ __global__ __launch_bounds__(256) void join_kernel(const Product<T> p, int split
       *(uintx4_t*)to = uintx4_t{a[0], a[1], b[0], b[1]};
     }
   };
+  auto take = [&](const T* from, floatx4_t (&x)[2]) {
+    if constexpr (sizeof(T) == 4) {
+      x[0] = *(const floatx4_t*)from;
+      x[1] = col + 4 < N ? *(const floatx4_t*)(from + 4) : floatx4_t{0.f, 0.f, 0.f, 0.f};
+    } else {
+      const uintx4_t b = *(const uintx4_t*)from;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) x[t][2 * i] = bf16_lo_to_f32(b[2 * t + i]), x[t][2 * i + 1] = bf16_hi_to_f32(b[2 * t + i]);
+    }
+  };
   if constexpr (KIND == kPlain) {
     put(p.c + row * N + col, v[0][0], v[0][1]);
   } else {
@@ -399,16 +409,17 @@ __global__ __launch_bounds__(256) void join_kernel(const Product<T> p, int split
           put(p.c2 + row * 2 * N + N + col, v[1][0], v[1][1]);
         }
       } else {
-        const T *a = p.saved + row * 2 * N + col, *u = a + N;
-        floatx4_t da[2], du[2];
+        floatx4_t a[2], u[2], da[2], du[2];
+        const T* at = p.saved + row * 2 * N + col;
+        take(at, a);
+        take(at + N, u);
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            if (sizeof(T) == 4 && col + 4 * t >= N) break;
             float f, slope;
-            activate<T, act.value>(value_of(a[4 * t + i]), f, slope);
-            da[t][i] = v[0][t][i] * value_of(u[4 * t + i]) * slope;
+            activate<T, act.value>(a[t][i], f, slope);
+            da[t][i] = v[0][t][i] * u[t][i] * slope;
             du[t][i] = v[0][t][i] * f;
           }
         put(p.c + row * 2 * N + col, da[0], da[1]);
