@@ -137,5 +137,7 @@ def test_gated_ffn_workspace():
     wb = lambda op, N, C, F, dt: mg.workspace_bytes(op, N, 0, F, 1, C, dt)
     for op in (mg.OP_GATED_FFN_FWD, mg.OP_GATED_FFN_BWD):
         assert wb(op, 0, 64, 32, 1) == 0 and wb(op, 10, 60, 32, 1) == 0 and wb(op, 10, 64, 32, 5) == 0
-    assert wb(mg.OP_GATED_FFN_FWD, 1, 5120, 13696, 1) == 0
+    assert 0 < wb(mg.OP_GATED_FFN_FWD, 1, 5120, 13696, 1) <= 16 * 5120 * 4   # splits of one token's second product
+    assert wb(mg.OP_GATED_FFN_FWD, 32760, 1536, 4096, 1) == 0               # whole rounds of tiles
+    assert max(wb(mg.OP_GATED_FFN_FWD, n, 1536, 4096, 1) for n in range(1, 3000, 37)) <= 32 * 256 * 65536 * 4
     assert wb(mg.OP_GATED_FFN_BWD, 32760, 1536, 4096, 1) >= 32760 * 8192 * 2
