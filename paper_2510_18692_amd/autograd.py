@@ -9,7 +9,8 @@ gradient is returned for the router input x unless `grad_x=True` (the optional d
 backward).  Everything runs in the HIP library; the autograd function itself is native
 (csrc/torch_binding.cpp), so that the backward pass does not enter the interpreter.
 `layer_norm`, `residual_norm`, `gated_ffn`, `rotary` and `moga_diff_attention` have first derivatives only: gradients taken with
-create_graph=True raise an error where they are differentiated again.
+create_graph=True raise an error where they are differentiated again.  Before a step whose backward is captured into a graph, let go of the eager
+results of the same leaves (see moga_diff_attention).
 """
 from __future__ import annotations
 

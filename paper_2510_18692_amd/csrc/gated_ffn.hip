@@ -49,8 +49,8 @@ __device__ __forceinline__ void activate(float a, float& f, float& slope) {
     f = a * p;
     slope = fmaf(a * 0.39894228040143268f, e, p);
   } else {
-    constexpr float k = 1.5957691216057308f, c = 0.044715f;   // 2 sqrt(2 / pi)
-    const float a2 = a * a, p = inverse<T>(1.f + exp_neg<T>(k * a * fmaf(c, a2, 1.f)));
+    constexpr float k = 1.5957691216057308f, c = 0.044715f;   // 2 sqrt(2 / pi); beyond |a| = 100 p is 0 or 1, and a^2 may not be infinite
+    const float a2 = fminf(a * a, 1e4f), p = inverse<T>(1.f + exp_neg<T>(k * a * fmaf(c, a2, 1.f)));
     f = a * p;
     slope = fmaf(f * (1.f - p), k * fmaf(3.f * c, a2, 1.f), p);
   }
@@ -267,7 +267,7 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 2 ? 3 : 2) void product_kernel(
   for (int m = 0; m < TM; ++m) fa[m] = oa.get(m, 0);
   if constexpr (!A_KFIRST) oa.turn(0, other);
   if constexpr (!B_KFIRST) ob.turn(0, other);
-  for (int s = 0; s < k_count; s += BK) {
+  for (int left = (k_count - 1) / BK; left >= 0; --left) {
     half(std::integral_constant<int, 0>{});
     if constexpr (A_KFIRST) oa.turn(0, other);
     if constexpr (B_KFIRST) ob.turn(0, other);

@@ -681,7 +681,7 @@ struct ResidualNorm {
     if (type != at::kFloat && type != at::kBFloat16) raise(PyExc_TypeError, std::string("unsupported dtype ") + c10::toString(type));
     need_like(y, x, x.sizes(), type, "y");
     need(!tokens_per_row || *tokens_per_row >= 1, "tokens_per_row: at least 1");
-    if (tokens_per_row && N > 0) rows = (N + *tokens_per_row - 1) / *tokens_per_row;
+    if (tokens_per_row && N > 0) rows = (N - 1) / *tokens_per_row + 1;
     need_like(post_weight, x, {C}, at::kFloat, "post_weight");
     need_like(weight, x, {C}, at::kFloat, "weight");
     need_like(bias, x, {C}, at::kFloat, "bias");

@@ -72,8 +72,8 @@ def test_bad_tokens_do_not_touch_the_others(dtype, N):
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_large_arguments(act, dtype):
     """Arguments whose exponential overflows: act is a or 0, its derivative 1 or 0, nothing is NaN."""
-    x = torch.zeros((4, 8), device="cuda", dtype=dtype)
-    x[:, 0] = torch.tensor([1e4, -1e4, 3e18, -3e18], device="cuda")
+    x = torch.zeros((6, 8), device="cuda", dtype=dtype)
+    x[:, 0] = torch.tensor([1e4, -1e4, 3e18, -3e18, 1e2, -1e2], device="cuda")
     wi, wo = (torch.zeros(s, device="cuda", dtype=dtype) for s in ((16, 8), (8, 8)))
     wi[0, 0], wi[8, 0], wo[0, 0] = 1.0, 1.0, 1.0
     y, au, h = mg.moga_gated_ffn_fwd(x, wi, wo, act)
@@ -85,6 +85,27 @@ def test_large_arguments(act, dtype):
     d_x, d_wi, d_wo = mg.moga_gated_ffn_bwd(dy, x, wi, wo, au, h, act)
     assert d_x.isfinite().all()
     within(d_x[:, 0], torch.where(a > 0, 2 * a, 0), 8 * ref.HALF_STEP[dtype] * a.abs(), "d_x")
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_arguments_whose_square_overflows(act, dtype):
+    """a = +-1e30 beside u = 1e-30: h is 1 or 0, and so are the derivatives by either, times the other."""
+    x = torch.zeros((2, 8), device="cuda", dtype=dtype)
+    x[:, 0], x[:, 1] = torch.tensor([1e15, -1e15], device="cuda"), 1e-15
+    wi, wo = (torch.zeros(s, device="cuda", dtype=dtype) for s in ((16, 8), (8, 8)))
+    wi[0, 0], wi[8, 1], wo[0, 0] = 1e15, 1e-15, 1.0
+    y, au, h = mg.moga_gated_ffn_fwd(x, wi, wo, act)
+    dy = torch.zeros_like(x)
+    dy[:, 0] = 1
+    d_x, d_wi, d_wo = mg.moga_gated_ffn_bwd(dy, x, wi, wo, au, h, act)
+    e = 16 * ref.HALF_STEP[dtype]   # roundings of x, w, a, u, h and of the results
+    on = torch.tensor([1.0, 0.0], device="cuda", dtype=torch.float64)
+    within(h[:, 0], on, e * on, "h")
+    within(d_x[:, 0], on * 1e-15, e * 1e-15 * on, "d_x by a")      # u act'(a) w
+    within(d_x[:, 1], on * 1e15, e * 1e15 * on, "d_x by u")        # act(a) w
+    assert y.isfinite().all() and d_x.isfinite().all() and d_wo.isfinite().all()
+    assert not d_wi.isnan().any() and d_wi[8, 0].isinf()   # act(a) x is 1e30 * 1e15, past fp32's range
 
 
 def test_parts_of_the_backward():

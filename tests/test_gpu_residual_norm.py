@@ -129,6 +129,14 @@ def test_constant_and_zero_rows():
     assert (h == 0).all() and (stats[2] == 3).all()
 
 
+def test_tokens_per_row_past_all_tokens():
+    t, p = _inputs(50, 96, F32, BF, 8)
+    want = _run(t, p, "rms", "layer", 1.0, None)
+    for each in (50, 51, 2 ** 63 - 1):
+        got = _run(t, p, "rms", "layer", 1.0, each)
+        assert all(torch.equal(a, b) for a, b in zip((*got[:3], *got[3]), (*want[:3], *want[3])))
+
+
 def test_no_tokens():
     t, p = _inputs(0, 64, F32, BF, 1)
     r, h, _, d = _run(t, p, "rms", "layer", 1.0, 5)
