@@ -606,8 +606,9 @@ int moga_residual_norm_bwd(const moga_residual_norm* args, const float* stats, c
  * Gated feed-forward:  [a, u] = x W_in^T,  h = act(a) * u,  y = h W_out^T
  * x, y [N, C], w_in [2 F, C] (the F rows of a, then the F rows of u), w_out [C, F], h [N, F]; all of dtype F32 or BF16, C <= 65536 and F <= 262144
  * multiples of 8 (F32: of 4), N < 2^31.  act: silu a / (1 + e^-a), gelu a (1 + erf(a / sqrt 2)) / 2, or gelu's tanh form.
- * h is written in any case (the second product reads it); au [N, 2 F] = [a, u] for a backward, else NULL.  fp32 sums; h is taken from the unrounded a
- * and u, and a, u, h and y are rounded once.  Results repeat bit by bit.  Workspace: MOGA_OP_GATED_FFN_FWD.
+ * h is written in any case (the second product reads it); au for a backward, else NULL: [N, 2 F] = [a, u], and of BF16 behind it [N, F / 2] bytes, two
+ * more bits of each a and u (4.5 N F bytes in all, F32 8 N F).  fp32 sums; h is taken from the unrounded a and u, and a, u, h and y are rounded once.
+ * Results repeat bit by bit.  Workspace: MOGA_OP_GATED_FFN_FWD.
  */
 int moga_gated_ffn_fwd(const void* x, const void* w_in, const void* w_out, int dtype, int64_t N, int C, int F, int activation, void* h,
                        void* au_or_null, void* y, void* ws, size_t ws_bytes, void* stream);

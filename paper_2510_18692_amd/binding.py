@@ -487,7 +487,7 @@ def moga_residual_norm_bwd(d_r, d_h, x, stats, y=None, gate=None, post_weight=No
 
 def moga_gated_ffn_fwd(x, w_in, w_out, activation="silu", want_saved=True, stream=None):
     """[a, u] = x w_in^T, h = act(a) * u, y = h w_out^T.  x [N, C], w_in [2 F, C], w_out [C, F]; activation "silu", "gelu" or "gelu_tanh"
-    -> (y [N, C], [a, u] [N, 2 F] | None, h [N, F] | None)"""
+    -> (y [N, C], au | None, h [N, F] | None); au, for the backward, begins with [a, u] [N, 2 F]"""
     return _nat.gated_ffn_fwd(x, w_in, w_out, _one_of(ACTIVATIONS, activation, "activation"), want_saved, _st(stream))
 
 

@@ -74,13 +74,40 @@ struct Product {
   int N, act;            // kGated: N = F, b [2 F][ldb]
   int64_t K;
   T* c;                  // [M][N]; kGated: h; kGatedBwd: [da, du], [M][2 N]
-  T* c2;                 // kGated: [a, u], [M][2 N], or NULL
-  const T* saved;        // kGatedBwd: [a, u]
+  T* c2;                 // kGated: [a, u], [M][2 N], and finer() behind it, or NULL
+  const T* saved;        // kGatedBwd: the same
   // blocks below `whole` have a tile each, the `left` tiles behind them are split along k: block whole + split * left + tile
   unsigned tiles_m, tiles_n, whole, left;
   int64_t k_each;        // k of a split
   float* part;           // their sums, [split][left][BM][BN], or NULL for splits of all of k
 };
+
+// a and u go to the backward in bf16 with two more bits each, half a byte a pair: the rounded value's distance from the value, in quarters of a step of
+// bf16 from -1/4 on.  What the backward makes of them is rounded itself (da, du); from a and u in bf16 alone the gradients of x and W_in are off by
+// 1.76 times what a single rounding of the result is (2-norm, 32,760 x 1536 x 4096), with these bits by 1.45.  A zero stays one.
+template <typename T>
+__device__ __forceinline__ auto finer(T* c2, int64_t M, int64_t N) {
+  return (std::conditional_t<std::is_const_v<T>, const unsigned char, unsigned char>*)(c2 + M * 2 * N);
+}
+__device__ __forceinline__ unsigned finer_bits(float v, unsigned rounded) {   // rounded: v in bf16, as the upper half
+  const int d = (int)(__float_as_uint(v) - rounded);
+  return (unsigned)max(0, min(3, (d + 0x6000) >> 14));
+}
+__device__ __forceinline__ float finer_value(unsigned rounded, unsigned bits) {
+  const unsigned v = rounded + (bits << 14) - 0x4000u;
+  return __uint_as_float((rounded & 0x7f800000u) == 0x7f800000u ? rounded : v);
+}
+// Neighbouring columns of a and u, rounded: the bits of all of them, a column's u above its a.
+template <int COLS>
+__device__ __forceinline__ unsigned finer_pack(const float (&a)[COLS], const float (&u)[COLS], const unsigned (&ra)[COLS / 2], const unsigned (&ru)[COLS / 2]) {
+  unsigned all = 0;
+#pragma unroll
+  for (int i = 0; i < COLS; ++i) {
+    const unsigned x = i & 1 ? ra[i / 2] & 0xffff0000u : ra[i / 2] << 16, y = i & 1 ? ru[i / 2] & 0xffff0000u : ru[i / 2] << 16;
+    all |= (finer_bits(a[i], x) | finer_bits(u[i], y) << 2) << (4 * i);
+  }
+  return all;
+}
 
 __device__ __forceinline__ uintx2_t pack4(floatx4_t v) { return uintx2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}; }
 
@@ -124,12 +151,15 @@ __device__ __forceinline__ void put_unit(float* row, int col, int g, int64_t N, 
 template <typename T> struct Saved;
 template <> struct Saved<unsigned short> {
   uintx4_t a, u;
-  __device__ __forceinline__ void load(const unsigned short* row, int64_t F, int col, int g, bool ok) {
+  unsigned bits;
+  __device__ __forceinline__ void load(const unsigned short* row, const unsigned char* fine, int64_t F, int col, int g, bool ok) {
     col += unit_column(g);
     a = u = uintx4_t{0, 0, 0, 0};
+    bits = 0;
     if (ok && col < F) {
       a = *(const uintx4_t*)(row + col);
       u = *(const uintx4_t*)(row + F + col);
+      bits = *(const unsigned*)(fine + col / 2);
     }
   }
   template <int ACT>
@@ -139,11 +169,18 @@ template <> struct Saved<unsigned short> {
     uintx4_t da4, du4;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      float f0, s0, f1, s1;
-      activate<unsigned short, ACT>(bf16_lo_to_f32(a[i]), f0, s0);
-      activate<unsigned short, ACT>(bf16_hi_to_f32(a[i]), f1, s1);
-      da4[i] = pack_bf16x2(dh[2 * i] * bf16_lo_to_f32(u[i]) * s0, dh[2 * i + 1] * bf16_hi_to_f32(u[i]) * s1);
-      du4[i] = pack_bf16x2(dh[2 * i] * f0, dh[2 * i + 1] * f1);
+      float da[2], du[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const unsigned at = 8 * i + 4 * k;
+        const float av = finer_value(k ? a[i] & 0xffff0000u : a[i] << 16, bits >> at & 3), uv = finer_value(k ? u[i] & 0xffff0000u : u[i] << 16, bits >> (at + 2) & 3);
+        float f, slope;
+        activate<unsigned short, ACT>(av, f, slope);
+        da[k] = dh[2 * i + k] * uv * slope;
+        du[k] = dh[2 * i + k] * f;
+      }
+      da4[i] = pack_bf16x2(da[0], da[1]);
+      du4[i] = pack_bf16x2(du[0], du[1]);
     }
     col += unit_column(g);
     if (ok && col < F) {
@@ -154,7 +191,7 @@ template <> struct Saved<unsigned short> {
 };
 template <> struct Saved<float> {
   floatx4_t a[2], u[2];
-  __device__ __forceinline__ void load(const float* row, int64_t F, int col, int g, bool ok) {
+  __device__ __forceinline__ void load(const float* row, const unsigned char*, int64_t F, int col, int g, bool ok) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const int at = col + 16 * t + 4 * g;
@@ -186,6 +223,62 @@ template <> struct Saved<float> {
     }
   }
 };
+
+// Eight columns of a row: h, and a and u for the backward.
+template <int ACT>
+__device__ __forceinline__ void put_gated_eight(const Product<unsigned short>& p, int64_t row, int col, const float (&a)[8], const float (&u)[8]) {
+  const int64_t N = p.N;
+  uintx4_t h;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float f0, f1, slope;
+    activate<unsigned short, ACT>(a[2 * i], f0, slope);
+    activate<unsigned short, ACT>(a[2 * i + 1], f1, slope);
+    h[i] = pack_bf16x2(f0 * u[2 * i], f1 * u[2 * i + 1]);
+  }
+  *(uintx4_t*)(p.c + row * N + col) = h;
+  if (p.c2) {
+    unsigned ra[4], ru[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      ra[i] = pack_bf16x2(a[2 * i], a[2 * i + 1]);
+      ru[i] = pack_bf16x2(u[2 * i], u[2 * i + 1]);
+    }
+    *(uintx4_t*)(p.c2 + row * 2 * N + col) = uintx4_t{ra[0], ra[1], ra[2], ra[3]};
+    *(uintx4_t*)(p.c2 + row * 2 * N + N + col) = uintx4_t{ru[0], ru[1], ru[2], ru[3]};
+    *(unsigned*)(finer(p.c2, p.M, N) + row * N / 2 + col / 2) = finer_pack<8>(a, u, ra, ru);
+  }
+}
+
+// A row's h, and its a and u for the backward, of 32 columns from col on: a's sums in a0 and a1, u's in u0 and u1.
+template <int ACT>
+__device__ __forceinline__ void put_gated(const Product<unsigned short>& p, int64_t row, int col, int g, bool ok, floatx4_t a0, floatx4_t a1, floatx4_t u0,
+                                          floatx4_t u1) {
+  float a[8], u[8];
+  unit_eight(a0, a1, a);
+  unit_eight(u0, u1, u);
+  col += unit_column(g);
+  if (ok && col < p.N) put_gated_eight<ACT>(p, row, col, a, u);
+}
+template <int ACT>
+__device__ __forceinline__ void put_gated(const Product<float>& p, int64_t row, int col, int g, bool ok, floatx4_t a0, floatx4_t a1, floatx4_t u0,
+                                          floatx4_t u1) {
+  const int64_t N = p.N;
+  floatx4_t h[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float f, slope;
+      activate<float, ACT>(t ? a1[i] : a0[i], f, slope);
+      h[t][i] = f * (t ? u1[i] : u0[i]);
+    }
+  put_unit(p.c + row * N, col, g, N, ok, h[0], h[1]);
+  if (p.c2) {
+    put_unit(p.c2 + row * 2 * N, col, g, N, ok, a0, a1);
+    put_unit(p.c2 + row * 2 * N + N, col, g, N, ok, u0, u1);
+  }
+}
 
 // WM x WN waves, TM x TN tiles of 16 x 16 each
 template <typename T, Kind KIND, bool A_KFIRST, bool B_KFIRST, int WM, int WN, int TM, int TN>
@@ -300,7 +393,7 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 2 ? 3 : 2) void product_kernel(
   auto fetch_saved = [&](int m) {
     const int64_t row = m0 + (wm * TM + m) * 16 + r;
 #pragma unroll
-    for (int u = 0; u < FETCHED; ++u) saved[m % AHEAD][u].load(p.saved + row * 2 * N, N, col0 + 32 * u, g, row < p.M);
+    for (int u = 0; u < FETCHED; ++u) saved[m % AHEAD][u].load(p.saved + row * 2 * N, finer(p.saved, p.M, N) + row * N / 2, N, col0 + 32 * u, g, row < p.M);
   };
   auto rows = [&](auto act) {
     constexpr int ACT = act.value;
@@ -315,20 +408,7 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 2 ? 3 : 2) void product_kernel(
       } else if constexpr (KIND == kGated) {
         static_assert(UNITS == 2);   // of 64 columns the first unit is a's, the second u's
         const int col = n0 + wn * TN * 8;
-        floatx4_t h[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float f, slope;
-            activate<T, ACT>(acc[m][t][i], f, slope);
-            h[t][i] = f * acc[m][t + 2][i];
-          }
-        put_unit(p.c + row * N, col, g, N, ok, h[0], h[1]);
-        if (p.c2) {
-          put_unit(p.c2 + row * 2 * N, col, g, N, ok, acc[m][0], acc[m][1]);
-          put_unit(p.c2 + row * 2 * N + N, col, g, N, ok, acc[m][2], acc[m][3]);
-        }
+        put_gated<ACT>(p, row, col, g, ok, acc[m][0], acc[m][1], acc[m][2], acc[m][3]);
       } else {
 #pragma unroll
         for (int u = 0; u < UNITS; ++u)
@@ -393,7 +473,12 @@ __global__ __launch_bounds__(256) void join_kernel(const Product<T> p, int split
     put(p.c + row * N + col, v[0][0], v[0][1]);
   } else {
     with_activation(p.act, [&](auto act) {
-      if constexpr (KIND == kGated) {
+      if constexpr (KIND == kGated && sizeof(T) == 2) {
+        float a[8], u[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a[i] = v[0][i / 4][i % 4], u[i] = v[1][i / 4][i % 4];
+        put_gated_eight<act.value>(p, row, col, a, u);
+      } else if constexpr (KIND == kGated) {
         floatx4_t h[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -413,6 +498,14 @@ __global__ __launch_bounds__(256) void join_kernel(const Product<T> p, int split
         const T* at = p.saved + row * 2 * N + col;
         take(at, a);
         take(at + N, u);
+        if constexpr (sizeof(T) == 2) {
+          const unsigned bits = *(const unsigned*)(finer(p.saved, p.M, N) + row * N / 2 + col / 2);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            a[i / 4][i % 4] = finer_value(__float_as_uint(a[i / 4][i % 4]), bits >> 4 * i & 3);
+            u[i / 4][i % 4] = finer_value(__float_as_uint(u[i / 4][i % 4]), bits >> (4 * i + 2) & 3);
+          }
+        }
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -532,6 +625,12 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(const Product<T> p) {
       if (p.c2) {
         put(p.c2 + row * 2 * N + col, v[0]);
         put(p.c2 + row * 2 * N + N + col, v[1]);
+        if constexpr (ES == 2) {
+          const uintx2_t x = pack4(v[0]), y = pack4(v[1]);
+          const float a[4] = {v[0][0], v[0][1], v[0][2], v[0][3]}, u[4] = {v[1][0], v[1][1], v[1][2], v[1][3]};
+          const unsigned ra[2] = {x[0], x[1]}, ru[2] = {y[0], y[1]};
+          *(unsigned short*)(finer(p.c2, p.M, N) + row * N / 2 + col / 2) = (unsigned short)finer_pack<4>(a, u, ra, ru);
+        }
       }
     } else {
       put(p.c + row * N + col, v[0]);

@@ -753,9 +753,10 @@ struct FfnSizes {
     need_like(w_in, x, {2 * F, C}, x.scalar_type(), "w_in");
     need_like(w_out, x, {C, F}, x.scalar_type(), "w_out");
   }
+  int64_t saved(const Tensor& x) const { return x.scalar_type() == at::kBFloat16 ? N * F * 9 / 4 : N * F * 2; }
 };
 
-// y, [a, u], h; the latter two are returned for a backward only
+// y, [a, u] as the C call lays it out, h; the latter two are returned for a backward only
 std::tuple<Tensor, OptTensor, OptTensor> gated_ffn_fwd(const Tensor& x, const Tensor& w_in, const Tensor& w_out, int64_t act, bool want_saved,
                                                        const OptStream& stream) {
   require(x, w_in, w_out);
@@ -764,7 +765,7 @@ std::tuple<Tensor, OptTensor, OptTensor> gated_ffn_fwd(const Tensor& x, const Te
   const FfnSizes s(x, w_in, w_out);
   Tensor y = call.make(x.sizes(), x), h = call.make({s.N, s.F}, x);
   OptTensor au, ws;
-  if (want_saved) au = call.make({s.N, 2 * s.F}, x);
+  if (want_saved) au = call.make({s.saved(x)}, x);
   const size_t bytes = moga_workspace_bytes(MOGA_OP_GATED_FFN_FWD, s.N, 0, to_int(s.F), 1, to_int(s.C), dt(x));
   if (bytes) ws = call.workspace(bytes, x);
   check("moga_gated_ffn_fwd", moga_gated_ffn_fwd(ptr(x), ptr(w_in), ptr(w_out), dt(x), s.N, to_int(s.C), to_int(s.F), to_int(act), ptr(h), ptr(au),
@@ -780,7 +781,7 @@ std::tuple<OptTensor, OptTensor, OptTensor> gated_ffn_bwd(const Tensor& d_y, con
   const Call call(stream);
   const FfnSizes s(x, w_in, w_out);
   need_like(d_y, x, x.sizes(), x.scalar_type(), "d_y");
-  need_like(au, x, {s.N, 2 * s.F}, x.scalar_type(), "au");
+  need_like(au, x, {s.saved(x)}, x.scalar_type(), "au");
   need_like(h, x, {s.N, s.F}, x.scalar_type(), "h");
   OptTensor d_x, d_w_in, d_w_out, ws;
   if (want_dx) d_x = call.make(x.sizes(), x);

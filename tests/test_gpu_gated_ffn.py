@@ -23,7 +23,7 @@ def _check(N, C, F, dtype, act, seed=0):
     y, au, h = mg.moga_gated_ffn_fwd(x, wi, wo, act)
     d_x, d_wi, d_wo = mg.moga_gated_ffn_bwd(dy, x, wi, wo, au, h, act)
     want = ref.gated_ffn(x, wi, wo, act, dy)
-    got = dict(y=y, au=au, h=h, d_x=d_x, d_w_in=d_wi, d_w_out=d_wo)
+    got = dict(y=y, au=au[:2 * N * F].view(N, 2 * F), h=h, d_x=d_x, d_w_in=d_wi, d_w_out=d_wo)
     for k, v in got.items():
         within(v, *want[k], k)
     alone, none, _ = mg.moga_gated_ffn_fwd(x, wi, wo, act, want_saved=False)
@@ -50,7 +50,30 @@ def test_long_sums_and_repeated_bits(dtype, N, C, F):
     for _ in range(3):
         y, au, h = mg.moga_gated_ffn_fwd(x, wi, wo)
         d = mg.moga_gated_ffn_bwd(dy, x, wi, wo, au, h)
-        assert all(torch.equal(a, b) for a, b in zip((y, au, h, *d), got.values()))
+        assert all(torch.equal(a, b) for a, b in zip((y, au[:2 * N * F].view(N, 2 * F), h, *d), got.values()))
+
+
+@pytest.mark.parametrize("N", [1, 30, 130, 500, 3000])
+def test_two_more_bits_of_a_and_u(N):
+    """Behind the rounded a and u: their distance from the values in quarters of a step of bf16 (2^-7 of the power of two below), from -1/4 to 1/2.  What is
+    put together is off by at most a quarter of a step, and by an eighth where the rounding went down by no more than three eighths."""
+    C, F = 72, 136
+    x, wi, wo, _ = _inputs(N, C, F, BF, 4)
+    x[N // 2] = 0
+    _, au, _ = mg.moga_gated_ffn_fwd(x, wi, wo)
+    want, e = ref.gated_ffn(x, wi, wo, "silu")["au"]
+    e = e - ref.HALF_STEP[BF] * want.abs()   # of the fp32 sums alone
+    rounded = au[:2 * N * F].view(N, 2, F)
+    b = au[2 * N * F:].view(torch.uint8).view(N, F // 2)
+    pairs = torch.stack([b & 15, b >> 4], -1).view(N, F)
+    bits = torch.stack([pairs & 3, pairs >> 2], 1).double()
+    step = torch.exp2(torch.floor(torch.log2(rounded.double().abs().clamp(min=1e-30))) - 7)
+    got = rounded.double() + torch.sign(rounded.double()) * step * (bits - 1) / 4
+    off = (got - want.view(N, 2, F)).abs()
+    assert (off <= step / 4 * 1.0001 + e.view(N, 2, F)).all()
+    # uniform in [-1/2, 1/2] of a step: an eighth of them lie below -3/8, and are off by an eighth to a quarter
+    assert (off <= step / 8 * 1.0001 + e.view(N, 2, F)).double().mean() > 0.8
+    assert (rounded[N // 2] == 0).all() and (bits[N // 2] == 1).all()
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
@@ -181,6 +204,6 @@ def test_refuses():
     with pytest.raises(mg.MogaError):
         mg.moga_gated_ffn_fwd(*_inputs(4, 8, 12, BF, 1)[:3])
     with pytest.raises(ValueError):
-        mg.moga_gated_ffn_bwd(dy, x, wi, wo, au[:4].contiguous(), h)
+        mg.moga_gated_ffn_bwd(dy, x, wi, wo, au[:-8].contiguous(), h)
     with pytest.raises(TypeError):
         mg.moga_gated_ffn_bwd(dy.float(), x, wi, wo, au, h)
