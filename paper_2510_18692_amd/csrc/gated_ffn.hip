@@ -388,7 +388,7 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 2 ? 3 : 2) void product_kernel(
     return;
   }
   // the saved rows of AHEAD rows of tiles are on their way
-  constexpr int AHEAD = KIND == kGatedBwd ? 3 : 1, FETCHED = KIND == kGatedBwd ? UNITS : 1;
+  constexpr int AHEAD = KIND == kGatedBwd ? 2 : 1, FETCHED = KIND == kGatedBwd ? UNITS : 1;
   Saved<T> saved[AHEAD][FETCHED];
   auto fetch_saved = [&](int m) {
     const int64_t row = m0 + (wm * TM + m) * 16 + r;
