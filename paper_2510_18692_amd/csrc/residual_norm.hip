@@ -564,7 +564,7 @@ void deal(ResNorm& p, int64_t rows, int blocks, int least, bool sums) {
   p.pieces = std::min(most, rows == 1 || (sums && blocks / rows >= 4) ? blocks / rows : (4 * blocks + rows - 1) / rows);
   p.len = (tokens + p.pieces - 1) / p.pieces;
   p.pieces = (tokens + p.len - 1) / p.len;
-  p.items = rows * p.pieces;
+  p.items = (rows - 1) * p.pieces + (p.N - (rows - 1) * p.each + p.len - 1) / p.len;   // none past the last token
 }
 int blocks_of(const Shape& s, int waves) { return 256 * std::max(1, waves / s.waves); }
 
@@ -651,7 +651,7 @@ extern "C" int moga_residual_norm_fwd(const moga_residual_norm* a, void* r, void
   return launch_status();
 }
 
-// M: rows of gate, scale and shift.  deal() makes no more pieces than this.
+// M: rows of gate, scale and shift.  deal() makes no more pieces than this: all but the last of each row are of kBwdLeast tokens a lane group or more.
 extern "C" size_t moga_residual_norm_bwd_ws_bytes(int64_t N, int M, int C) {
   if (N <= 0 || M < 1 || M > N || C < 1 || C > kNormMaxC || N >= ((int64_t)1 << 31)) return 0;
   const Shape s = shape_of(C);

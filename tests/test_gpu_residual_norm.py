@@ -1,4 +1,6 @@
 """The residual norm, forward and backward, against 64 bits; bounds in block_parts_ref."""
+import ctypes
+
 import pytest
 import torch
 
@@ -7,6 +9,7 @@ from paper_2510_18692_amd.autograd import residual_norm
 
 from . import block_parts_ref as ref
 from .block_ref import within
+from .test_block_parts import Args
 
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
@@ -135,6 +138,22 @@ def test_tokens_per_row_past_all_tokens():
     for each in (50, 51, 2 ** 63 - 1):
         got = _run(t, p, "rms", "layer", 1.0, each)
         assert all(torch.equal(a, b) for a, b in zip((*got[:3], *got[3]), (*want[:3], *want[3])))
+
+
+@pytest.mark.parametrize("N,C,each", [(1001, 5120, 1000), (1001, 520, 500), (4097, 96, 4096), (2049, 300, 1024)])
+def test_short_last_row_of_the_gate_stays_in_its_workspace(N, C, each):
+    t, p = _inputs(N, C, BF, BF, 11, each=each)
+    _check(t, p, "rms", "rms", 1.0, each)
+    _, _, stats, want = _run(t, p, "rms", "rms", 1.0, each)
+    a = Args(**{k: v.data_ptr() for k, v in dict(x=t["x"], y=t["y"], **p).items()}, N=N, tokens_per_row=each, C=C, x_dtype=1, y_dtype=1, post=1, pre=1,
+             residual_scale=1.0, eps=1e-5)
+    need, guard = mg.workspace_bytes(mg.OP_RESIDUAL_NORM_BWD, N, 0, 0, -(-N // each), C, 1), 4 << 20
+    ws = torch.full((need + guard,), 0x5a, dtype=torch.uint8, device="cuda")
+    out = [torch.empty_like(v) for v in want]
+    ptrs = [v.data_ptr() for v in (stats, t["d_r"], t["d_h"], *out, ws)]
+    assert mg.load().moga_residual_norm_bwd(ctypes.byref(a), *map(ctypes.c_void_p, ptrs), ctypes.c_size_t(need), None) == 0
+    torch.cuda.synchronize()
+    assert (ws[need:] == 0x5a).all() and all(torch.equal(x, y) for x, y in zip(out, want))
 
 
 def test_no_tokens():
