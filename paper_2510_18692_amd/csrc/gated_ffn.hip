@@ -2,6 +2,10 @@
 //
 //   [a, u] = x W_in^T,  h = act(a) u,  y = h W_out^T
 //   dh = d_y W_out,  da = dh u act'(a),  du = dh act(a),  d_x = [da, du] W_in,  d_W_in = [da, du]^T x,  d_W_out = d_y^T h
+//
+// Six matrix products, 6 N C F operations forward and 12 N C F backward, the activation and its derivative in the epilogues of the two that make h and dh:
+// [a, u] leaves a block's registers once, dh never.  From some hundred tokens on bound by the products (product_kernel), with few tokens by the
+// weights' bytes (few_kernel).  h comes from the unrounded a and u, da and du from a and u as the forward kept them (finer()) and the unrounded dh.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -280,7 +284,25 @@ __device__ __forceinline__ void put_gated(const Product<float>& p, int64_t row, 
   }
 }
 
-// WM x WN waves, TM x TN tiles of 16 x 16 each
+// One tile of a product: WM x WN waves, TM x TN tiles of 16 x 16 each.
+//
+// Blocks of 256 x 256 (a CU each) read 2 bytes of operands from the caches for 256 operations, twice the reuse of 128 x 128 (two to a CU).  A step's two halves
+// of k alternate: the operands of a half are read from LDS while the products of the other run, and the loads of the step after next go out one with
+// each row of tiles; a step has one barrier.  A row of tiles goes out in whole 16 bytes a lane (permlane exchange), without a trip through LDS.
+//
+// bf16, 32,760 tokens, us and TFLOP/s by kernel (the forward without a backward; a library's square product of 16,384 reaches 1,530 on the same card):
+//                                      C 1536, F 4096     C 5120, F 13696
+//   in  (kGated, rows x rows)          772   1,070        7,212   1,270
+//   out (kPlain, rows x rows)          342   1,210        3,318   1,380
+//   dh  (kGatedBwd, rows x columns)    560     740        4,059   1,130
+//   dx  (kPlain, rows x columns)       618   1,330        6,546   1,400
+//   dW_in, dW_out (columns x columns)  637 + 37 and 340 + 23 to join   6,577 + 21 and 3,392 + 11
+// The long products are bound by power: the matrix cores are busy 0.71 to 0.75 of the cycles at 1.75 to 1.85 GHz of 2.4.  Fed from no loads at all the loop
+// makes 1,650 to 1,730, from loads of the same lines over and over 1,430 to 1,500: the rest is what bringing 64 KB a step from the caches costs in time
+// and in clock.  LDS has no bank conflicts and is busy 0.28 of the cycles.  With C = 1536 a tile's 24 steps (35 us) are followed by its epilogue,
+// beside which its CU has no products: dh takes 358 us without its 544 KB a block of a, u, da and du, 434 with the loads alone, 466 with the stores alone.
+// Starting half of the CUs half a tile later puts that traffic beside the others' products and gains nothing.
+// Fp32, 8,192 x 4096 x 4096, blocks of 128: 143 TFLOP/s of rows x rows, 129 to 132 with columns (4-byte reads), of a library's 153.
 template <typename T, Kind KIND, bool A_KFIRST, bool B_KFIRST, int WM, int WN, int TM, int TN>
 __global__ __launch_bounds__(64 * WM * WN, TM == 2 ? 3 : 2) void product_kernel(const Product<T> p) {
   constexpr int THREADS = 64 * WM * WN, BM = 16 * WM * TM, BN = 16 * WN * TN;
@@ -387,7 +409,8 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 2 ? 3 : 2) void product_kernel(
       for (int n = 0; n < TN; ++n) *(floatx4_t*)(out + ((wm * TM + m) * 16 + r) * BN + 16 * n + 4 * g) = acc[m][n];
     return;
   }
-  // the saved rows of AHEAD rows of tiles are on their way
+  // the saved rows of AHEAD rows of tiles are on their way: of one 550 us (32,760 x 1536 x 4096), of two 541, of three, which do
+  // not fit the registers, 622
   constexpr int AHEAD = KIND == kGatedBwd ? 2 : 1, FETCHED = KIND == kGatedBwd ? UNITS : 1;
   Saved<T> saved[AHEAD][FETCHED];
   auto fetch_saved = [&](int m) {
@@ -424,8 +447,9 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 2 ? 3 : 2) void product_kernel(
   else with_activation(p.act, rows);
 }
 
-// Tiles that were split along k: the sums of their splits, in order, and what a block does with its sums.  A thread has eight columns of a row (kGated:
-// of a, and the same eight of u); blockIdx.x is the tile, blockIdx.y a run of its rows.
+// Tiles that were split along k: the sums of their splits, in order (results repeat bit by bit), and what a block does with its sums.  A thread has eight
+// columns of a row (kGated: of a, and the same eight of u); blockIdx.x is the tile, blockIdx.y a run of its rows.  Bound by the partial sums' bytes, which
+// come from the cache behind the L2s where they fit: 192 tiles of 256 x 256 in four splits (201 MB) 37 us, 5.4 TB/s.
 template <typename T, Kind KIND, int BM, int BN>
 __global__ __launch_bounds__(256) void join_kernel(const Product<T> p, int splits) {
   constexpr int COLS = KIND == kGated ? BN / 2 : BN, SETS = KIND == kGated ? 2 : 1, PER = COLS / 8;
@@ -524,7 +548,10 @@ __global__ __launch_bounds__(256) void join_kernel(const Product<T> p, int split
 
 // ---- few tokens ----
 // A block owns 16 columns of C (GATED: 16 of a and the same 16 of u) for up to 16 TT tokens.  Its waves take turns of 128 bytes of k, so that a weight
-// is read once, a line at a time, and their sums meet in LDS.  Loads past k, F or the last token give zeros (buffer bounds).
+// is read once, a line at a time, and their sums meet in LDS.  Loads past k, F or the last token give zeros (buffer bounds).  The products of 16 tokens cost
+// a matrix instruction what one token's cost it, so there is no form for a single one.
+// Bound by HBM: 1 token, C 5120, F 13696, bf16: 53 us for W_in's 281 MB, 25 for W_out's 140 and 5 for the join (5.3 and 5.6 TB/s of weights, some of them
+// from the cache behind the L2s where passes follow each other).  24 tokens, 1536 x 4096: 8.2, 5.8 and 2.2 us, launches and their chain of loads.
 template <typename T, bool GATED, int TT, int WAVES, int U>
 __global__ __launch_bounds__(64 * WAVES) void few_kernel(const Product<T> p) {
   constexpr int ES = sizeof(T), SETS = GATED ? 2 : 1;
@@ -638,7 +665,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(const Product<T> p) {
   }
 }
 
-// Sums of the splits of few tokens' rows, in order, rounded once.
+// Sums of the splits of few tokens' rows, in order, rounded once.  Bound by its launch and one chain of loads (2.2 to 4.7 us).
 template <typename T>
 __global__ __launch_bounds__(64) void few_join_kernel(const float* __restrict__ part, int splits, int64_t n, T* __restrict__ c) {
   const int64_t i = ((int64_t)blockIdx.x * 64 + threadIdx.x) * 4;
@@ -663,6 +690,9 @@ bool few_tokens(int64_t N, int C, int F, int dtype) {
 }
 
 // How a product is cut: blocks of 256 x 256, 128 x 128 or 64 x 128, whole rounds of them, and the tiles behind those in `splits` runs of k_each along k.
+// The cheapest by a model of measured costs.  us of blocks of 256 x 256, 128 x 128 and 64 x 128, bf16: in of 1,563 x 1536 x 4104 45, 54, 63; dh 52, 36, 50;
+// dh of 32,760 tokens with k 512 (F 2048) 185, 215, 202 and k 1,536 (F 4096) 560, 643, 725; fp32, in of 2,050 x 512 x 1368 -, 72, 57.  dW_in of 32,760 x 1536
+// x 4096, 192 tiles of 256 x 256: in four splits 637 + 37, whole 706.
 struct TileShape {
   int bm, bn, resident;       // rows and columns; blocks on the chip at a time
   // microseconds: a step of bf16 and of fp32 with all of them running, a block's start and end, what writing a split's sums adds to it

@@ -6,6 +6,8 @@
 // reads, bf16 columns with transposed 8-byte reads, fp32 columns with 4-byte reads.  Chunks of a staged row are exchanged (xor) so that the lanes of
 // a read fall on different banks; the exchange is made in the global addresses, since a direct load fills LDS in lane order.
 // Rows, columns and k past the operand's end are read as zeros: their buffer offset is put past the buffer's range.
+// Direct loads need no registers on the way and leave the vector units free: the address of a load is one of a thread's few offsets plus a scalar base
+// that moves on by a step.  Steps of 128 bytes are whole lines of either layout.
 #pragma once
 
 #include "lds_pipe.h"

@@ -9,7 +9,11 @@
 //   rows d_weight = sum (1 + scale) A2, d_bias = sum (1 + scale) A1, d_post_weight = residual_scale sum gate B.
 //
 // Bound by HBM: the forward reads x and y and writes r and h, the backward reads x, y, d_r and d_h and writes d_x and d_y, each once; r is computed
-// again from x and y, which are there, and so in 32 bits, while a stored r is rounded.
+// again from x and y, which are there, and so in 32 bits, while a stored r is rounded.  A row stays in registers between its two norms (two passes over
+// them, mean and then centred squares), the next row is on its way, and the shares of the parameters' gradients stay there from token to token.
+// 99,840 x 5120 bf16, RMS norms before and after: forward 838 us (4.9 TB/s of what it moves), backward 1,239 (4.9), its sums 9; 32,760 x 1536, stream fp32,
+// block bf16, 21 rows of the gate: 116 (5.2), 214 (4.2) and 11; 4,099 x 1535 fp32, rows that start at any 4 bytes: 26, 35, 8 and 4.  torch's copy reaches 4.8.
+// Beyond 8,192 columns a lane has two pieces of a row, and the backward's six rows of values do not fit its registers: 10,000 x 16384 bf16 2.8 ms.
 #include <algorithm>
 #include <cmath>
 
@@ -463,7 +467,7 @@ struct ResNormSums {
   float* over;   // [groups][3][C]: weighted sums of the rows of a group of blocks, where there are several groups
 };
 
-// Sums over the pieces of each row of the gate: 16 columns a block, whose 16 threads each take every 16th piece; rows in `gridDim.y`
+// Sums over the pieces of each row of the gate, in a fixed order: 16 columns a block, whose 16 threads each take every 16th piece; rows in `gridDim.y`
 // groups.  Bound by its chain of loads: of 32 columns and 8 threads, with whole lines, it takes a third longer.
 __global__ __launch_bounds__(256) void residual_norm_sums_kernel(const ResNorm p, const float* __restrict__ part, const ResNormSums o, int64_t rows) {
   __shared__ float acc[3][16][17];
