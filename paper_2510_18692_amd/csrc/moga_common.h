@@ -69,7 +69,7 @@ template <int L, typename F>
 __device__ __forceinline__ int lanes_reduce(int v, F f) {
   if constexpr (L >= 64) v = combine_xor<32>(v, f);
   if constexpr (L >= 32) v = combine_xor<16>(v, f);
-  v = combine_xor<8>(v, f);
+  if constexpr (L >= 16) v = combine_xor<8>(v, f);
   v = combine_xor<4>(v, f);
   v = combine_xor<2>(v, f);
   return combine_xor<1>(v, f);

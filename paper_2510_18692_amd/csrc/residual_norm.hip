@@ -96,7 +96,7 @@ struct Parked {
   }
 };
 
-// How the tokens of a piece are dealt out: LANES = 16 or 64 to a token, four waves a block; LANES = 0: a token to a block.
+// How the tokens of a piece are dealt out: LANES = 8 to 64 to a token, four waves a block; LANES = 0: a token to a block.
 template <int LANES>
 struct Lanes {
   static constexpr int kRows = LANES ? 256 / LANES : 1;
@@ -430,15 +430,20 @@ __global__ __launch_bounds__(64 * WAVES, WAVES > 4 ? 4 : 3) void residual_norm_b
     } else {
       __shared__ float acc[3][LANES * PARTS * 8];
       const int wave = threadIdx.x >> 6;
-      if constexpr (LANES == 16) {   // the four tokens of a wave
+      if constexpr (LANES < 64) {   // the tokens of a wave
+        auto all = [](float t) {
+          int v = __float_as_int(t);
+          if constexpr (LANES <= 8) v = combine_xor<8>(v, AddF{});
+          if constexpr (LANES <= 16) v = combine_xor<16>(v, AddF{});
+          return __int_as_float(combine_xor<32>(v, AddF{}));
+        };
 #pragma unroll
         for (int q = 0; q < PARTS; ++q)
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            auto four = [](float t) { return __int_as_float(combine_xor<32>(combine_xor<16>(__float_as_int(t), AddF{}), AddF{})); };
-            a1[q][i] = four(a1[q][i]);
-            a2[q][i] = four(a2[q][i]);
-            bs[q][i] = four(bs[q][i]);
+            a1[q][i] = all(a1[q][i]);
+            a2[q][i] = all(a2[q][i]);
+            bs[q][i] = all(bs[q][i]);
           }
       }
       __syncthreads();   // the last item's sums are read
@@ -545,13 +550,15 @@ __global__ __launch_bounds__(256) void residual_norm_over_kernel(const float* __
   if (o.d_post_weight) o.d_post_weight[col] = s[2];
 }
 
-// 8 columns a lane up to 8,192: a token goes to 16 lanes up to 128 columns, to a wave up to 512, else to a block of a wave per 512.
+// 8 columns a lane up to 8,192: a token goes to 8 lanes up to 64 columns, 16 up to 128, 32 up to 256, a wave up to 512, else to a block of a wave per 512.
+// Lanes without columns are bytes that are not on their way: 10^8 values bf16, C 256 by waves 182 us forward and 635 backward, by 32 lanes 171 and 276; C 64 by
+// 16 lanes 186 and 672, by 8 176 and 309; still half idle, C 136 181 and 580, C 264 180 and 600, C 520 192 and 628.
 struct Shape {
   int lanes, parts, waves, rows;
 };
 Shape shape_of(int C) {
-  if (C <= 128) return {16, 1, 4, 16};
-  if (C <= 512) return {64, 1, 4, 4};
+  for (int lanes = 8; lanes <= 64; lanes *= 2)
+    if (C <= 8 * lanes) return {lanes, 1, 4, 256 / lanes};
   return {0, C <= 8192 ? 1 : 2, std::min(kBlockWaves, (C + 511) / 512), 1};
 }
 
@@ -610,7 +617,9 @@ int check_residual_norm(const moga_residual_norm* a) {
 template <typename F>
 void with_shape(const Shape& s, F&& f) {
 #define MOGA_SHAPE(L, P, W) f(std::integral_constant<int, L>{}, std::integral_constant<int, P>{}, std::integral_constant<int, W>{})
-  if (s.lanes == 16) MOGA_SHAPE(16, 1, 4);
+  if (s.lanes == 8) MOGA_SHAPE(8, 1, 4);
+  else if (s.lanes == 16) MOGA_SHAPE(16, 1, 4);
+  else if (s.lanes == 32) MOGA_SHAPE(32, 1, 4);
   else if (s.lanes == 64) MOGA_SHAPE(64, 1, 4);
   else if (s.waves <= 4) MOGA_SHAPE(0, 1, 4);
   else if (s.parts == 1) MOGA_SHAPE(0, 1, kBlockWaves);

@@ -81,7 +81,7 @@ def test_each_parameter_alone(left):
     _check(t, p, "rms", "layer", 1.0, 20)
 
 
-@pytest.mark.parametrize("N,C,each", [(20011, 128, None), (20011, 128, 97), (6000, 1536, 1560), (9001, 24, 1), (5000, 520, 2)])
+@pytest.mark.parametrize("N,C,each", [(20011, 128, None), (20011, 128, 97), (30011, 64, 501), (20011, 250, 300), (20011, 256, None), (6000, 1536, 1560), (9001, 24, 1), (5000, 520, 2)])
 def test_many_tokens_and_repeated_bits(N, C, each):
     t, p = _inputs(N, C, F32, BF, 3, each=each)
     first = _check(t, p, "rms", "layer", 1.0, each)
