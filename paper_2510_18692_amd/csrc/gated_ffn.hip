@@ -86,6 +86,35 @@ struct Product {
   float* part;           // their sums, [split][left][BM][BN], or NULL for splits of all of k
 };
 
+// What a block does.
+struct Work {
+  bool is_split;
+  unsigned tile, behind, split;   // behind: of the blocks behind `whole`
+  template <typename T>
+  __device__ __forceinline__ explicit Work(const Product<T>& p) {
+    is_split = p.part && blockIdx.x >= p.whole;
+    behind = is_split ? blockIdx.x - p.whole : 0;
+    split = is_split ? behind / p.left : 0;
+    tile = is_split ? p.whole + behind - split * p.left : blockIdx.x;
+  }
+};
+// The product that a tile of two products' list belongs to; it shares k and the list with the first.
+template <typename T>
+__device__ __forceinline__ void select(Product<T>& p, const Product<T>& second, unsigned& tile) {
+  const unsigned tiles = p.tiles_m * p.tiles_n;
+  if (tile < tiles) return;
+  tile -= tiles;
+  p.a = second.a;
+  p.b = second.b;
+  p.lda = second.lda;
+  p.ldb = second.ldb;
+  p.M = second.M;
+  p.N = second.N;
+  p.c = second.c;
+  p.tiles_m = second.tiles_m;
+  p.tiles_n = second.tiles_n;
+}
+
 // a and u go to the backward in bf16 with two more bits each, half a byte a pair: the rounded value's distance from the value, in quarters of a step of
 // bf16 from -1/4 on.  What the backward makes of them is rounded itself (da, du); from a and u in bf16 alone the gradients of x and W_in are off by
 // 1.76 times what a single rounding of the result is (2-norm, 32,760 x 1536 x 4096), with these bits by 1.45.  A zero stays one.
@@ -296,7 +325,7 @@ __device__ __forceinline__ void put_gated(const Product<float>& p, int64_t row, 
 //   out (kPlain, rows x rows)          342   1,210        3,318   1,380
 //   dh  (kGatedBwd, rows x columns)    560     740        4,059   1,130
 //   dx  (kPlain, rows x columns)       618   1,330        6,546   1,400
-//   dW_in, dW_out (columns x columns)  637 + 37 and 340 + 23 to join   6,577 + 21 and 3,392 + 11
+//   dW_in, dW_out (columns x columns)  963 + 12 to join  1,280   9,964 + 35  1,380
 // The long products are bound by power: the matrix cores are busy 0.71 to 0.75 of the cycles at 1.75 to 1.85 GHz of 2.4.  Fed from no loads at all the loop
 // makes 1,650 to 1,730, from loads of the same lines over and over 1,430 to 1,500: the rest is what bringing 64 KB a step from the caches costs in time
 // and in clock.  LDS has no bank conflicts and is busy 0.28 of the cycles.  With C = 1536 a tile's 24 steps (35 us) are followed by its epilogue,
@@ -304,7 +333,7 @@ __device__ __forceinline__ void put_gated(const Product<float>& p, int64_t row, 
 // Starting half of the CUs half a tile later puts that traffic beside the others' products and gains nothing.
 // Fp32, 8,192 x 4096 x 4096, blocks of 128: 143 TFLOP/s of rows x rows, 129 to 132 with columns (4-byte reads), of a library's 153.
 template <typename T, Kind KIND, bool A_KFIRST, bool B_KFIRST, int WM, int WN, int TM, int TN>
-__global__ __launch_bounds__(64 * WM * WN, TM == 2 ? 3 : 2) void product_kernel(const Product<T> p) {
+__device__ __forceinline__ void product_tile(const Product<T>& p, const Work& work) {
   constexpr int THREADS = 64 * WM * WN, BM = 16 * WM * TM, BN = 16 * WN * TN;
   using OpA = Operand<T, A_KFIRST, BM, THREADS, TM>;
   using OpB = Operand<T, B_KFIRST, BN, THREADS, TN>;
@@ -314,13 +343,11 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 2 ? 3 : 2) void product_kernel(
   const unsigned lds = lds_addr_uniform(s_mem);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
 
-  const bool is_split = p.part && blockIdx.x >= p.whole;
-  const unsigned behind = is_split ? blockIdx.x - p.whole : 0, split = is_split ? behind / p.left : 0;
   unsigned bm, bn;
-  tile_of(is_split ? p.whole + behind - split * p.left : blockIdx.x, p.tiles_m, p.tiles_n, bm, bn);
+  tile_of(work.tile, p.tiles_m, p.tiles_n, bm, bn);
 
-  const int64_t m0 = (int64_t)bm * BM, k0 = split * p.k_each;
-  const int n0 = bn * (KIND == kGated ? BN / 2 : BN), k_count = (int)(is_split ? min(p.k_each, p.K - k0) : p.K);
+  const int64_t m0 = (int64_t)bm * BM, k0 = work.split * p.k_each;
+  const int n0 = bn * (KIND == kGated ? BN / 2 : BN), k_count = (int)(work.is_split ? min(p.k_each, p.K - k0) : p.K);
   OpA oa;
   OpB ob;
   oa.init(p.a, p.lda, m0, p.M, k0, k_count, wm * TM, lds);
@@ -401,8 +428,8 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 2 ? 3 : 2) void product_kernel(
   const int r = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
   const int64_t N = p.N;
   const int col0 = n0 + wn * TN * 16;
-  if (is_split) {
-    float* out = p.part + (size_t)behind * BM * BN + wn * TN * 16;
+  if (work.is_split) {
+    float* out = p.part + (size_t)work.behind * BM * BN + wn * TN * 16;
 #pragma unroll
     for (int m = 0; m < TM; ++m)
 #pragma unroll
@@ -446,15 +473,26 @@ __global__ __launch_bounds__(64 * WM * WN, TM == 2 ? 3 : 2) void product_kernel(
   if constexpr (KIND == kPlain) rows(std::integral_constant<int, 0>{});
   else with_activation(p.act, rows);
 }
+template <typename T, Kind KIND, bool A_KFIRST, bool B_KFIRST, int WM, int WN, int TM, int TN>
+__global__ __launch_bounds__(64 * WM * WN, TM == 2 ? 3 : 2) void product_kernel(const Product<T> p) {
+  product_tile<T, KIND, A_KFIRST, B_KFIRST, WM, WN, TM, TN>(p, Work(p));
+}
+// Two products of the same k in one list of tiles: fewer of them are behind the last whole round.
+template <typename T, bool A_KFIRST, bool B_KFIRST, int WM, int WN, int TM, int TN>
+__global__ __launch_bounds__(64 * WM * WN, TM == 2 ? 3 : 2) void product_pair_kernel(Product<T> p, const Product<T> second) {
+  Work work(p);
+  select(p, second, work.tile);
+  product_tile<T, kPlain, A_KFIRST, B_KFIRST, WM, WN, TM, TN>(p, work);
+}
 
 // Tiles that were split along k: the sums of their splits, in order (results repeat bit by bit), and what a block does with its sums.  A thread has eight
 // columns of a row (kGated: of a, and the same eight of u); blockIdx.x is the tile, blockIdx.y a run of its rows.  Bound by the partial sums' bytes, which
-// come from the cache behind the L2s where they fit: 192 tiles of 256 x 256 in four splits (201 MB) 37 us, 5.4 TB/s.
+// come from the cache behind the L2s where they fit: 148 tiles of 256 x 256 in five splits (194 MB) 35 us, 5.5 TB/s.
 template <typename T, Kind KIND, int BM, int BN>
-__global__ __launch_bounds__(256) void join_kernel(const Product<T> p, int splits) {
+__device__ __forceinline__ void join_tile(const Product<T>& p, unsigned tile, int splits) {
   constexpr int COLS = KIND == kGated ? BN / 2 : BN, SETS = KIND == kGated ? 2 : 1, PER = COLS / 8;
   unsigned bm, bn;
-  tile_of(p.whole + blockIdx.x, p.tiles_m, p.tiles_n, bm, bn);
+  tile_of(tile, p.tiles_m, p.tiles_n, bm, bn);
   const int at = blockIdx.y * 256 + threadIdx.x, r = at / PER, c = at % PER * 8;
   const int64_t row = (int64_t)bm * BM + r, N = p.N;
   const int col = bn * COLS + c;
@@ -544,6 +582,16 @@ __global__ __launch_bounds__(256) void join_kernel(const Product<T> p, int split
       }
     });
   }
+}
+template <typename T, Kind KIND, int BM, int BN>
+__global__ __launch_bounds__(256) void join_kernel(const Product<T> p, int splits) {
+  join_tile<T, KIND, BM, BN>(p, p.whole + blockIdx.x, splits);
+}
+template <typename T, int BM, int BN>
+__global__ __launch_bounds__(256) void join_pair_kernel(Product<T> p, const Product<T> second, int splits) {
+  unsigned tile = p.whole + blockIdx.x;
+  select(p, second, tile);
+  join_tile<T, kPlain, BM, BN>(p, tile, splits);
 }
 
 // ---- few tokens ----
@@ -692,30 +740,37 @@ bool few_tokens(int64_t N, int C, int F, int dtype) {
 // How a product is cut: blocks of 256 x 256, 128 x 128 or 64 x 128, whole rounds of them, and the tiles behind those in `splits` runs of k_each along k.
 // The cheapest by a model of measured costs.  us of blocks of 256 x 256, 128 x 128 and 64 x 128, bf16: in of 1,563 x 1536 x 4104 45, 54, 63; dh 52, 36, 50;
 // dh of 32,760 tokens with k 512 (F 2048) 185, 215, 202 and k 1,536 (F 4096) 560, 643, 725; fp32, in of 2,050 x 512 x 1368 -, 72, 57.  dW_in of 32,760 x 1536
-// x 4096, 192 tiles of 256 x 256: in four splits 637 + 37, whole 706.
+// x 4096 alone, 192 tiles of 256 x 256: in four splits 637 + 37, whole 706.
 struct TileShape {
   int bm, bn, resident;       // rows and columns; blocks on the chip at a time
   // microseconds: a step of bf16 and of fp32 with all of them running, a block's start and end, what writing a split's sums adds to it
   double step, step32, ends, sums;
 };
 constexpr TileShape kTiles[] = {{256, 256, 256, 1.45, 0, 12, 6}, {128, 128, 512, 1.0, 4.1, 7, 3}, {64, 128, 768, 0.9, 3.2, 6, 2}};
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 struct Cut {
   int shape, splits;
   int64_t k_each;
-  unsigned tiles_m, tiles_n, whole, left;
+  unsigned whole, left;
+  double cost;
   size_t part_bytes() const { return splits > 1 ? (size_t)splits * left * kTiles[shape].bm * kTiles[shape].bn * sizeof(float) : 0; }
 };
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+struct Size {
+  int64_t M, N;
+  unsigned tiles_m(const TileShape& t) const { return (unsigned)ceil_div(M, t.bm); }
+  unsigned tiles_n(const TileShape& t, Kind kind) const { return (unsigned)ceil_div(N, kind == kGated ? t.bn / 2 : t.bn); }
+};
 
-Cut cut_of(int64_t M, int64_t N, int64_t K, int dtype, Kind kind) {
+// Of one product, or of several of the same k in one list of tiles.
+Cut cut_of(std::initializer_list<Size> sizes, int64_t K, int dtype, Kind kind) {
   const int bk = dtype == MOGA_F32 ? 32 : 64;
   const int64_t steps = ceil_div(K, bk);
   Cut best{};
-  double least = 0;
   for (int shape = dtype == MOGA_F32 ? 1 : 0; shape < 3; ++shape) {
     const TileShape& t = kTiles[shape];
     const double step = dtype == MOGA_F32 ? t.step32 : t.step, mb = t.bm * t.bn * 4e-6;   // a tile's sums in MB
-    const int64_t tiles_m = ceil_div(M, t.bm), tiles_n = ceil_div(N, kind == kGated ? t.bn / 2 : t.bn), tiles = tiles_m * tiles_n;
+    int64_t tiles = 0;
+    for (const Size& size : sizes) tiles += (int64_t)size.tiles_m(t) * size.tiles_n(t, kind);
     const int64_t whole = tiles / t.resident * t.resident, left = tiles - whole;
     for (int s = 1; s <= 32; ++s) {
       const int64_t each = ceil_div(steps, s);
@@ -723,36 +778,60 @@ Cut cut_of(int64_t M, int64_t N, int64_t K, int dtype, Kind kind) {
       double cost = whole / t.resident * (steps * step + t.ends);
       if (left) cost += ceil_div(left * s, t.resident) * (each * step + t.ends);
       if (s > 1) cost += 5 + ceil_div(left * s, t.resident) * t.sums + left * s * mb * 0.27;
-      if (least == 0 || cost < least) {
-        least = cost;
-        best = {shape, s, s > 1 ? each * bk : K, (unsigned)tiles_m, (unsigned)tiles_n, (unsigned)(s > 1 ? whole : tiles), (unsigned)(s > 1 ? left : 0)};
-      }
+      if (best.splits == 0 || cost < best.cost) best = {shape, s, s > 1 ? each * bk : K, (unsigned)(s > 1 ? whole : tiles), (unsigned)(s > 1 ? left : 0), cost};
     }
   }
   return best;
 }
+Cut cut_of(int64_t M, int64_t N, int64_t K, int dtype, Kind kind) { return cut_of({{M, N}}, K, dtype, kind); }
 
-template <typename T, Kind KIND, bool AK, bool BK, int WN, int TM>
-void launch_tiles(const Product<T>& p, int splits, hipStream_t st) {
-  constexpr int BM = 32 * TM, BN = 64 * WN;
-  product_kernel<T, KIND, AK, BK, 2, WN, TM, 4><<<p.whole + p.left * splits, 128 * WN, 0, st>>>(p);
-  if (p.left) join_kernel<T, KIND, BM, BN><<<dim3(p.left, BM * BN / (KIND == kGated ? 4096 : 2048)), 256, 0, st>>>(p, splits);
+template <typename T>
+void apply_cut(Product<T>& p, const Cut& c, Kind kind, void* part) {
+  const Size size{p.M, p.N};
+  p.tiles_m = size.tiles_m(kTiles[c.shape]);
+  p.tiles_n = size.tiles_n(kTiles[c.shape], kind);
+  p.whole = c.whole;
+  p.left = c.left;
+  p.k_each = c.k_each;
+  p.part = c.splits > 1 ? (float*)part : nullptr;
+}
+// f(waves along n, rows of tiles of a wave), as constants
+template <typename T, typename F>
+void with_tiles(int shape, F&& f) {
+  if constexpr (sizeof(T) == 2) {
+    if (shape == 0) return f(std::integral_constant<int, 4>{}, std::integral_constant<int, 8>{});
+  }
+  if (shape == 1) f(std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{});
+  else f(std::integral_constant<int, 2>{}, std::integral_constant<int, 2>{});
 }
 
 template <typename T, Kind KIND, bool AK, bool BK>
 void launch_product(Product<T> p, int dtype, void* part, hipStream_t st) {
   const Cut c = cut_of(p.M, p.N, p.K, dtype, KIND);
-  p.tiles_m = c.tiles_m;
-  p.tiles_n = c.tiles_n;
-  p.whole = c.whole;
-  p.left = c.left;
-  p.k_each = c.k_each;
-  p.part = c.splits > 1 ? (float*)part : nullptr;
-  if constexpr (sizeof(T) == 2) {
-    if (c.shape == 0) return launch_tiles<T, KIND, AK, BK, 4, 8>(p, c.splits, st);
+  apply_cut(p, c, KIND, part);
+  with_tiles<T>(c.shape, [&](auto wn, auto tm) {
+    constexpr int WN = wn.value, TM = tm.value, BM = 32 * TM, BN = 64 * WN;
+    product_kernel<T, KIND, AK, BK, 2, WN, TM, 4><<<p.whole + p.left * c.splits, 128 * WN, 0, st>>>(p);
+    if (p.left) join_kernel<T, KIND, BM, BN><<<dim3(p.left, BM * BN / (KIND == kGated ? 4096 : 2048)), 256, 0, st>>>(p, c.splits);
+  });
+}
+
+// Two products of the same k, in one list of tiles where that takes fewer rounds.  Both weights' gradients of 32,760 x 1536 x 4096: 288 tiles, a whole round and
+// 32 in eight splits, 963 + 12 us; by themselves 192 in four splits and 96 in five, 1,037 us.  2,050 x 512 x 1368 fp32 105 and 107 us.
+template <typename T, bool AK, bool BK>
+void launch_two(Product<T> p, Product<T> q, int dtype, void* part, hipStream_t st) {
+  const Cut c = cut_of({{p.M, p.N}, {q.M, q.N}}, p.K, dtype, kPlain);
+  if (c.cost >= cut_of(p.M, p.N, p.K, dtype, kPlain).cost + cut_of(q.M, q.N, q.K, dtype, kPlain).cost) {
+    launch_product<T, kPlain, AK, BK>(p, dtype, part, st);
+    return launch_product<T, kPlain, AK, BK>(q, dtype, part, st);
   }
-  if (c.shape == 1) launch_tiles<T, KIND, AK, BK, 2, 4>(p, c.splits, st);
-  else launch_tiles<T, KIND, AK, BK, 2, 2>(p, c.splits, st);
+  apply_cut(p, c, kPlain, part);
+  apply_cut(q, c, kPlain, part);
+  with_tiles<T>(c.shape, [&](auto wn, auto tm) {
+    constexpr int WN = wn.value, TM = tm.value, BM = 32 * TM, BN = 64 * WN;
+    product_pair_kernel<T, AK, BK, 2, WN, TM, 4><<<p.whole + p.left * c.splits, 128 * WN, 0, st>>>(p, q);
+    if (p.left) join_pair_kernel<T, BM, BN><<<dim3(p.left, BM * BN / 2048), 256, 0, st>>>(p, q, c.splits);
+  });
 }
 
 // Few tokens: a block for every 16 columns and, of a plain product with fewer than kFewBlocks of those, every run of k, no shorter than 1 KB.
@@ -819,7 +898,8 @@ size_t ffn_bwd_part(int64_t N, int F, int dtype) { return round_up((size_t)N * 2
 size_t ffn_bwd_ws(int64_t N, int C, int F, int dtype) {
   const int64_t F2 = 2 * (int64_t)F;
   return ffn_bwd_part(N, F, dtype) + std::max({cut_of(N, F, C, dtype, kGatedBwd).part_bytes(), cut_of(N, C, F2, dtype, kPlain).part_bytes(),
-                                               cut_of(F2, C, N, dtype, kPlain).part_bytes(), cut_of(C, F, N, dtype, kPlain).part_bytes()});
+                                               cut_of(F2, C, N, dtype, kPlain).part_bytes(), cut_of(C, F, N, dtype, kPlain).part_bytes(),
+                                               cut_of({{F2, C}, {C, F}}, N, dtype, kPlain).part_bytes()});
 }
 
 template <typename T>
@@ -833,8 +913,10 @@ void ffn_bwd(const void* d_y, const void* x, const void* w_in, const void* w_out
     launch_product<T, kGatedBwd, false, true>(dh, dtype, part, st);
   }
   if (d_x) launch_product<T, kPlain, false, true>(product<T>(ws, 2 * (int64_t)F, w_in, C, N, C, 2 * (int64_t)F, d_x), dtype, part, st);
-  if (d_w_in) launch_product<T, kPlain, true, true>(product<T>(ws, 2 * (int64_t)F, x, C, 2 * (int64_t)F, C, N, d_w_in), dtype, part, st);
-  if (d_w_out) launch_product<T, kPlain, true, true>(product<T>(d_y, C, h, F, C, F, N, d_w_out), dtype, part, st);
+  const Product<T> w_in_grad = product<T>(ws, 2 * (int64_t)F, x, C, 2 * (int64_t)F, C, N, d_w_in), w_out_grad = product<T>(d_y, C, h, F, C, F, N, d_w_out);
+  if (d_w_in && d_w_out) launch_two<T, true, true>(w_in_grad, w_out_grad, dtype, part, st);
+  else if (d_w_in) launch_product<T, kPlain, true, true>(w_in_grad, dtype, part, st);
+  else if (d_w_out) launch_product<T, kPlain, true, true>(w_out_grad, dtype, part, st);
 }
 
 int check_ffn(int64_t N, int C, int F, int dtype, int act) {
@@ -844,7 +926,8 @@ int check_ffn(int64_t N, int C, int F, int dtype, int act) {
   const int v = dtype == MOGA_F32 ? 4 : 8;
   if (C % v || F % v || C > kFfnMaxC || F > kFfnMaxF || N >= ((int64_t)1 << 31)) return MOGA_ERR_UNSUPPORTED;
   // blocks of the largest grids, and bytes of 256 rows within 31 bits
-  const int64_t most = std::max({ceil_div(N, 64) * ceil_div(F, 64), ceil_div(N, 64) * ceil_div(C, 128), ceil_div(2 * (int64_t)F, 64) * ceil_div(C, 128)});
+  const int64_t most = std::max({ceil_div(N, 64) * ceil_div(F, 64), ceil_div(N, 64) * ceil_div(C, 128),
+                                 ceil_div(2 * (int64_t)F, 64) * ceil_div(C, 128) + ceil_div(C, 64) * ceil_div(F, 128)});
   return grid_fits(most + 32 * 768, 512) ? MOGA_OK : MOGA_ERR_UNSUPPORTED;
 }
 

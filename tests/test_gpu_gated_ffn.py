@@ -44,7 +44,8 @@ def test_f32(N, C, F, act):
     _check(N, C, F, F32, act)
 
 
-@pytest.mark.parametrize("dtype,N,C,F", [(BF, 20000, 128, 264), (BF, 9001, 520, 136), (BF, 300, 264, 16392), (F32, 9001, 132, 68), (BF, 2600, 1032, 1544)])
+@pytest.mark.parametrize("dtype,N,C,F", [(BF, 20000, 128, 264), (BF, 9001, 520, 136), (BF, 300, 264, 16392), (F32, 9001, 132, 68), (BF, 2600, 1032, 1544), (BF, 2126, 1296, 1936),
+                                         (BF, 4601, 1544, 3104), (F32, 541, 792, 3128)])
 def test_long_sums_and_repeated_bits(dtype, N, C, F):
     (x, wi, wo, dy), got = _check(N, C, F, dtype, "silu")
     for _ in range(3):
