@@ -116,7 +116,7 @@ struct RowSum {
       __syncthreads();
       const int waves = blockDim.x >> 6, lane = threadIdx.x & 15;
 #pragma unroll
-      for (int k = 0; k < K; ++k) v[k] = lanes_sum<16>(lane < waves ? lds[turn][lane & (WAVES - 1)][k] : 0.f);
+      for (int k = 0; k < K; ++k) v[k] = lanes_sum<16>(lane < waves ? lds[turn][min(lane, WAVES - 1)][k] : 0.f);
       turn ^= 1;
     }
   }

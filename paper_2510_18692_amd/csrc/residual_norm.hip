@@ -34,7 +34,10 @@ struct ResNorm {
 
 constexpr int kBlockWaves = 16;   // of a block that owns a token, at most
 
-// Eight columns of a row.  EVEN: rows are whole eights, and a lane has all of one or none; else the row's last piece is looked at column by column.
+// Eight columns of a row.  EVEN: rows are whole eights, and a lane has all of one or none; else the row's last piece is looked at column by column
+// (10^8 values bf16, backward: C 264 595 us so and 312 even, C 768 477 and 289, C 1000 380 and 284).
+// The values stay as they lie until get(): without the asm the compiler unpacks them right behind the loads, for which the next row's do not have the
+// registers (backward of 10^8 values bf16, C 5120: 597 us).
 template <typename T, bool EVEN> struct Eight;
 template <bool EVEN> struct Eight<unsigned short, EVEN> {
   Bytes16<unsigned short> b;
@@ -42,7 +45,9 @@ template <bool EVEN> struct Eight<unsigned short, EVEN> {
     if constexpr (EVEN) b = col < C ? *(const Bytes16<unsigned short>*)(row + col) : Bytes16<unsigned short>{};
     else b = load_part(row, col, C, last);
   }
-  __device__ __forceinline__ void get(float (&f)[8], int col, int C) const {
+  __device__ __forceinline__ void get(float (&f)[8], int col, int C) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm("" : "+v"(b.w[i]));
     unpack(b, f);
     if constexpr (!EVEN) clear_past(f, col, C);
   }
@@ -56,7 +61,9 @@ template <bool EVEN> struct Eight<float, EVEN> {
       else b[i] = load_part(row, col + 4 * i, C, last);
     }
   }
-  __device__ __forceinline__ void get(float (&f)[8], int col, int C) const {
+  __device__ __forceinline__ void get(float (&f)[8], int col, int C) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) asm("" : "+v"(b[i / 4].w[i % 4]));
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(b[i / 4].w[i % 4]);
     if constexpr (!EVEN) clear_past(f, col, C);
@@ -282,8 +289,10 @@ struct ResNormGrads {
 };
 
 // The shares of the tokens that run beside each other in a block are added in a fixed order: results repeat bit by bit.
-template <typename TX, typename TY, int LANES, int PARTS, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, WAVES > 4 ? 4 : 3) void residual_norm_bwd_kernel(const ResNorm p, const ResNormGrads o) {
+// Three waves a SIMD; of blocks of three waves, of which a CU takes four only where each SIMD has room for one wave more, four (10^8 values, C 1536: bf16 282 us
+// instead of 325, stream fp32 401 instead of 433; the other blocks lose up to a tenth so, fp32 alone gains nothing).
+template <typename TX, typename TY, int LANES, int PARTS, int WAVES, bool EVEN>
+__global__ __launch_bounds__(64 * WAVES, WAVES > 4 || (WAVES == 3 && sizeof(TY) == 2) ? 4 : 3) void residual_norm_bwd_kernel(const ResNorm p, const ResNormGrads o) {
 #pragma clang fp contract(off)   // g is one value in its mean and in what the mean is taken from
   __shared__ float lds[2][WAVES][2];
   RowSum<LANES, 2, WAVES> sum{lds};
@@ -301,8 +310,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES > 4 ? 4 : 3) void residual_norm_b
   for (int64_t item = blockIdx.x; item < p.items; item += gridDim.x) {
     const Piece piece(p, item);
     int64_t row = piece.first + d.slot;
-    Eight<TX, false> nx[PARTS], nr[PARTS];
-    Eight<TY, false> ny[PARTS], nh[PARTS];
+    Eight<TX, EVEN> nx[PARTS], nr[PARTS];
+    Eight<TY, EVEN> ny[PARTS], nh[PARTS];
     float st[4];
     auto fetch = [&](int64_t at) {
       const bool last = at + 1 == p.N;
@@ -380,12 +389,15 @@ __global__ __launch_bounds__(64 * WAVES, WAVES > 4 ? 4 : 3) void residual_norm_b
 #pragma unroll
         for (int q = 0; q < PARTS; ++q) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) D[q][i] += r * (g[q][i] - m0 - f[q][i] * m1);
-          clear_past(D[q], col[q], C);
+          for (int i = 0; i < 8; ++i) {
+            D[q][i] += r * (g[q][i] - m0 - f[q][i] * m1);
+            if (EVEN) D[q][i] = col[q] < C ? D[q][i] : 0.f;
+          }
+          if constexpr (!EVEN) clear_past(D[q], col[q], C);
         }
       }
 #pragma unroll
-      for (int q = 0; q < PARTS; ++q) store8<false>((TX*)o.d_x + row * C, col[q], C, D[q]);
+      for (int q = 0; q < PARTS; ++q) store8<EVEN>((TX*)o.d_x + row * C, col[q], C, D[q]);
       if (y) {
         float s[2] = {0.f, 0.f};
 #pragma unroll
@@ -406,7 +418,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES > 4 ? 4 : 3) void residual_norm_b
             for (int i = 0; i < 8; ++i) D[q][i] = r_y * (D[q][i] - m0 - v[q][i] * m1);
         }
 #pragma unroll
-        for (int q = 0; q < PARTS; ++q) store8<false>((TY*)o.d_y + row * C, col[q], C, D[q]);
+        for (int q = 0; q < PARTS; ++q) store8<EVEN>((TY*)o.d_y + row * C, col[q], C, D[q]);
       }
     }
     if (!o.part) continue;
@@ -551,8 +563,8 @@ __global__ __launch_bounds__(256) void residual_norm_over_kernel(const float* __
 }
 
 // 8 columns a lane up to 8,192: a token goes to 8 lanes up to 64 columns, 16 up to 128, 32 up to 256, a wave up to 512, else to a block of a wave per 512.
-// Lanes without columns are bytes that are not on their way: 10^8 values bf16, C 256 by waves 182 us forward and 635 backward, by 32 lanes 171 and 276; C 64 by
-// 16 lanes 186 and 672, by 8 176 and 309; still half idle, C 136 181 and 580, C 264 180 and 600, C 520 192 and 628.
+// Lanes without columns are bytes that are not on their way: 10^8 values bf16, C 64 by 8 lanes 176 us forward and 298 backward, by 16 186 and 672 (before the
+// even form); what is left of it, C 264 178 and 312, C 520 184 and 382.
 struct Shape {
   int lanes, parts, waves, rows;
 };
@@ -621,6 +633,7 @@ void with_shape(const Shape& s, F&& f) {
   else if (s.lanes == 16) MOGA_SHAPE(16, 1, 4);
   else if (s.lanes == 32) MOGA_SHAPE(32, 1, 4);
   else if (s.lanes == 64) MOGA_SHAPE(64, 1, 4);
+  else if (s.waves == 3) MOGA_SHAPE(0, 1, 3);
   else if (s.waves <= 4) MOGA_SHAPE(0, 1, 4);
   else if (s.parts == 1) MOGA_SHAPE(0, 1, kBlockWaves);
   else MOGA_SHAPE(0, 2, kBlockWaves);
@@ -697,7 +710,10 @@ extern "C" int moga_residual_norm_bwd(const moga_residual_norm* a, const float* 
     const unsigned grid = (unsigned)std::min<int64_t>(p.items, 8 * blocks_of(s, kBwdWaves));
     with_types(a->x_dtype, a->y_dtype, [&](auto tx, auto ty) {
       with_shape(s, [&](auto lanes, auto parts, auto waves) {
-        residual_norm_bwd_kernel<decltype(tx), decltype(ty), lanes.value, parts.value, waves.value><<<grid, 64 * s.waves, 0, st>>>(p, o);
+        using TX = decltype(tx);
+        using TY = decltype(ty);
+        if (p.C % 8 == 0) residual_norm_bwd_kernel<TX, TY, lanes.value, parts.value, waves.value, true><<<grid, 64 * s.waves, 0, st>>>(p, o);
+        else residual_norm_bwd_kernel<TX, TY, lanes.value, parts.value, waves.value, false><<<grid, 64 * s.waves, 0, st>>>(p, o);
       });
     });
   } else {
