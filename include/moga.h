@@ -615,7 +615,8 @@ int moga_gated_ffn_fwd(const void* x, const void* w_in, const void* w_out, int d
 /*
  * Backward of moga_gated_ffn_fwd, from its au and h:  dh = d_y W_out,  da = dh * u * act'(a),  du = dh * act(a) (rounded once),
  *   d_x = [da, du] W_in;  d_w_in = [da, du]^T x;  d_w_out = d_y^T h        each like what it is the gradient of, each NULL to skip
- * of N == 0 tokens the weights' gradients are zeros.  Workspace: MOGA_OP_GATED_FFN_BWD (it holds [da, du]).
+ * of N == 0 tokens the weights' gradients are zeros.  Results repeat bit by bit; d_w_in and d_w_out asked for together may be summed in another order than
+ * each alone.  Workspace: MOGA_OP_GATED_FFN_BWD (it holds [da, du]).
  */
 int moga_gated_ffn_bwd(const void* d_y, const void* x, const void* w_in, const void* w_out, const void* au, const void* h, int dtype, int64_t N,
                        int C, int F, int activation, void* d_x_or_null, void* d_w_in_or_null, void* d_w_out_or_null, void* ws, size_t ws_bytes,

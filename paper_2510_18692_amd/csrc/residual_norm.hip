@@ -11,9 +11,9 @@
 // Bound by HBM: the forward reads x and y and writes r and h, the backward reads x, y, d_r and d_h and writes d_x and d_y, each once; r is computed
 // again from x and y, which are there, and so in 32 bits, while a stored r is rounded.  A row stays in registers between its two norms (two passes over
 // them, mean and then centred squares), the next row is on its way, and the shares of the parameters' gradients stay there from token to token.
-// 99,840 x 5120 bf16, RMS norms before and after: forward 838 us (4.9 TB/s of what it moves), backward 1,239 (4.9), its sums 9; 32,760 x 1536, stream fp32,
-// block bf16, 21 rows of the gate: 116 (5.2), 214 (4.2) and 11; 4,099 x 1535 fp32, rows that start at any 4 bytes: 26, 35, 8 and 4.  torch's copy reaches 4.8.
-// Beyond 8,192 columns a lane has two pieces of a row, and the backward's six rows of values do not fit its registers: 10,000 x 16384 bf16 2.8 ms.
+// 99,840 x 5120 bf16, RMS norms before and after: forward 832 us (4.9 TB/s of what it moves), backward 1,239 (4.9), its sums 9; 32,760 x 1536, stream fp32,
+// block bf16, 21 rows of the gate: 116 (5.2), 196 (4.6) and 11; 4,099 x 1535 fp32, rows that start at any 4 bytes: 25, 33, 8 and 4.  torch's copy reaches 4.8.
+// Beyond 8,192 columns a lane has two pieces of a row, and the backward's six rows of values do not fit its registers: 6,103 x 16384 bf16 1.54 ms, 0.78 TB/s.
 #include <algorithm>
 #include <cmath>
 
