@@ -597,11 +597,18 @@ ResNorm make(const moga_residual_norm* a) {
           a->residual_scale, a->eps, 1, 1, 1};
 }
 constexpr int kFwdWaves = 24, kBwdWaves = 12;   // of a CU
-constexpr int kBwdLeast = 8;                    // tokens of a lane group and piece
+// Tokens of a lane group and piece, of the backward: a piece's tokens take their turns, and so do 64 pieces whose sums are added up.
+// Few tokens go in shorter pieces: bf16, us with one row of the gate, pieces of 8 tokens and these: C 5120, 8 tokens 26 and 10, 300 31 and 22, 1,560 37 and 35;
+// C 512, 63 tokens 24 and 9, 3,000 19 and 17, 8,000 23 and 25.
+int bwd_least(int64_t N, const Shape& s) {
+  int least = 1;
+  while (least < 8 && (int64_t)least * least * 64 * s.rows < N) ++least;
+  return least;
+}
 
 ResNorm make_bwd(const moga_residual_norm* a) {
   ResNorm p = make(a);
-  if (a->N > 0) deal(p, (a->N + p.each - 1) / p.each, blocks_of(shape_of(p.C), kBwdWaves), kBwdLeast, true);
+  if (a->N > 0) deal(p, (a->N + p.each - 1) / p.each, blocks_of(shape_of(p.C), kBwdWaves), bwd_least(a->N, shape_of(p.C)), true);
   return p;
 }
 
@@ -677,11 +684,11 @@ extern "C" int moga_residual_norm_fwd(const moga_residual_norm* a, void* r, void
   return launch_status();
 }
 
-// M: rows of gate, scale and shift.  deal() makes no more pieces than this: all but the last of each row are of kBwdLeast tokens a lane group or more.
+// M: rows of gate, scale and shift.  deal() makes no more pieces than this: all but the last of each row are of bwd_least tokens a lane group or more.
 extern "C" size_t moga_residual_norm_bwd_ws_bytes(int64_t N, int M, int C) {
   if (N <= 0 || M < 1 || M > N || C < 1 || C > kNormMaxC || N >= ((int64_t)1 << 31)) return 0;
   const Shape s = shape_of(C);
-  const int64_t items = M + std::min<int64_t>(4 * blocks_of(s, kBwdWaves), N / (s.rows * kBwdLeast));
+  const int64_t items = M + std::min<int64_t>(4 * blocks_of(s, kBwdWaves), N / (s.rows * bwd_least(N, s)));
   return ((size_t)items + kOverGroups) * 3 * C * sizeof(float);
 }
 
