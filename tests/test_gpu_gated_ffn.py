@@ -132,6 +132,27 @@ def test_arguments_whose_square_overflows(act, dtype):
     assert not d_wi.isnan().any() and d_wi[8, 0].isinf()   # act(a) x is 1e30 * 1e15, past fp32's range
 
 
+def test_lower_tail_of_gelu():
+    """fp32, a = -2 .. -12 exactly: h and the gradients by a and by u, relative to themselves.  Phi(a) = erfc(z) / 2 with z = -a / sqrt 2 off by 2 u (the constant
+    and the product), where d ln erfc / dz is below 2 z + 2 / z in size: 2 u (2 z^2 + 2) = (2 a^2 + 4) u, and 32 u (16 ulp) for erfc itself.  The density: its
+    argument a^2 / 2 twice rounded, a^2 u, 4 u (2 ulp) for exp and 4 u for its products.  Products of the results and the derivative's sum: 8 u."""
+    n = 41
+    a = -2 - torch.arange(n, device="cuda", dtype=torch.float64) / 4
+    x, wi, wo = (torch.zeros(s, device="cuda") for s in ((n, 4), (8, 4), (4, 4)))
+    x[:, 0], x[:, 1] = a.float(), 1
+    wi[0, 0], wi[4, 1], wo[0, 0] = 1, 1, 1
+    _, au, h = mg.moga_gated_ffn_fwd(x, wi, wo, "gelu")
+    dy = torch.zeros_like(x)
+    dy[:, 0] = 1
+    d_x, _, _ = mg.moga_gated_ffn_bwd(dy, x, wi, wo, au, h, "gelu")
+    u, phi, density = ref.U, torch.erfc(-a * 0.5 ** 0.5) / 2, torch.exp(-a * a / 2) * (2 * torch.pi) ** -0.5
+    e_phi, e_density = (2 * a * a + 36) * u * phi, (a * a + 8) * u * density
+    e_act = a.abs() * (e_phi + 8 * u * phi)
+    within(h[:, 0], a * phi, e_act, "h")
+    within(d_x[:, 1], a * phi, e_act, "by u")
+    within(d_x[:, 0], phi + a * density, e_phi + 8 * u * phi + a.abs() * (e_density + 8 * u * density), "by a")
+
+
 def test_parts_of_the_backward():
     x, wi, wo, dy = _inputs(300, 136, 264, BF, 1)
     _, au, h = mg.moga_gated_ffn_fwd(x, wi, wo)
