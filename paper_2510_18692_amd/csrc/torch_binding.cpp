@@ -1143,23 +1143,27 @@ struct ResidualNormFunction : public torch::autograd::Function<ResidualNormFunct
     const std::vector<int64_t> k = ctx->saved_data["kinds"].toIntVector(), sizes = ctx->saved_data["sizes"].toIntVector();
     const std::vector<double> f = ctx->saved_data["factors"].toDoubleVector();
     const auto type = (at::ScalarType)k[3];
-    const ResidualNorm p(s[0], or_none(s[1]), or_none(s[2]), or_none(s[3]), or_none(s[4]), or_none(s[5]), or_none(s[6]), or_none(s[7]), k[0], k[1], f[0],
-                         k[2] ? std::optional<int64_t>(k[2]) : std::nullopt, f[1], type);
+    const bool has_r = s[1].defined(), has_h = k[1] != MOGA_NORM_NONE;
+    const Tensor by_r = has_r ? grads[0] : Tensor(), by_h = has_h ? grads[has_r ? 1 : 0] : Tensor();
+    variable_list out(15);
+    if (!by_r.defined() && !by_h.defined()) return out;
+    // An h that nothing came of: the call without its norm, whose 1 / deviation may be infinite (eps 0, a row of zeros) and not times 0.
+    auto of_h = [&](const Tensor& t) { return by_h.defined() ? or_none(t) : std::nullopt; };
+    const ResidualNorm p(s[0], or_none(s[1]), or_none(s[2]), or_none(s[3]), of_h(s[4]), of_h(s[5]), of_h(s[6]), of_h(s[7]), k[0],
+                         by_h.defined() ? k[1] : (int64_t)MOGA_NORM_NONE, f[0], k[2] ? std::optional<int64_t>(k[2]) : std::nullopt, f[1], type);
     auto rows = [&](const Tensor& t) { return t.defined() ? OptTensor(aligned(t.contiguous().view(p.x.sizes()))) : std::nullopt; };
-    const bool has_r = p.y.has_value(), has_h = p.pre != MOGA_NORM_NONE;
-    const OptTensor d_r = has_r ? rows(grads[0]) : std::nullopt;
-    OptTensor d_h = has_h ? rows(grads[has_r ? 1 : 0]) : std::nullopt;
-    if (has_h && !d_h) d_h = at::zeros(p.x.sizes(), p.x.options().dtype(type));
     // inputs are counted without those that are absent
     bool params = false;
     for (size_t i = 2, at = s[1].defined() ? 2 : 1; i < 8; ++i)
       if (s[i].defined()) params = ctx->needs_input_grad(at++) || params;
-    auto [d_x, d_y, d_gate, d_post, d_w, d_b, d_scale, d_shift] = residual_norm_bwd(p, d_r, d_h, s[8], params, std::nullopt);
-    variable_list out(15);
+    auto [d_x, d_y, d_gate, d_post, d_w, d_b, d_scale, d_shift] = residual_norm_bwd(p, rows(by_r), rows(by_h), s[8], params, std::nullopt);
     out[0] = d_x.view(sizes);
     if (d_y) out[1] = d_y->view(sizes);
     out[2] = or_empty(d_gate), out[3] = or_empty(d_post), out[4] = or_empty(d_w), out[5] = or_empty(d_b), out[6] = or_empty(d_scale);
     out[7] = or_empty(d_shift);
+    if (params && !by_h.defined())
+      for (int i = 4; i < 8; ++i)
+        if (s[i].defined()) out[i] = at::zeros_like(s[i]);
     return first_only(out, grads);
   }
 };

@@ -209,6 +209,39 @@ def test_autograd():
         (g.square().sum() + x.square().sum()).backward()
 
 
+@pytest.mark.parametrize("post", ["none", "rms"])
+def test_an_output_that_nothing_comes_of(post):
+    """r alone: its gradients are those of the call without a norm of r, also where that norm divides by 0 (eps 0, r = 0); the parameters of h have zeros."""
+    t, p = _inputs(12, 72, F32, F32, 2, absent=() if post == "rms" else ("post_weight",), each=5)
+    t["x"][4], p["gate"][0] = 0, 0   # tokens 0 .. 4 go by row 0
+    leaves = {k: v.clone().requires_grad_() for k, v in dict(x=t["x"], y=t["y"], **{k: v for k, v in p.items() if v is not None}).items()}
+    r, h = residual_norm(**leaves, post=post, pre="layer", tokens_per_row=5, eps=0.0)
+    assert (r[4] == 0).all() and h[4].isnan().all()
+    grads = dict(zip(leaves, torch.autograd.grad(r, list(leaves.values()), t["d_r"])))
+    how = dict(y=t["y"], gate=p["gate"], post_weight=p["post_weight"], post=post, pre="none", tokens_per_row=5, eps=0.0)
+    _, _, stats = mg.moga_residual_norm_fwd(t["x"], **how)
+    want = mg.moga_residual_norm_bwd(t["d_r"], None, t["x"], stats, **how)
+    for k, g in grads.items():
+        assert torch.equal(g, torch.zeros_like(leaves[k]) if k in ("weight", "bias", "scale", "shift") else getattr(want, "d_" + k)), k
+
+
+def test_outputs_that_nothing_comes_of():
+    class Stop(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, t):
+            return t.clone()
+
+        @staticmethod
+        def backward(ctx, g):
+            return None
+
+    x = torch.zeros((3, 72), device="cuda", requires_grad=True)
+    w = torch.ones(72, device="cuda", requires_grad=True)
+    r, h = residual_norm(x, x * 0, weight=w, pre="rms", eps=0.0)
+    (x.sum() + Stop.apply(r).sum() + Stop.apply(h).sum()).backward()
+    assert (x.grad == 1).all() and w.grad is None
+
+
 def test_refuses():
     t, p = _inputs(8, 64, F32, BF, 1, each=4)
     how = dict(y=t["y"], **p, post="rms", pre="layer", tokens_per_row=4)
