@@ -605,7 +605,8 @@ int moga_residual_norm_bwd(const moga_residual_norm* args, const float* stats, c
 /*
  * Gated feed-forward:  [a, u] = x W_in^T,  h = act(a) * u,  y = h W_out^T
  * x, y [N, C], w_in [2 F, C] (the F rows of a, then the F rows of u), w_out [C, F], h [N, F]; all of dtype F32 or BF16, C <= 65536 and F <= 262144
- * multiples of 8 (F32: of 4), N < 2^31.  act: silu a / (1 + e^-a), gelu a (1 + erf(a / sqrt 2)) / 2, or gelu's tanh form.
+ * multiples of 8 (F32: of 4), N < 2^31 and, in launches of fewer than 2^32 threads, ceil(N / 256) times the greater of ceil(F / 128) and ceil(C / 256) below
+ * 2^23 - 2^13 (F32: ceil(N / 128), ceil(F / 64), ceil(C / 128) and 2^24 - 2^14), an h of some 500 GB.  act: silu a / (1 + e^-a), gelu a (1 + erf(a / sqrt 2)) / 2, or gelu's tanh form.
  * h is written in any case (the second product reads it); au for a backward, else NULL: [N, 2 F] = [a, u], and of BF16 behind it [N, F / 2] bytes, two
  * more bits of each a and u (4.5 N F bytes in all, F32 8 N F).  fp32 sums; h is taken from the unrounded a and u, and a, u, h and y are rounded once.
  * Results repeat bit by bit.  Workspace: MOGA_OP_GATED_FFN_FWD.

@@ -746,6 +746,7 @@ bool few_tokens(int64_t N, int C, int F, int dtype) {
 // x 4096 alone, 192 tiles of 256 x 256: in four splits 637 + 37, whole 706.
 struct TileShape {
   int bm, bn, resident;       // rows and columns; blocks on the chip at a time
+  int threads() const { return bn * 2; }
   // microseconds: a step of bf16 and of fp32 with all of them running, a block's start and end, what writing a split's sums adds to it
   double step, step32, ends, sums;
 };
@@ -756,6 +757,7 @@ struct Cut {
   int64_t k_each;
   unsigned whole, left;
   double cost;
+  bool fits() const { return splits > 0; }   // a launch of fewer than 2^32 threads
   size_t part_bytes() const { return splits > 1 ? (size_t)splits * left * kTiles[shape].bm * kTiles[shape].bn * sizeof(float) : 0; }
 };
 struct Size {
@@ -764,7 +766,8 @@ struct Size {
   unsigned tiles_n(const TileShape& t, Kind kind) const { return (unsigned)ceil_div(N, kind == kGated ? t.bn / 2 : t.bn); }
 };
 
-// Of one product, or of several of the same k in one list of tiles.
+constexpr int kMostSplits = 32;
+// Of one product, or of several of the same k in one list of tiles; of no shape (fits()) where none does.
 Cut cut_of(std::initializer_list<Size> sizes, int64_t K, int dtype, Kind kind) {
   const int bk = dtype == MOGA_F32 ? 32 : 64;
   const int64_t steps = ceil_div(K, bk);
@@ -774,8 +777,9 @@ Cut cut_of(std::initializer_list<Size> sizes, int64_t K, int dtype, Kind kind) {
     const double step = dtype == MOGA_F32 ? t.step32 : t.step, mb = t.bm * t.bn * 4e-6;   // a tile's sums in MB
     int64_t tiles = 0;
     for (const Size& size : sizes) tiles += (int64_t)size.tiles_m(t) * size.tiles_n(t, kind);
+    if (!grid_fits(tiles + kMostSplits * t.resident, t.threads())) continue;
     const int64_t whole = tiles / t.resident * t.resident, left = tiles - whole;
-    for (int s = 1; s <= 32; ++s) {
+    for (int s = 1; s <= kMostSplits; ++s) {
       const int64_t each = ceil_div(steps, s);
       if (s > 1 && (left == 0 || each < 4 || ceil_div(steps, each) != s)) continue;
       double cost = whole / t.resident * (steps * step + t.ends);
@@ -824,7 +828,7 @@ void launch_product(Product<T> p, int dtype, void* part, hipStream_t st) {
 template <typename T, bool AK, bool BK>
 void launch_two(Product<T> p, Product<T> q, int dtype, void* part, hipStream_t st) {
   const Cut c = cut_of({{p.M, p.N}, {q.M, q.N}}, p.K, dtype, kPlain);
-  if (c.cost >= cut_of(p.M, p.N, p.K, dtype, kPlain).cost + cut_of(q.M, q.N, q.K, dtype, kPlain).cost) {
+  if (!c.fits() || c.cost >= cut_of(p.M, p.N, p.K, dtype, kPlain).cost + cut_of(q.M, q.N, q.K, dtype, kPlain).cost) {
     launch_product<T, kPlain, AK, BK>(p, dtype, part, st);
     return launch_product<T, kPlain, AK, BK>(q, dtype, part, st);
   }
@@ -922,16 +926,19 @@ void ffn_bwd(const void* d_y, const void* x, const void* w_in, const void* w_out
   else if (d_w_out) launch_product<T, kPlain, true, true>(w_out_grad, dtype, part, st);
 }
 
-int check_ffn(int64_t N, int C, int F, int dtype, int act) {
+int check_ffn(int64_t N, int C, int F, int dtype, int act, bool backward) {
   if (N < 0 || C < 1 || F < 1) return MOGA_ERR_INVALID_ARG;
   if (dtype != MOGA_F32 && dtype != MOGA_BF16) return MOGA_ERR_UNSUPPORTED;
   if (act != MOGA_ACT_SILU && act != MOGA_ACT_GELU && act != MOGA_ACT_GELU_TANH) return MOGA_ERR_UNSUPPORTED;
   const int v = dtype == MOGA_F32 ? 4 : 8;
   if (C % v || F % v || C > kFfnMaxC || F > kFfnMaxF || N >= ((int64_t)1 << 31)) return MOGA_ERR_UNSUPPORTED;
-  // blocks of the largest grids, and bytes of 256 rows within 31 bits
-  const int64_t most = std::max({ceil_div(N, 64) * ceil_div(F, 64), ceil_div(N, 64) * ceil_div(C, 128),
-                                 ceil_div(2 * (int64_t)F, 64) * ceil_div(C, 128) + ceil_div(C, 64) * ceil_div(F, 128)});
-  return grid_fits(most + 32 * 768, 512) ? MOGA_OK : MOGA_ERR_UNSUPPORTED;
+  const int64_t F2 = 2 * (int64_t)F;
+  // sizes whose smallest tiles fit, whichever are taken, else those that are
+  const int64_t most = std::max({ceil_div(N, 64) * ceil_div(F, 64), ceil_div(N, 64) * ceil_div(C, 128), ceil_div(F2, 64) * ceil_div(C, 128), ceil_div(C, 64) * ceil_div(F, 128)});
+  if (grid_fits(most + kMostSplits * 768, 512)) return MOGA_OK;
+  const auto fits = [&](int64_t M, int64_t n, int64_t K, Kind kind) { return cut_of(M, n, K, dtype, kind).fits(); };
+  if (backward) return fits(N, F, C, kGatedBwd) && fits(N, C, F2, kPlain) && fits(F2, C, N, kPlain) && fits(C, F, N, kPlain) ? MOGA_OK : MOGA_ERR_UNSUPPORTED;
+  return fits(N, F, C, kGated) && fits(N, C, F, kPlain) ? MOGA_OK : MOGA_ERR_UNSUPPORTED;
 }
 
 }  // namespace
@@ -940,15 +947,15 @@ int check_ffn(int64_t N, int C, int F, int dtype, int act) {
 using namespace moga;
 
 extern "C" size_t moga_gated_ffn_fwd_ws_bytes(int64_t N, int C, int F, int dtype) {
-  return check_ffn(N, C, F, dtype, MOGA_ACT_SILU) == MOGA_OK && N > 0 ? ffn_fwd_ws(N, C, F, dtype) : 0;
+  return check_ffn(N, C, F, dtype, MOGA_ACT_SILU, false) == MOGA_OK && N > 0 ? ffn_fwd_ws(N, C, F, dtype) : 0;
 }
 extern "C" size_t moga_gated_ffn_bwd_ws_bytes(int64_t N, int C, int F, int dtype) {
-  return check_ffn(N, C, F, dtype, MOGA_ACT_SILU) == MOGA_OK && N > 0 ? ffn_bwd_ws(N, C, F, dtype) : 0;
+  return check_ffn(N, C, F, dtype, MOGA_ACT_SILU, true) == MOGA_OK && N > 0 ? ffn_bwd_ws(N, C, F, dtype) : 0;
 }
 
 extern "C" int moga_gated_ffn_fwd(const void* x, const void* w_in, const void* w_out, int dtype, int64_t N, int C, int F, int activation, void* h,
                                   void* au, void* y, void* ws, size_t ws_bytes, void* stream) {
-  const int bad = check_ffn(N, C, F, dtype, activation);
+  const int bad = check_ffn(N, C, F, dtype, activation, false);
   if (bad) return bad;
   if (N == 0) return MOGA_OK;
   if (!x || !w_in || !w_out || !h || !y) return MOGA_ERR_INVALID_ARG;
@@ -965,7 +972,7 @@ extern "C" int moga_gated_ffn_fwd(const void* x, const void* w_in, const void* w
 extern "C" int moga_gated_ffn_bwd(const void* d_y, const void* x, const void* w_in, const void* w_out, const void* au, const void* h, int dtype,
                                   int64_t N, int C, int F, int activation, void* d_x, void* d_w_in, void* d_w_out, void* ws, size_t ws_bytes,
                                   void* stream) {
-  const int bad = check_ffn(N, C, F, dtype, activation);
+  const int bad = check_ffn(N, C, F, dtype, activation, true);
   if (bad) return bad;
   if (!(aligned16(d_y) && aligned16(x) && aligned16(w_in) && aligned16(w_out) && aligned16(au) && aligned16(h) && aligned16(d_x) &&
         aligned16(d_w_in) && aligned16(d_w_out) && aligned16(ws)))

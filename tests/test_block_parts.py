@@ -133,6 +133,19 @@ def test_gated_ffn_refuses():
     assert bwd(dx=None, dwi=None, dwo=None, p=None) == 0 and bwd(N=0, dwi=None, dwo=None, p=None) == 0
 
 
+def test_gated_ffn_takes_what_fits_a_launch():
+    """x is not there: -1 for sizes that are taken, -2 for others."""
+    fwd = lambda N, C, F, dt: mg.load().moga_gated_ffn_fwd(None, FAKE, FAKE, dt, N, C, F, 0, FAKE, None, FAKE, FAKE, 1 << 40, None)
+    bwd = lambda N, C, F, dt: mg.load().moga_gated_ffn_bwd(None, FAKE, FAKE, FAKE, FAKE, FAKE, dt, N, C, F, 0, FAKE, None, None, FAKE, 1 << 60, None)
+    for call in (fwd, bwd):
+        assert call(4000000, 5120, 13696, 1) == -1 and call(4000000, 5120, 13696, 0) == -1
+        for dt, rows, most in ((1, 256, 2 ** 23 - 2 ** 13), (0, 128, 2 ** 24 - 2 ** 14)):
+            assert call(rows * (most - 1), 8, 8, dt) == -1 and call(rows * most, 8, 8, dt) == -2
+            assert call((1 << 31) - 1, 65536, 8, dt) == -2 and call((1 << 31) - 1, 8, 262144, dt) == -2
+        assert call((1 << 31) - 1, 512, 1368, 1) == -2 and call(1, 65536, 262144, 1) == -1
+    assert mg.workspace_bytes(mg.OP_GATED_FFN_BWD, 4000000, 0, 13696, 1, 5120, 1) >= 4000000 * 2 * 13696 * 2
+
+
 def test_gated_ffn_workspace():
     wb = lambda op, N, C, F, dt: mg.workspace_bytes(op, N, 0, F, 1, C, dt)
     for op in (mg.OP_GATED_FFN_FWD, mg.OP_GATED_FFN_BWD):

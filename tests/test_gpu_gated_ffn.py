@@ -163,6 +163,22 @@ def test_parts_of_the_backward():
     assert mg.moga_gated_ffn_bwd(dy, x, wi, wo, au, h, want_dx=False, want_dw_in=False, want_dw_out=False) == (None, None, None)
 
 
+def test_half_a_billion_tokens():
+    """537,001,792 tokens, millions of blocks and tensors of more than 2^32 values.  The same rows over and over have the same results over and over (each sum
+    is one step of k, whatever the tiles)."""
+    n, times, C, F = 4099, 131008, 8, 8
+    x, wi, wo, dy = _inputs(n, C, F, BF, 5)
+    y0, au0, h0 = mg.moga_gated_ffn_fwd(x, wi, wo)
+    d0 = mg.moga_gated_ffn_bwd(dy, x, wi, wo, au0, h0, want_dw_in=False, want_dw_out=False)[0]
+    many = lambda t: t.repeat(times, 1)
+    big = many(x)
+    y, au, h = mg.moga_gated_ffn_fwd(big, wi, wo)
+    d = mg.moga_gated_ffn_bwd(many(dy), big, wi, wo, au, h, want_dw_in=False, want_dw_out=False)[0]
+    for got, want in ((y, y0), (h, h0), (au[:2 * n * times * F].view(-1, 2 * F), au0[:2 * n * F].view(n, 2 * F)), (d, d0)):
+        got, want = got.view(times, -1).view(torch.int64), want.reshape(-1).view(torch.int64)
+        assert all((got[i:i + 4096] == want).all() for i in range(0, times, 4096))
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_no_tokens(dtype):
     x, wi, wo, dy = _inputs(0, 16, 24, dtype, 1)
