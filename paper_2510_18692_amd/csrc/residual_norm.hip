@@ -685,10 +685,12 @@ extern "C" int moga_residual_norm_fwd(const moga_residual_norm* a, void* r, void
 }
 
 // M: rows of gate, scale and shift.  deal() makes no more pieces than this: all but the last of each row are of bwd_least tokens a lane group or more.
+// Fewer tokens need no more bytes, though bwd_least falls with them: pieces of k - 1 tokens are 64 (k - 1) at most.
 extern "C" size_t moga_residual_norm_bwd_ws_bytes(int64_t N, int M, int C) {
   if (N <= 0 || M < 1 || M > N || C < 1 || C > kNormMaxC || N >= ((int64_t)1 << 31)) return 0;
   const Shape s = shape_of(C);
-  const int64_t items = M + std::min<int64_t>(4 * blocks_of(s, kBwdWaves), N / (s.rows * bwd_least(N, s)));
+  const int least = bwd_least(N, s);
+  const int64_t items = M + std::min<int64_t>(4 * blocks_of(s, kBwdWaves), std::max<int64_t>(N / (s.rows * least), 64 * (least - 1)));
   return ((size_t)items + kOverGroups) * 3 * C * sizeof(float);
 }
 

@@ -108,6 +108,15 @@ def test_residual_norm_workspace():
     assert wb(100000, 1000, 5120) > wb(100000, 1, 5120)
 
 
+@pytest.mark.parametrize("C", [24, 96, 300, 512, 520, 1536, 5120, 16384])
+def test_residual_norm_workspace_grows_with_the_tokens(C):
+    """Room for the longest call is room for every shorter one, with one row of the gate or rows of as many tokens."""
+    wb = lambda N, M: mg.workspace_bytes(mg.OP_RESIDUAL_NORM_BWD, N, 0, 0, M, C, 1)
+    for each in (1 << 40, 1000, 97, 1):
+        sizes = [wb(N, -(-N // each)) for N in [*range(1, 5000), *range(5000, 300000, 331)]]
+        assert sizes == sorted(sizes), each
+
+
 def test_gated_ffn_refuses():
     fwd = lambda x=FAKE, wi=FAKE, wo=FAKE, dt=1, N=4, C=64, F=32, act=0, h=FAKE, au=FAKE, y=FAKE, p=FAKE, n=1 << 40: mg.load().moga_gated_ffn_fwd(
         x, wi, wo, dt, N, C, F, act, h, au, y, p, n, None)
