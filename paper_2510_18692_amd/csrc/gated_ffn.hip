@@ -767,30 +767,78 @@ struct Size {
 };
 
 constexpr int kMostSplits = 32;
+double step_of(const TileShape& t, int dtype) { return dtype == MOGA_F32 ? t.step32 : t.step; }
+int steps_of(int64_t K, int dtype) { return (int)ceil_div(K, dtype == MOGA_F32 ? 32 : 64); }
+int first_shape(int dtype) { return dtype == MOGA_F32 ? 1 : 0; }
+
+// Splits of the tiles behind the last whole round.
+struct Splits {
+  int s;
+  double cost;
+};
+Splits splits_of(const TileShape& t, int64_t left, int64_t steps, double step) {
+  Splits best{};
+  const double mb = t.bm * t.bn * 4e-6;   // a tile's sums in MB
+  for (int s = 1; s <= kMostSplits; ++s) {
+    const int64_t each = ceil_div(steps, s);
+    if (s > 1 && (left == 0 || each < 4 || ceil_div(steps, each) != s)) continue;
+    double cost = left ? ceil_div(left * s, t.resident) * (each * step + t.ends) : 0;
+    if (s > 1) cost += 5 + ceil_div(left * s, t.resident) * t.sums + left * s * mb * 0.27;
+    if (best.s == 0 || cost < best.cost) best = {s, cost};
+  }
+  return best;
+}
+
 // Of one product, or of several of the same k in one list of tiles; of no shape (fits()) where none does.
 Cut cut_of(std::initializer_list<Size> sizes, int64_t K, int dtype, Kind kind) {
   const int bk = dtype == MOGA_F32 ? 32 : 64;
-  const int64_t steps = ceil_div(K, bk);
+  const int64_t steps = steps_of(K, dtype);
   Cut best{};
-  for (int shape = dtype == MOGA_F32 ? 1 : 0; shape < 3; ++shape) {
+  for (int shape = first_shape(dtype); shape < 3; ++shape) {
     const TileShape& t = kTiles[shape];
-    const double step = dtype == MOGA_F32 ? t.step32 : t.step, mb = t.bm * t.bn * 4e-6;   // a tile's sums in MB
+    const double step = step_of(t, dtype);
     int64_t tiles = 0;
     for (const Size& size : sizes) tiles += (int64_t)size.tiles_m(t) * size.tiles_n(t, kind);
     if (!grid_fits(tiles + kMostSplits * t.resident, t.threads())) continue;
     const int64_t whole = tiles / t.resident * t.resident, left = tiles - whole;
-    for (int s = 1; s <= kMostSplits; ++s) {
-      const int64_t each = ceil_div(steps, s);
-      if (s > 1 && (left == 0 || each < 4 || ceil_div(steps, each) != s)) continue;
-      double cost = whole / t.resident * (steps * step + t.ends);
-      if (left) cost += ceil_div(left * s, t.resident) * (each * step + t.ends);
-      if (s > 1) cost += 5 + ceil_div(left * s, t.resident) * t.sums + left * s * mb * 0.27;
-      if (best.splits == 0 || cost < best.cost) best = {shape, s, s > 1 ? each * bk : K, (unsigned)(s > 1 ? whole : tiles), (unsigned)(s > 1 ? left : 0), cost};
-    }
+    const Splits split = splits_of(t, left, steps, step);
+    const double cost = whole / t.resident * (steps * step + t.ends) + split.cost;
+    if (best.splits == 0 || cost < best.cost)
+      best = {shape, split.s, split.s > 1 ? ceil_div(steps, split.s) * bk : K, (unsigned)(split.s > 1 ? whole : tiles), (unsigned)(split.s > 1 ? left : 0), cost};
   }
   return best;
 }
 Cut cut_of(int64_t M, int64_t N, int64_t K, int dtype, Kind kind) { return cut_of({{M, N}}, K, dtype, kind); }
+
+// Bytes of the splits of a product of any number of rows up to M.  Tiles behind the last whole round repeat after `resident` rows of tiles.
+size_t most_part_bytes(int64_t M, int64_t N, int64_t K, int dtype, Kind kind) {
+  size_t most = 0;
+  for (int shape = first_shape(dtype); shape < 3; ++shape) {
+    const TileShape& t = kTiles[shape];
+    const Size size{M, N};
+    for (int64_t m = std::min<int64_t>(size.tiles_m(t), t.resident); m > 0; --m) {
+      const int64_t left = m * size.tiles_n(t, kind) % t.resident;
+      const int s = splits_of(t, left, steps_of(K, dtype), step_of(t, dtype)).s;
+      if (s > 1) most = std::max(most, (size_t)s * left * t.bm * t.bn * sizeof(float));
+    }
+  }
+  return most;
+}
+// Of products of any k up to K: beyond 1,024 steps as for all splits that there are.
+size_t most_part_bytes_k(std::initializer_list<Size> sizes, int64_t K, int dtype) {
+  size_t most = 0;
+  for (int shape = first_shape(dtype); shape < 3; ++shape) {
+    const TileShape& t = kTiles[shape];
+    int64_t tiles = 0;
+    for (const Size& size : sizes) tiles += (int64_t)size.tiles_m(t) * size.tiles_n(t, kPlain);
+    const int64_t left = tiles % t.resident;
+    const int steps = steps_of(K, dtype);
+    int s = left && steps > 1024 ? kMostSplits : 1;
+    for (int k = std::min(steps, 1024); left && k > 0; --k) s = std::max(s, splits_of(t, left, k, step_of(t, dtype)).s);
+    if (s > 1) most = std::max(most, (size_t)s * left * t.bm * t.bn * sizeof(float));
+  }
+  return most;
+}
 
 template <typename T>
 void apply_cut(Product<T>& p, const Cut& c, Kind kind, void* part) {
@@ -909,6 +957,16 @@ size_t ffn_bwd_ws(int64_t N, int C, int F, int dtype) {
                                                cut_of({{F2, C}, {C, F}}, N, dtype, kPlain).part_bytes()});
 }
 
+// What is enough for any number of tokens up to N: the splits of a call depend on how many tiles are behind its last whole round.
+size_t ffn_fwd_room(int64_t N, int C, int F, int dtype) {
+  return std::max({few_part_bytes(std::min<int64_t>(N, kFewTokens), C, F, dtype), most_part_bytes(N, F, C, dtype, kGated), most_part_bytes(N, C, F, dtype, kPlain)});
+}
+size_t ffn_bwd_room(int64_t N, int C, int F, int dtype) {
+  const int64_t F2 = 2 * (int64_t)F;
+  return ffn_bwd_part(N, F, dtype) + std::max({most_part_bytes(N, F, C, dtype, kGatedBwd), most_part_bytes(N, C, F2, dtype, kPlain), most_part_bytes_k({{F2, C}}, N, dtype),
+                                               most_part_bytes_k({{C, F}}, N, dtype), most_part_bytes_k({{F2, C}, {C, F}}, N, dtype)});
+}
+
 template <typename T>
 void ffn_bwd(const void* d_y, const void* x, const void* w_in, const void* w_out, const void* au, const void* h, int dtype, int64_t N, int C, int F,
              int act, void* d_x, void* d_w_in, void* d_w_out, void* ws, hipStream_t st) {
@@ -951,6 +1009,13 @@ extern "C" size_t moga_gated_ffn_fwd_ws_bytes(int64_t N, int C, int F, int dtype
 }
 extern "C" size_t moga_gated_ffn_bwd_ws_bytes(int64_t N, int C, int F, int dtype) {
   return check_ffn(N, C, F, dtype, MOGA_ACT_SILU, true) == MOGA_OK && N > 0 ? ffn_bwd_ws(N, C, F, dtype) : 0;
+}
+
+extern "C" size_t moga_gated_ffn_fwd_preferred(int64_t N, int C, int F, int dtype) {
+  return check_ffn(N, C, F, dtype, MOGA_ACT_SILU, false) == MOGA_OK && N > 0 ? ffn_fwd_room(N, C, F, dtype) : 0;
+}
+extern "C" size_t moga_gated_ffn_bwd_preferred(int64_t N, int C, int F, int dtype) {
+  return check_ffn(N, C, F, dtype, MOGA_ACT_SILU, true) == MOGA_OK && N > 0 ? ffn_bwd_room(N, C, F, dtype) : 0;
 }
 
 extern "C" int moga_gated_ffn_fwd(const void* x, const void* w_in, const void* w_out, int dtype, int64_t N, int C, int F, int activation, void* h,

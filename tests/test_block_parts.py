@@ -163,3 +163,18 @@ def test_gated_ffn_workspace():
     assert wb(mg.OP_GATED_FFN_FWD, 32760, 1536, 4096, 1) == 0               # whole rounds of tiles
     assert max(wb(mg.OP_GATED_FFN_FWD, n, 1536, 4096, 1) for n in range(1, 3000, 37)) <= 32 * 256 * 65536 * 4
     assert wb(mg.OP_GATED_FFN_BWD, 32760, 1536, 4096, 1) >= 32760 * 8192 * 2
+
+
+@pytest.mark.parametrize("dt", [0, 1])
+@pytest.mark.parametrize("C,F", [(8, 8), (128, 8192), (264, 520), (512, 1368), (1536, 4096), (5120, 13696), (72, 4104)])
+def test_gated_ffn_room_for_any_number_of_tokens(C, F, dt):
+    """The preferred bytes grow with the tokens and are enough for every shorter call."""
+    for op in (mg.OP_GATED_FFN_FWD, mg.OP_GATED_FFN_BWD):
+        room = lambda N: mg.load().moga_workspace_preferred_bytes(op, N, 0, 0, F, 1, C, dt)
+        need, last = 0, 0
+        for N in [*range(1, 700), *range(700, 9000, 29), *range(9000, 140000, 1777)]:
+            need = max(need, mg.workspace_bytes(op, N, 0, F, 1, C, dt))
+            if N < 80 or N % 7 == 0:
+                assert need <= room(N) and last <= room(N), (op, N)
+                last = room(N)
+        assert room(100000) <= room(100001) and room(0) == 0
