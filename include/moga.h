@@ -626,6 +626,13 @@ int moga_gated_ffn_bwd(const void* d_y, const void* x, const void* w_in, const v
                        void* stream);
 
 /*
+ * Tests run every kernel of the feed-forward's products at any size: calls of more tokens than go by the weights' rows take tiles of shape 0 (256 x 256, BF16
+ * only, else as 1), 1 (128 x 128) or 2 (64 x 128) in rounds of `round`, those behind the last whole round in `splits` (1 to 32; 1: whole) along k, both
+ * weights' gradients in one launch (together) or two, and moga_workspace_bytes says so.  Anything else: the calls choose again.  Host-only.
+ */
+void moga_debug_set_ffn_tiles(int shape, int round, int splits, int together);
+
+/*
  * Rotary positions.  The first R channels of a head (R even, R <= D; the others are copied) are R / 2 pairs: channels (2 i, 2 i + 1) if
  * interleaved, else (i, i + R / 2).  Pair i of a token at position p is turned by the angle p * inv_freq[i] and multiplied by factor:
  *   y1 = factor * (x1 cos - x2 sin),  y2 = factor * (x2 cos + x1 sin)

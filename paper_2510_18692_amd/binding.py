@@ -61,6 +61,7 @@ _SIGNATURES = {
     "moga_attn_bwd_status_offset": (_sz, [_i64, _i32]),
     "moga_debug_set_spin_limit": (None, [_i32]),
     "moga_debug_set_small_group_rows": (None, [_i64]),
+    "moga_debug_set_ffn_tiles": (None, [_i32, _i32, _i32, _i32]),
     "moga_debug_small_calls": (_i32, [_i32, _i32, _vp, _vp, _i32]),
     "moga_debug_attn_blocks": (None, [_i32, _i64, _i64, _i32, _i32, _sz, _vp]),
     "moga_permute_bwd": (_i32, [_vp, _vp, _vp, _i32, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _vp]),
@@ -278,6 +279,11 @@ def attn_bwd_status(ws, Nq, H):
 def set_small_group_rows(rows: int) -> None:
     """Mean group size below which the bf16 attention calls use their small-group kernels (< 0: defaults)."""
     load().moga_debug_set_small_group_rows(int(rows))
+
+
+def set_ffn_tiles(shape=-1, round=1, splits=1, together=True) -> None:
+    """Tiles of the feed-forward's products (moga_debug_set_ffn_tiles; without arguments: the calls choose)."""
+    load().moga_debug_set_ffn_tiles(int(shape), int(round), int(splits), int(together))
 
 
 def attn_blocks(op, Nq, Nk, H, M, ws_bytes):

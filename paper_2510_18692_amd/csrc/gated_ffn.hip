@@ -7,6 +7,7 @@
 // [a, u] leaves a block's registers once, dh never.  From some hundred tokens on bound by the products (product_kernel), with few tokens by the
 // weights' bytes (few_kernel).  h comes from the unrounded a and u, da and du from a and u as the forward kept them (finer()) and the unrounded dh.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <type_traits>
 
@@ -789,19 +790,35 @@ Splits splits_of(const TileShape& t, int64_t left, int64_t steps, double step) {
   return best;
 }
 
+// Test hook: tiles of one shape, `round` of them to a round, those behind the last whole round in `splits` where k has as many steps, both weights' gradients in
+// one list or not.  In one word, so that a call sees all of it; 0: none.
+struct Forced {
+  int shape, round, splits, together;
+};
+std::atomic<long long> g_forced{0};
+bool forced(Forced& f) {
+  const long long v = g_forced.load();
+  f = {(int)(v & 255) - 1, (int)(v >> 24), (int)(v >> 8 & 255), (int)(v >> 16 & 255)};
+  return v != 0;
+}
+
 // Of one product, or of several of the same k in one list of tiles; of no shape (fits()) where none does.
 Cut cut_of(std::initializer_list<Size> sizes, int64_t K, int dtype, Kind kind) {
   const int bk = dtype == MOGA_F32 ? 32 : 64;
   const int64_t steps = steps_of(K, dtype);
   Cut best{};
+  Forced f;
+  const bool is_forced = forced(f);
   for (int shape = first_shape(dtype); shape < 3; ++shape) {
-    const TileShape& t = kTiles[shape];
+    if (is_forced && shape != std::max(f.shape, first_shape(dtype))) continue;
+    TileShape t = kTiles[shape];
+    if (is_forced) t.resident = f.round;
     const double step = step_of(t, dtype);
     int64_t tiles = 0;
     for (const Size& size : sizes) tiles += (int64_t)size.tiles_m(t) * size.tiles_n(t, kind);
     if (!grid_fits(tiles + kMostSplits * t.resident, t.threads())) continue;
     const int64_t whole = tiles / t.resident * t.resident, left = tiles - whole;
-    const Splits split = splits_of(t, left, steps, step);
+    const Splits split = is_forced ? Splits{left ? (int)ceil_div(steps, ceil_div(steps, f.splits)) : 1, 0.} : splits_of(t, left, steps, step);
     const double cost = whole / t.resident * (steps * step + t.ends) + split.cost;
     if (best.splits == 0 || cost < best.cost)
       best = {shape, split.s, split.s > 1 ? ceil_div(steps, split.s) * bk : K, (unsigned)(split.s > 1 ? whole : tiles), (unsigned)(split.s > 1 ? left : 0), cost};
@@ -876,7 +893,8 @@ void launch_product(Product<T> p, int dtype, void* part, hipStream_t st) {
 template <typename T, bool AK, bool BK>
 void launch_two(Product<T> p, Product<T> q, int dtype, void* part, hipStream_t st) {
   const Cut c = cut_of({{p.M, p.N}, {q.M, q.N}}, p.K, dtype, kPlain);
-  if (!c.fits() || c.cost >= cut_of(p.M, p.N, p.K, dtype, kPlain).cost + cut_of(q.M, q.N, q.K, dtype, kPlain).cost) {
+  Forced f;
+  if (forced(f) ? !f.together : !c.fits() || c.cost >= cut_of(p.M, p.N, p.K, dtype, kPlain).cost + cut_of(q.M, q.N, q.K, dtype, kPlain).cost) {
     launch_product<T, kPlain, AK, BK>(p, dtype, part, st);
     return launch_product<T, kPlain, AK, BK>(q, dtype, part, st);
   }
@@ -1003,6 +1021,11 @@ int check_ffn(int64_t N, int C, int F, int dtype, int act, bool backward) {
 }  // namespace moga
 
 using namespace moga;
+
+extern "C" void moga_debug_set_ffn_tiles(int shape, int round, int splits, int together) {
+  const bool on = shape >= 0 && shape < 3 && round > 0 && splits > 0 && splits <= kMostSplits;
+  g_forced.store(on ? (long long)round << 24 | (together ? 1 : 0) << 16 | splits << 8 | (shape + 1) : 0);
+}
 
 extern "C" size_t moga_gated_ffn_fwd_ws_bytes(int64_t N, int C, int F, int dtype) {
   return check_ffn(N, C, F, dtype, MOGA_ACT_SILU, false) == MOGA_OK && N > 0 ? ffn_fwd_ws(N, C, F, dtype) : 0;
