@@ -27,7 +27,7 @@ extern "C" const char* moga_status_string(int status) {
   }
 }
 
-extern "C" int moga_version(void) { return 107; }
+extern "C" int moga_version(void) { return 108; }
 
 // Test hook: overrides the mean group size below which the bf16 attention calls pick their
 // small-group kernels (negative: each call's own default).

@@ -5,7 +5,8 @@
 //
 // Six matrix products, 6 N C F operations forward and 12 N C F backward, the activation and its derivative in the epilogues of the two that make h and dh:
 // [a, u] leaves a block's registers once, dh never.  From some hundred tokens on bound by the products (product_kernel), with few tokens by the
-// weights' bytes (few_kernel).  h comes from the unrounded a and u, da and du from a and u as the forward kept them (finer()) and the unrounded dh.
+// weights' bytes (few_kernel).  h comes from the unrounded a and u, da and du from a and u as the forward kept them (finer()) and the unrounded dh;
+// the three are rounded to the inputs' type once, as operands of the next product.
 #include <algorithm>
 #include <atomic>
 #include <cmath>

@@ -41,7 +41,7 @@ __device__ __forceinline__ unsigned short f32_to_bf16_bits(float f) {
   return (unsigned short)(pack_bf16x2(f, 0.f) & 0xffffu);
 }
 
-// Butterfly reductions over L = 16, 32 or 64 neighbouring lanes (distances L / 2 .. 1) with cross-lane data paths of the vector
+// Butterfly reductions over L = 8, 16, 32 or 64 neighbouring lanes (distances L / 2 .. 1) with cross-lane data paths of the vector
 // unit.  (__shfl_xor goes through LDS, some 120 cycles a step: the fp32 router at 4,096 x 128, 8 groups and the row sums of the
 // scatter backward wait for little else.)  All L lanes are active.
 template <int CTRL>
