@@ -597,7 +597,8 @@ ResNorm make(const moga_residual_norm* a) {
           a->residual_scale, a->eps, 1, 1, 1};
 }
 constexpr int kFwdWaves = 24, kBwdWaves = 12;   // of a CU
-// Tokens of a lane group and piece, of the backward: a piece's tokens take their turns, and so do 64 pieces whose sums are added up.
+// Tokens of a lane group and piece, of the backward: a piece's tokens take their turns, and so do the pieces whose sums are added up, 64 at a time.  With
+// k tokens of each of a block's s.rows lane groups that is k turns and N / (64 k s.rows) turns, fewest in all where the two are alike: k^2 = N / (64 s.rows).
 // Few tokens go in shorter pieces: bf16, us with one row of the gate, pieces of 8 tokens and these: C 5120, 8 tokens 26 and 10, 300 31 and 22, 1,560 37 and 35;
 // C 512, 63 tokens 24 and 9, 3,000 19 and 17, 8,000 23 and 25.
 int bwd_least(int64_t N, const Shape& s) {
